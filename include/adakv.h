@@ -298,6 +298,136 @@ int adakv_decode_step(const adakv_layer *L, const void *q_new, const void *k_new
                       float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * ---- Attention limited to a window and a few first tokens -----------------------------------
+ *
+ * A row sees the keys no more than window - 1 places before it and, however far back, the first
+ * `sinks` ones.  window >= 1, sinks >= 0 (else ADAKV_EINVAL); a window as long as the sequence
+ * leaves all of it visible.
+ */
+
+/*
+ * Causal attention over the prompts: for sequence b, its N_b = n_b + w rows and query head i, row r
+ *
+ *     out[tok_off[b] + r][i][:] = sum_j softmax_j(scale * q[tok_off[b] + r][i] . K[tok_off[b] + j][i / g]) V[tok_off[b] + j][i / g][:]
+ *
+ * over the visible j: j <= r and (j > r - window or j < sinks).  row_lse[b][i][k] is the natural log of the
+ * same sum of exp for row r = n_b + k, as adakv_score takes it.  Logits and sums are accumulated in
+ * fp32; 16-bit layers round the softmax weights to their type for the second product.  Keys and
+ * values that a row does not see have no part in its result, infinities and NaN included.
+ * Of L the call uses dtype, h_q, h_kv, d, w, batch, n, tok_off, scale and the strides.
+ *
+ *   q        (device) rows as K's; element (row, i, e) at row*q_stride_tok + i*q_stride_head + e, both
+ *                     strides >= d and rows 16-byte aligned
+ *   K, V     (device) strided as in the layer, rows 16-byte aligned
+ *   out      (device) [rows][h_q][d] contiguous, L->dtype, 16-byte aligned; rows of no sequence stay as they are
+ *   row_lse  (device) [batch][h_q][w] fp32, written; may be NULL
+ * Supported (else ADAKV_EUNSUPPORTED): up to 2^28 rows a sequence; at most 2^32 rows times query heads in
+ * all, each sequence's rows counted in 64s.
+ */
+int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
+                      int64_t q_stride_head, const void *K, const void *V, int32_t window,
+                      int32_t sinks, void *out, float *row_lse, void *hip_stream);
+
+/*
+ * adakv_decode_attn and adakv_decode_step over a segment's visible rows: with len rows held (the
+ * appended one included) those are t < sinks and t >= len - window.  Arguments as for the two calls; a
+ * workspace of adakv_decode_workspace_bytes(L, headroom) bytes does.
+ */
+int adakv_decode_window_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
+                             int32_t headroom, const void *K_cache, const void *V_cache,
+                             const int32_t *seg_len, int32_t window, int32_t sinks, float *out,
+                             float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void *k_new,
+                             const void *v_new, const int32_t *cu_seqlens, int32_t headroom,
+                             void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow,
+                             int32_t window, int32_t sinks, float *out, float *lse, void *ws,
+                             size_t ws_bytes, void *hip_stream);
+
+/*
+ * ---- The decode-side cache in 8 bits ----------------------------------------------------------
+ *
+ * K_q8 and V_q8 have the layout of K_cache and V_cache with one byte an element: an e4m3 number (the
+ * format without infinities: largest 448, NaN 0x7f) that stands for itself times the scale of its block.
+ * A block is ADAKV_Q8_BLOCK rows of a segment, counted from the segment's first row; block j of
+ * segment s has its scales at
+ *
+ *     k_scale[start_s / ADAKV_Q8_BLOCK + s + j],  v_scale likewise    (start_s as above, division rounding down)
+ *
+ * in arrays of adakv_q8_scales(L, headroom) floats.  A scale is a power of two 2^k: the smallest with
+ * every finite magnitude of the block <= 448 * 2^k, but not below 2^-60 or above 2^100.  Values are rounded to
+ * nearest, halves to even; beyond 448 * 2^100 they saturate, and what is no finite number is stored
+ * as NaN.  L->dtype is the type of K, V, q_new, k_new and v_new.
+ */
+#define ADAKV_Q8_BLOCK 32
+/* Floats in k_scale and in v_scale (0 on invalid input). */
+size_t adakv_q8_scales(const adakv_layer *L, int32_t headroom);
+
+/* adakv_cache_build into an 8-bit cache.  Arguments as there; K_q8, V_q8 16-byte aligned. */
+int adakv_cache_build_q8(const adakv_layer *L, const void *K, const void *V,
+                         const int32_t *indices, const int32_t *cu_seqlens, int32_t headroom,
+                         void *K_q8, void *V_q8, float *k_scale, float *v_scale, int32_t *seg_len,
+                         void *hip_stream);
+
+/*
+ * adakv_append to an 8-bit cache.  A row that begins a block sets its scale.  In a block with rows
+ * the scale stays if it is large enough for the new row; else the block takes the new row's scale and its
+ * earlier rows are rounded again to it (exact but for magnitudes below 2^-6 of the new scale).
+ */
+int adakv_append_q8(const adakv_layer *L, const void *k_new, const void *v_new,
+                    const int32_t *cu_seqlens, int32_t headroom, void *K_q8, void *V_q8,
+                    float *k_scale, float *v_scale, int32_t *seg_len, int32_t *overflow,
+                    void *hip_stream);
+
+/*
+ * adakv_decode_attn and adakv_decode_step over an 8-bit cache: the attention of q_new over the values
+ * that the cache stands for, accumulated in fp32 (the appended row is attended as it was stored).
+ *   ws (device) adakv_decode_workspace_bytes(L, headroom) bytes
+ */
+int adakv_decode_attn_q8(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
+                         int32_t headroom, const void *K_q8, const void *V_q8,
+                         const float *k_scale, const float *v_scale, const int32_t *seg_len,
+                         float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int adakv_decode_step_q8(const adakv_layer *L, const void *q_new, const void *k_new,
+                         const void *v_new, const int32_t *cu_seqlens, int32_t headroom,
+                         void *K_q8, void *V_q8, float *k_scale, float *v_scale, int32_t *seg_len,
+                         int32_t *overflow, float *out, float *lse, void *ws, size_t ws_bytes,
+                         void *hip_stream);
+
+/*
+ * ---- Sequences of a decode-side cache, moved ---------------------------------------------------
+ *
+ * A cache of `count` sequences, of which sequence i is sequence from[i] of L's as it stands: its segments'
+ * rows, lengths and capacities, with headroom_out spare rows behind every segment.  A sequence named
+ * twice is forked, one that is not named is dropped; a larger head-room gives full segments room
+ * again.  The result is the cache of a layer with n and B of the named sequences, in that order.
+ *
+ *     cu_out[i*h_kv + c + 1] - cu_out[i*h_kv + c] = cu_seqlens[s + 1] - cu_seqlens[s],  s = from[i]*h_kv + c
+ *     len_out[i*h_kv + c] = min(seg_len[s], capacity there); if that is less than seg_len[s], the rows behind
+ *                           are left out and *overflow is set to 1 (it is never cleared)
+ *
+ * Rows that no segment holds are not written.  Source and destination must not overlap (ADAKV_EINVAL).
+ *
+ *   from     (host) [count], each in [0, batch); 1 <= count <= ADAKV_MAX_BATCH
+ *   cu_out   (device) [count*h_kv + 1] int32, written; len_out (device) [count*h_kv] int32, written
+ *   K_out, V_out (device) [sum_i B[from[i]] + count*h_kv*headroom_out][d], L->dtype, 16-byte aligned; below
+ *                2^31 rows (else ADAKV_EUNSUPPORTED)
+ *   overflow (device) one int32, or NULL
+ */
+int adakv_cache_move(const adakv_layer *L, int32_t count, const int32_t *from,
+                     const int32_t *cu_seqlens, int32_t headroom, const void *K_cache,
+                     const void *V_cache, const int32_t *seg_len, int32_t headroom_out,
+                     int32_t *cu_out, void *K_out, void *V_out, int32_t *len_out,
+                     int32_t *overflow, void *hip_stream);
+
+/* The same for a cache in 8 bits: rows and scales. */
+int adakv_cache_move_q8(const adakv_layer *L, int32_t count, const int32_t *from,
+                        const int32_t *cu_seqlens, int32_t headroom, const void *K_q8,
+                        const void *V_q8, const float *k_scale, const float *v_scale,
+                        const int32_t *seg_len, int32_t headroom_out, int32_t *cu_out,
+                        void *K_out, void *V_out, float *k_scale_out, float *v_scale_out,
+                        int32_t *len_out, int32_t *overflow, void *hip_stream);
+
+/*
  * Layer budgets for the pyramidal variant (Section 3.4: Ada-Pyramid differs from Ada-SnapKV only
  * in how the total budget is spread over the layers, "via pre-set hyper-parameters" that the
  * paper does not give; inside a layer the algorithm is the same).  Host arithmetic only.  The

@@ -10,6 +10,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -83,6 +84,21 @@ def load_library():
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args
+    L64 = ctypes.c_int64
+    for name, args in (("adakv_window_attn", [P, V, L64, L64, V, V, I, I, V, V, V]),
+                       ("adakv_decode_window_attn", [P, V, V, I, V, V, V, I, I, V, V, V, Z, V]),
+                       ("adakv_decode_window_step", [P, V, V, V, V, I, V, V, V, V, I, I, V, V, V, Z, V]),
+                       ("adakv_cache_build_q8", [P, V, V, V, V, I, V, V, V, V, V, V]),
+                       ("adakv_append_q8", [P, V, V, V, I, V, V, V, V, V, V, V]),
+                       ("adakv_decode_attn_q8", [P, V, V, I, V, V, V, V, V, V, V, V, Z, V]),
+                       ("adakv_decode_step_q8", [P, V, V, V, V, I, V, V, V, V, V, V, V, V, V, Z, V]),
+                       ("adakv_cache_move", [P, I, V, V, I, V, V, V, I, V, V, V, V, V, V]),
+                       ("adakv_cache_move_q8", [P, I, V, V, I, V, V, V, V, V, I, V, V, V, V, V, V, V, V])):
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = args
+    lib.adakv_q8_scales.restype = Z
+    lib.adakv_q8_scales.argtypes = [P, I]
     lib.adakv_decode_workspace_bytes.restype = Z
     lib.adakv_decode_workspace_bytes.argtypes = [P, I]
     lib.adakv_pyramid_budgets.restype = ctypes.c_int
@@ -140,6 +156,15 @@ class Layer:
     def from_workload(cls, wl, **kw):
         return cls(wl.dtype, wl.h_q, wl.h_kv, wl.d, wl.w, wl.pool_k, wl.alpha, wl.n, wl.B,
                    tok_off=wl.tok_off, **kw)
+
+    def pick(self, picks) -> "Layer":
+        """The layer of a moved cache: its sequence i is this one's sequence picks[i] (its K and V, if it has any, are
+        packed one after the other)."""
+        if not picks or any(not 0 <= int(b) < self.batch for b in picks):
+            raise ValueError(f"picks must name sequences of the layer, 0 to {self.batch - 1}, one at least")
+        ks, vs = (s if given else None for s, given in zip((self.k_strides, self.v_strides), self.strides_given))
+        return Layer(self.torch_dtype, self.h_q, self.h_kv, self.d, self.w, self.pool_k, self.alpha, [self.n[b] for b in picks],
+                     [self.B[b] for b in picks], scale=self.scale, k_strides=ks, v_strides=vs, flags=int(self.c.flags))
 
     @property
     def last_token_row(self):
@@ -554,8 +579,10 @@ def append(layer: Layer, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, s
 
 
 def decode_attn(layer: Layer, q_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, out=None,
-                lse=None, ws=None, stream=None, want_lse=False):
-    """adakv_decode_attn: out [batch, h_q, d] fp32 (and lse [batch, h_q] if asked for)."""
+                lse=None, ws=None, stream=None, want_lse=False, window=None, sinks=0):
+    """adakv_decode_attn: out [batch, h_q, d] fp32 (and lse [batch, h_q] if asked for).  With a `window`
+    (adakv_decode_window_attn) a segment's last `window` rows and its first `sinks` rows are all that is looked at."""
+    window, sinks = _window(window, sinks)
     lib = load_library()
     want = (layer.batch, layer.h_q, layer.d)
     if q_new.shape != want or not q_new.is_contiguous():
@@ -571,23 +598,28 @@ def decode_attn(layer: Layer, q_new, cu_seqlens, headroom, K_cache, V_cache, seg
         ws = torch.empty(max(decode_workspace_bytes(layer, headroom), 16), dtype=torch.uint8,
                          device=q_new.device)
     _check_decode_bufs(layer, headroom, K_cache, V_cache, cu_seqlens, seg_len, out, lse, ws)
-    st = lib.adakv_decode_attn(ctypes.byref(layer.c), _ptr(q_new, "q_new", layer.torch_dtype),
-                               _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom),
-                               _ptr(K_cache, "K_cache", layer.torch_dtype),
-                               _ptr(V_cache, "V_cache", layer.torch_dtype),
-                               _ptr(seg_len, "seg_len", torch.int32),
-                               _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32),
-                               ws.data_ptr(), ws.numel(), _stream(stream))
+    if window is not None:
+        _one_device(stream, q_new=q_new, cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len, out=out, lse=lse, ws=ws)
+    name, fn = ("adakv_decode_attn", lib.adakv_decode_attn) if window is None else ("adakv_decode_window_attn", lib.adakv_decode_window_attn)
+    st = fn(ctypes.byref(layer.c), _ptr(q_new, "q_new", layer.torch_dtype),
+            _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom),
+            _ptr(K_cache, "K_cache", layer.torch_dtype),
+            _ptr(V_cache, "V_cache", layer.torch_dtype),
+            _ptr(seg_len, "seg_len", torch.int32), *(() if window is None else (window, sinks)),
+            _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32),
+            ws.data_ptr(), ws.numel(), _stream(stream))
     if st != 0:
-        raise AdaKVError(st, "adakv_decode_attn")
+        raise AdaKVError(st, name)
     return (out, lse) if (want_lse or lse is not None) else out
 
 
 def decode_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len,
-                overflow=None, out=None, lse=None, ws=None, stream=None, want_lse=False):
-    """adakv_decode_step: append k_new/v_new to every segment and attend, in one call."""
+                overflow=None, out=None, lse=None, ws=None, stream=None, want_lse=False, window=None, sinks=0):
+    """adakv_decode_step: append k_new/v_new to every segment and attend, in one call.  `window`, `sinks`: as for
+    decode_attn (adakv_decode_window_step)."""
     lib = load_library()
-    if _marshal is not None and out is not None and ws is not None and (lse is not None or not want_lse):
+    window, sinks = _window(window, sinks)
+    if window is None and _marshal is not None and out is not None and ws is not None and (lse is not None or not want_lse):
         try:
             handle = _stream(stream)
         except (RuntimeError, AttributeError):      # no GPU, or no stream: the tensors are looked at first
@@ -617,19 +649,271 @@ def decode_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, K_cache
                          device=q_new.device)
     _check_decode_bufs(layer, headroom, K_cache, V_cache, cu_seqlens, seg_len, out, lse, ws)
     _need(overflow, 1, "overflow")
-    st = lib.adakv_decode_step(ctypes.byref(layer.c), _ptr(q_new, "q_new", layer.torch_dtype),
-                               _ptr(k_new, "k_new", layer.torch_dtype),
-                               _ptr(v_new, "v_new", layer.torch_dtype),
-                               _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom),
-                               _ptr(K_cache, "K_cache", layer.torch_dtype),
-                               _ptr(V_cache, "V_cache", layer.torch_dtype),
-                               _ptr(seg_len, "seg_len", torch.int32),
-                               _ptr(overflow, "overflow", torch.int32),
-                               _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32),
-                               ws.data_ptr(), ws.numel(), _stream(stream))
+    if window is not None:
+        _one_device(stream, q_new=q_new, k_new=k_new, v_new=v_new, cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache,
+                    seg_len=seg_len, overflow=overflow, out=out, lse=lse, ws=ws)
+    name, fn = ("adakv_decode_step", lib.adakv_decode_step) if window is None else ("adakv_decode_window_step", lib.adakv_decode_window_step)
+    st = fn(ctypes.byref(layer.c), _ptr(q_new, "q_new", layer.torch_dtype),
+            _ptr(k_new, "k_new", layer.torch_dtype),
+            _ptr(v_new, "v_new", layer.torch_dtype),
+            _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom),
+            _ptr(K_cache, "K_cache", layer.torch_dtype),
+            _ptr(V_cache, "V_cache", layer.torch_dtype),
+            _ptr(seg_len, "seg_len", torch.int32),
+            _ptr(overflow, "overflow", torch.int32), *(() if window is None else (window, sinks)),
+            _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32),
+            ws.data_ptr(), ws.numel(), _stream(stream))
     if st != 0:
-        raise AdaKVError(st, "adakv_decode_step")
+        raise AdaKVError(st, name)
     return (out, lse) if (want_lse or lse is not None) else out
+
+
+# ---- attention over the prompt, limited to a window and sinks -----------------------------------------
+def _window(window, sinks):
+    """`window` and `sinks` as the library takes them.  A window longer than any sequence means all rows."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks need a window")
+        return None, 0
+    window, sinks = int(window), int(sinks)
+    if window < 1 or sinks < 0:
+        raise ValueError(f"window must be 1 or more and sinks 0 or more, got {window} and {sinks}")
+    return min(window, 2**31 - 1), min(sinks, 2**31 - 1)
+
+
+def _one_device(stream, **tensors):
+    """All tensors of a call are on the device that it is launched on: the stream's, or the current one."""
+    where = _device(stream)
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if t.get_device() != where:
+            raise ValueError(f"{name} is on device {t.get_device()}, the call is launched on {where}")
+
+
+def _device(stream):
+    if stream is not None:
+        return stream.device.index
+    return torch.cuda.current_device() if _current_device is None else _current_device()
+
+
+def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, stream=None, want_lse=False):
+    """adakv_window_attn: causal attention of q [tokens, h_q, d] (any strides of tokens and heads) over the layer's
+    sequences, limited to the last `window` keys and the first `sinks`.  Returns out [tokens, h_q, d] in the layer's
+    dtype (rows of no sequence: as they were, zero in an `out` made here) and, if asked for, row_lse [batch, h_q, w] as
+    `score` and `compress` take it."""
+    lib = load_library()
+    window, sinks = _window(window, sinks)
+    if window is None:
+        raise ValueError("window must be given (the longest sequence's length for all of it)")
+    if q.dim() != 3 or q.shape[1] != layer.h_q or q.shape[2] != layer.d or (layer.d > 1 and q.stride(2) != 1):
+        raise ValueError(f"q must be [tokens, {layer.h_q}, {layer.d}] with contiguous rows")
+    rows = layer.last_token_row
+    if q.shape[0] < rows:
+        raise ValueError(f"q has {q.shape[0]} tokens, the layer's sequences reach {rows}")
+    _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
+    _check_kv(layer, V, "V", layer.v_strides, layer.strides_given[1])
+    if out is None:
+        out = torch.zeros((q.shape[0], layer.h_q, layer.d), dtype=layer.torch_dtype, device=q.device)
+    if row_lse is None and want_lse:
+        row_lse = torch.empty((layer.batch, layer.h_q, layer.w), dtype=torch.float32, device=q.device)
+    _need(out, rows * layer.h_q * layer.d, "out")
+    _need(row_lse, layer.batch * layer.h_q * layer.w, "row_lse")
+    dt = layer.torch_dtype
+    qp, kp, vp, op, lp = (_ptr(q, "q", dt), _ptr(K, "K", dt), _ptr(V, "V", dt), _ptr(out, "out", dt), _ptr(row_lse, "row_lse", torch.float32))
+    _one_device(stream, q=q, K=K, V=V, out=out, row_lse=row_lse)
+    st = lib.adakv_window_attn(ctypes.byref(layer.c), qp, q.stride(0), q.stride(1), kp, vp, window, sinks, op, lp, _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, "adakv_window_attn")
+    return (out, row_lse) if (want_lse or row_lse is not None) else out
+
+
+# ---- the decode-side cache in 8 bits --------------------------------------------------------------------
+class Q8Cache(NamedTuple):
+    """A cache in 8 bits: K and V [rows, d] torch.float8_e4m3fn, k_scale and v_scale fp32, one for each block of 32 rows
+    of a segment (block j of segment s, which starts at row r of the cache: at r // 32 + s + j)."""
+    K: torch.Tensor
+    V: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+Q8_BLOCK = 32           # ADAKV_Q8_BLOCK
+
+
+def q8_scales(layer: Layer, headroom: int) -> int:
+    """adakv_q8_scales: how many scales k_scale and v_scale hold."""
+    return int(load_library().adakv_q8_scales(ctypes.byref(layer.c), int(headroom)))
+
+
+def q8_cache(layer: Layer, headroom: int, device="cuda") -> Q8Cache:
+    """Memory for a cache in 8 bits: zeros."""
+    scales = q8_scales(layer, headroom)
+    if scales == 0:
+        raise ValueError("the layer or the head-room is not valid")
+    codes = [torch.zeros((cache_rows(layer, headroom), layer.d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+    return Q8Cache(*codes, *(torch.zeros(scales, dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _q8_ptrs(layer, headroom, cache):
+    """The four addresses of an 8-bit cache, and its tensors by name."""
+    K, V, ks, vs = cache
+    _check_cache(layer, headroom, K, V)
+    scales = cache_rows(layer, headroom) // Q8_BLOCK + layer._segments
+    _need(ks, scales, "k_scale")
+    _need(vs, scales, "v_scale")
+    f8 = torch.float8_e4m3fn
+    return ((_ptr(K, "K", f8), _ptr(V, "V", f8), _ptr(ks, "k_scale", torch.float32), _ptr(vs, "v_scale", torch.float32)),
+            dict(K=K, V=V, k_scale=ks, v_scale=vs))
+
+
+def _check_new(layer, k_new, v_new):
+    want = (layer.batch, layer.h_kv, layer.d)
+    if k_new.shape != want or v_new.shape != want or not (k_new.is_contiguous() and v_new.is_contiguous()):
+        raise ValueError(f"k_new and v_new must be contiguous {want}")
+
+
+def cache_build_q8(layer: Layer, K, V, indices, cu_seqlens, headroom, cache=None, seg_len=None, stream=None):
+    """adakv_cache_build_q8: the gather of cache_build into an 8-bit cache; returns (cache, seg_len)."""
+    lib = load_library()
+    if cache is None:
+        cache = q8_cache(layer, headroom, K.device)
+    if seg_len is None:
+        seg_len = torch.empty(layer._segments, dtype=torch.int32, device=K.device)
+    _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
+    _check_kv(layer, V, "V", layer.v_strides, layer.strides_given[1])
+    _need(indices, layer._rows_out, "indices")
+    _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
+    _need(seg_len, layer._segments, "seg_len")
+    at, named = _q8_ptrs(layer, headroom, cache)
+    args = (_ptr(K, "K", layer.torch_dtype), _ptr(V, "V", layer.torch_dtype), _ptr(indices, "indices", torch.int32),
+            _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom), *at, _ptr(seg_len, "seg_len", torch.int32))
+    _one_device(stream, K=K, V=V, indices=indices, cu_seqlens=cu_seqlens, seg_len=seg_len, **{"cache." + k: t for k, t in named.items()})
+    st = lib.adakv_cache_build_q8(ctypes.byref(layer.c), *args, _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, "adakv_cache_build_q8")
+    return cache, seg_len
+
+
+def append_q8(layer: Layer, k_new, v_new, cu_seqlens, headroom, cache, seg_len, overflow=None, stream=None):
+    """adakv_append_q8: one new K/V row per (sequence, KV head) behind each segment; seg_len grows."""
+    lib = load_library()
+    _check_new(layer, k_new, v_new)
+    _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
+    _need(seg_len, layer._segments, "seg_len")
+    _need(overflow, 1, "overflow")
+    at, named = _q8_ptrs(layer, headroom, cache)
+    args = (_ptr(k_new, "k_new", layer.torch_dtype), _ptr(v_new, "v_new", layer.torch_dtype),
+            _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom), *at, _ptr(seg_len, "seg_len", torch.int32),
+            _ptr(overflow, "overflow", torch.int32))
+    _one_device(stream, k_new=k_new, v_new=v_new, cu_seqlens=cu_seqlens, seg_len=seg_len, overflow=overflow, **named)
+    st = lib.adakv_append_q8(ctypes.byref(layer.c), *args, _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, "adakv_append_q8")
+    return seg_len
+
+
+def _decode_q8(name, layer, q_new, new, cu_seqlens, headroom, cache, seg_len, over, out, lse, ws, stream, want_lse):
+    """Both decoding calls: `new` and `over` are (k_new, v_new) and (overflow,), or empty."""
+    lib = load_library()
+    want = (layer.batch, layer.h_q, layer.d)
+    if q_new.shape != want or not q_new.is_contiguous():
+        raise ValueError(f"q_new must be contiguous {want}")
+    if new:
+        _check_new(layer, *new)
+        _need(over[0], 1, "overflow")
+    if out is None:
+        out = torch.empty(want, dtype=torch.float32, device=q_new.device)
+    if lse is None and want_lse:
+        lse = torch.empty(want[:2], dtype=torch.float32, device=q_new.device)
+    if ws is None:
+        ws = torch.empty(max(decode_workspace_bytes(layer, headroom), 16), dtype=torch.uint8, device=q_new.device)
+    at, named = _q8_ptrs(layer, headroom, cache)
+    _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
+    _need(seg_len, layer._segments, "seg_len")
+    _need(out, layer.batch * layer.h_q * layer.d, "out")
+    _need(lse, layer.batch * layer.h_q, "lse")
+    _check_ws(ws)
+    dt = layer.torch_dtype
+    args = (_ptr(q_new, "q_new", dt), *(_ptr(t, nm, dt) for t, nm in zip(new, ("k_new", "v_new"))),
+            _ptr(cu_seqlens, "cu_seqlens", torch.int32), int(headroom), *at, _ptr(seg_len, "seg_len", torch.int32),
+            *(_ptr(t, "overflow", torch.int32) for t in over), _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32))
+    _one_device(stream, q_new=q_new, cu_seqlens=cu_seqlens, seg_len=seg_len, out=out, lse=lse, ws=ws, **named,
+                **dict(zip(("k_new", "v_new"), new)), **dict(zip(("overflow",), over)))
+    st = getattr(lib, name)(ctypes.byref(layer.c), *args, ws.data_ptr(), ws.numel(), _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, name)
+    return (out, lse) if (want_lse or lse is not None) else out
+
+
+def decode_attn_q8(layer: Layer, q_new, cu_seqlens, headroom, cache, seg_len, out=None, lse=None, ws=None, stream=None, want_lse=False):
+    """adakv_decode_attn_q8: decode_attn over an 8-bit cache."""
+    return _decode_q8("adakv_decode_attn_q8", layer, q_new, (), cu_seqlens, headroom, cache, seg_len, (), out, lse, ws, stream, want_lse)
+
+
+def decode_step_q8(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, cache, seg_len, overflow=None, out=None, lse=None,
+                   ws=None, stream=None, want_lse=False):
+    """adakv_decode_step_q8: decode_step over an 8-bit cache."""
+    return _decode_q8("adakv_decode_step_q8", layer, q_new, (k_new, v_new), cu_seqlens, headroom, cache, seg_len, (overflow,), out,
+                      lse, ws, stream, want_lse)
+
+
+# ---- sequences of a cache, moved ------------------------------------------------------------------------
+def _move(name, layer, picks, cu_seqlens, headroom, src, seg_len, headroom_out, cu_out, dst, len_out, overflow, stream):
+    to = layer.pick(picks)
+    _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
+    _need(seg_len, layer._segments, "seg_len")
+    _need(overflow, 1, "overflow")
+    dev = cu_seqlens.device
+    if cu_out is None:
+        cu_out = torch.empty(to._segments + 1, dtype=torch.int32, device=dev)
+    if len_out is None:
+        len_out = torch.empty(to._segments, dtype=torch.int32, device=dev)
+    _need(cu_out, to._segments + 1, "cu_out")
+    _need(len_out, to._segments, "len_out")
+    (at, named), (at_out, named_out) = src(layer, headroom), dst(to, headroom_out)
+    i32 = torch.int32
+    args = (len(picks), (ctypes.c_int32 * len(picks))(*(int(b) for b in picks)), _ptr(cu_seqlens, "cu_seqlens", i32), int(headroom), *at,
+            _ptr(seg_len, "seg_len", i32), int(headroom_out), _ptr(cu_out, "cu_out", i32), *at_out, _ptr(len_out, "len_out", i32),
+            _ptr(overflow, "overflow", i32))
+    _one_device(stream, cu_seqlens=cu_seqlens, seg_len=seg_len, cu_out=cu_out, len_out=len_out, overflow=overflow, **named,
+                **{k + "_out": t for k, t in named_out.items()})
+    st = getattr(load_library(), name)(ctypes.byref(layer.c), *args, _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, name)
+    return to, cu_out, len_out
+
+
+def cache_move(layer: Layer, picks, cu_seqlens, headroom, K_cache, V_cache, seg_len, headroom_out, cu_out=None, K_out=None,
+               V_out=None, len_out=None, overflow=None, stream=None):
+    """adakv_cache_move: the cache of sequences picks[0], picks[1], ... (forked where named twice, dropped where not) with
+    other head-room.  Returns (layer.pick(picks), cu_out, K_out, V_out, len_out)."""
+    def cache(K, V):
+        def at(lay, hr):
+            _check_cache(lay, hr, K, V)
+            return tuple(_ptr(t, nm, lay.torch_dtype) for t, nm in ((K, "K_cache"), (V, "V_cache"))), dict(K=K, V=V)
+        return at
+
+    rows = cache_rows(layer.pick(picks), headroom_out)
+    if K_out is None:
+        K_out = torch.zeros((rows, layer.d), dtype=layer.torch_dtype, device=K_cache.device)
+    if V_out is None:
+        V_out = torch.zeros((rows, layer.d), dtype=layer.torch_dtype, device=V_cache.device)
+    to, cu_out, len_out = _move("adakv_cache_move", layer, picks, cu_seqlens, headroom, cache(K_cache, V_cache), seg_len, headroom_out,
+                                cu_out, cache(K_out, V_out), len_out, overflow, stream)
+    return to, cu_out, K_out, V_out, len_out
+
+
+def cache_move_q8(layer: Layer, picks, cu_seqlens, headroom, cache, seg_len, headroom_out, cu_out=None, out=None, len_out=None,
+                  overflow=None, stream=None):
+    """adakv_cache_move_q8: cache_move for an 8-bit cache.  Returns (layer.pick(picks), cu_out, out, len_out)."""
+    if out is None:
+        out = q8_cache(layer.pick(picks), headroom_out, cache.K.device)
+    to, cu_out, len_out = _move("adakv_cache_move_q8", layer, picks, cu_seqlens, headroom, lambda lay, hr: _q8_ptrs(lay, hr, cache), seg_len,
+                                headroom_out, cu_out, lambda lay, hr: _q8_ptrs(lay, hr, out), len_out, overflow, stream)
+    return to, cu_out, out, len_out
 
 
 class KernelTrace:

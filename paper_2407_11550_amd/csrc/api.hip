@@ -394,6 +394,206 @@ int adakv_decode_step(const adakv_layer *L, const void *q_new, const void *k_new
   return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
 }
 
+// ---- attention limited to a window and sinks ------------------------------------------------------
+int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok, int64_t q_stride_head,
+                      const void *K, const void *V, int32_t window, int32_t sinks, void *out,
+                      float *row_lse, void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if (window < 1 || sinks < 0 || q_stride_tok < L->d || q_stride_head < L->d) return ADAKV_EINVAL;
+  if (!q || !K || !V || !out) return ADAKV_EINVAL;
+  const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
+  if (q_stride_tok * esz % 16 != 0 || q_stride_head * esz % 16 != 0) return ADAKV_EUNSUPPORTED;
+  if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return ADAKV_EUNSUPPORTED;
+  long long blocks = 0;
+  for (int b = 0; b < st.batch; ++b) {
+    const long long rows = (long long)st.n[b] + dm.w;
+    if (rows > (1 << 28)) return ADAKV_EUNSUPPORTED;
+    blocks += (rows + 63) / 64;
+  }
+  if (blocks * dm.h_q > (1 << 20) * 64ll) return ADAKV_EUNSUPPORTED;
+  hipError_t e = launch_window_attn(st, dm, L->dtype, q, q_stride_tok, q_stride_head, K, V, window, sinks, out, row_lse,
+                                    (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+// (both forms; k_new == NULL: attention only)
+static int decode_window(const adakv_layer *L, const void *q_new, const void *k_new, const void *v_new, const int32_t *cu_seqlens,
+                         int32_t headroom, void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow, int32_t window,
+                         int32_t sinks, float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  if (window < 1 || sinks < 0) return ADAKV_EINVAL;
+  if (!q_new || !cu_seqlens || !K_cache || !V_cache || !seg_len || !out) return ADAKV_EINVAL;
+  if (!decode_supported(dm)) return ADAKV_EUNSUPPORTED;
+  if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(K_cache) || !aligned16(V_cache))
+    return ADAKV_EUNSUPPORTED;
+  if (!ws || ws_bytes < plan_decode(st, dm, L->dtype, headroom).total + 256) return ADAKV_EWORKSPACE;
+  char *wsp = (char *)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  const long long limit = (long long)window + sinks;
+  hipError_t e = launch_decode_window(st, dm, L->dtype, headroom, limit < INT_MAX ? (int)limit : INT_MAX, sinks, q_new, k_new, v_new,
+                                      cu_seqlens, K_cache, V_cache, seg_len, overflow, out, lse, wsp, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_decode_window_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
+                             int32_t headroom, const void *K_cache, const void *V_cache,
+                             const int32_t *seg_len, int32_t window, int32_t sinks, float *out,
+                             float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  return decode_window(L, q_new, nullptr, nullptr, cu_seqlens, headroom, (void *)K_cache, (void *)V_cache, (int32_t *)seg_len,
+                       nullptr, window, sinks, out, lse, ws, ws_bytes, hip_stream);
+}
+
+int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void *k_new,
+                             const void *v_new, const int32_t *cu_seqlens, int32_t headroom,
+                             void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow,
+                             int32_t window, int32_t sinks, float *out, float *lse, void *ws,
+                             size_t ws_bytes, void *hip_stream) {
+  if (!k_new || !v_new) return ADAKV_EINVAL;
+  return decode_window(L, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, window, sinks, out, lse,
+                       ws, ws_bytes, hip_stream);
+}
+
+// ---- the cache in 8 bits --------------------------------------------------------------------------
+size_t adakv_q8_scales(const adakv_layer *L, int32_t headroom) {
+  SeqTab st; Dims dm;
+  if (build_tables(L, st, dm) != ADAKV_OK || check_headroom(st, dm, headroom) != ADAKV_OK) return 0;
+  return (size_t)q8_scales(st, dm, headroom);
+}
+
+int adakv_cache_build_q8(const adakv_layer *L, const void *K, const void *V,
+                         const int32_t *indices, const int32_t *cu_seqlens, int32_t headroom,
+                         void *K_q8, void *V_q8, float *k_scale, float *v_scale, int32_t *seg_len,
+                         void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  if (!K || !V || !indices || !cu_seqlens || !K_q8 || !V_q8 || !k_scale || !v_scale || !seg_len) return ADAKV_EINVAL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(K_q8) || !aligned16(V_q8)) return ADAKV_EUNSUPPORTED;
+  hipError_t e = launch_cache_build_q8(st, dm, L->dtype, K, V, indices, cu_seqlens, headroom,
+                                       {(char *)K_q8, (char *)V_q8, k_scale, v_scale}, seg_len, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_append_q8(const adakv_layer *L, const void *k_new, const void *v_new,
+                    const int32_t *cu_seqlens, int32_t headroom, void *K_q8, void *V_q8,
+                    float *k_scale, float *v_scale, int32_t *seg_len, int32_t *overflow,
+                    void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  if (!k_new || !v_new || !cu_seqlens || !K_q8 || !V_q8 || !k_scale || !v_scale || !seg_len) return ADAKV_EINVAL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(K_q8) || !aligned16(V_q8)) return ADAKV_EUNSUPPORTED;
+  hipError_t e = launch_append_q8(st, dm, L->dtype, headroom, k_new, v_new, cu_seqlens,
+                                  {(char *)K_q8, (char *)V_q8, k_scale, v_scale}, seg_len, overflow, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+// (both forms; k_new == NULL: attention only)
+static int decode_q8(const adakv_layer *L, const void *q_new, const void *k_new, const void *v_new, const int32_t *cu_seqlens,
+                     int32_t headroom, const Q8Cache &c, int32_t *seg_len, int32_t *overflow, float *out, float *lse, void *ws,
+                     size_t ws_bytes, void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  if (!q_new || !cu_seqlens || !c.K || !c.V || !c.k_scale || !c.v_scale || !seg_len || !out) return ADAKV_EINVAL;
+  if (!decode_supported(dm)) return ADAKV_EUNSUPPORTED;
+  if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(c.K) || !aligned16(c.V)) return ADAKV_EUNSUPPORTED;
+  if (!ws || ws_bytes < plan_decode(st, dm, L->dtype, headroom).total + 256) return ADAKV_EWORKSPACE;
+  char *wsp = (char *)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  hipError_t e = launch_decode_q8(st, dm, L->dtype, headroom, q_new, k_new, v_new, cu_seqlens, c, seg_len, overflow, out, lse, wsp,
+                                  (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_decode_attn_q8(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
+                         int32_t headroom, const void *K_q8, const void *V_q8,
+                         const float *k_scale, const float *v_scale, const int32_t *seg_len,
+                         float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  return decode_q8(L, q_new, nullptr, nullptr, cu_seqlens, headroom, {(char *)K_q8, (char *)V_q8, (float *)k_scale, (float *)v_scale},
+                   (int32_t *)seg_len, nullptr, out, lse, ws, ws_bytes, hip_stream);
+}
+
+int adakv_decode_step_q8(const adakv_layer *L, const void *q_new, const void *k_new,
+                         const void *v_new, const int32_t *cu_seqlens, int32_t headroom,
+                         void *K_q8, void *V_q8, float *k_scale, float *v_scale, int32_t *seg_len,
+                         int32_t *overflow, float *out, float *lse, void *ws, size_t ws_bytes,
+                         void *hip_stream) {
+  if (!k_new || !v_new) return ADAKV_EINVAL;
+  return decode_q8(L, q_new, k_new, v_new, cu_seqlens, headroom, {(char *)K_q8, (char *)V_q8, k_scale, v_scale}, seg_len, overflow,
+                   out, lse, ws, ws_bytes, hip_stream);
+}
+
+// ---- sequences of a cache, moved --------------------------------------------------------------------
+struct Range { const void *at; size_t bytes; };
+static bool overlap(const Range &a, const Range &b) {
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
+}
+
+// (both forms; a cache in 8 bits has scales)
+static int cache_move(const adakv_layer *L, int32_t count, const int32_t *from, const int32_t *cu_seqlens, int32_t headroom,
+                      const Q8Cache &c, const int32_t *seg_len, int32_t headroom_out, int32_t *cu_out, const Q8Cache &o,
+                      int32_t *len_out, int32_t *overflow, void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  if (!from || count < 1 || count > ADAKV_MAX_BATCH || headroom_out < 0) return ADAKV_EINVAL;
+  const bool q8 = c.k_scale != nullptr;
+  if (!cu_seqlens || !c.K || !c.V || !seg_len || !cu_out || !o.K || !o.V || !len_out) return ADAKV_EINVAL;
+  const long long nseg = (long long)st.batch * dm.h_kv, nseg_out = (long long)count * dm.h_kv;
+  const long long rows = st.out_off[st.batch] + nseg * headroom;
+  long long rows_out = nseg_out * headroom_out;
+  for (int i = 0; i < count; ++i) {
+    if (from[i] < 0 || from[i] >= st.batch) return ADAKV_EINVAL;
+    rows_out += st.out_off[from[i] + 1] - st.out_off[from[i]];
+  }
+  if (rows_out >= (1ll << 31)) return ADAKV_EUNSUPPORTED;
+  if (!aligned16(c.K) || !aligned16(c.V) || !aligned16(o.K) || !aligned16(o.V)) return ADAKV_EUNSUPPORTED;
+  const size_t row = (size_t)dm.d * (q8 ? 1 : L->dtype == ADAKV_FP32 ? 4 : 2);
+  const size_t sc = (size_t)(rows / ADAKV_Q8_BLOCK + nseg) * 4, sc_out = (size_t)(rows_out / ADAKV_Q8_BLOCK + nseg_out) * 4;
+  const Range in[6] = {{c.K, rows * row}, {c.V, rows * row}, {cu_seqlens, (size_t)(nseg + 1) * 4}, {seg_len, (size_t)nseg * 4},
+                       {c.k_scale, sc}, {c.v_scale, sc}};
+  const Range res[7] = {{o.K, rows_out * row}, {o.V, rows_out * row}, {cu_out, (size_t)(nseg_out + 1) * 4},
+                        {len_out, (size_t)nseg_out * 4}, {o.k_scale, sc_out}, {o.v_scale, sc_out}, {overflow, 4}};
+  for (int i = 0; i < 7; ++i) {
+    for (const Range &r : in)
+      if (overlap(res[i], r)) return ADAKV_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(res[i], res[j])) return ADAKV_EINVAL;
+  }
+  hipError_t e = launch_cache_move(st, dm, (int)row, count, from, cu_seqlens, headroom, c.K, c.V, c.k_scale, c.v_scale, seg_len,
+                                   headroom_out, cu_out, o.K, o.V, o.k_scale, o.v_scale, len_out, overflow, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_cache_move(const adakv_layer *L, int32_t count, const int32_t *from,
+                     const int32_t *cu_seqlens, int32_t headroom, const void *K_cache,
+                     const void *V_cache, const int32_t *seg_len, int32_t headroom_out,
+                     int32_t *cu_out, void *K_out, void *V_out, int32_t *len_out,
+                     int32_t *overflow, void *hip_stream) {
+  return cache_move(L, count, from, cu_seqlens, headroom, {(char *)K_cache, (char *)V_cache, nullptr, nullptr}, seg_len, headroom_out,
+                    cu_out, {(char *)K_out, (char *)V_out, nullptr, nullptr}, len_out, overflow, hip_stream);
+}
+
+int adakv_cache_move_q8(const adakv_layer *L, int32_t count, const int32_t *from,
+                        const int32_t *cu_seqlens, int32_t headroom, const void *K_q8,
+                        const void *V_q8, const float *k_scale, const float *v_scale,
+                        const int32_t *seg_len, int32_t headroom_out, int32_t *cu_out,
+                        void *K_out, void *V_out, float *k_scale_out, float *v_scale_out,
+                        int32_t *len_out, int32_t *overflow, void *hip_stream) {
+  if (!k_scale || !v_scale || !k_scale_out || !v_scale_out) return ADAKV_EINVAL;
+  return cache_move(L, count, from, cu_seqlens, headroom, {(char *)K_q8, (char *)V_q8, (float *)k_scale, (float *)v_scale}, seg_len,
+                    headroom_out, cu_out, {(char *)K_out, (char *)V_out, k_scale_out, v_scale_out}, len_out, overflow, hip_stream);
+}
+
 int adakv_describe(const adakv_layer *L, int have_row_lse, char *out, size_t out_bytes) {
   SeqTab st; Dims dm;
   int rc = build_tables(L, st, dm);

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 #include <hip/hip_ext.h>
+#include <limits.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -169,16 +170,49 @@ struct DecodePlan {
   size_t seg_tab, total;            // per segment: first partial, partials, rows, appended
 };
 bool decode_supported(const Dims &dm);
-DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom);
+// limit: the most rows of a segment that the call looks at
+DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom, int limit = INT_MAX);
 // k_new == nullptr: attention only (cache and lengths are only read)
 hipError_t launch_decode_attn(const SeqTab &st, const Dims &dm, int dtype, int headroom,
                               const void *q, const void *k_new, const void *v_new, const int *cu,
                               void *Kc, void *Vc, int *seg_len, int *overflow, float *out,
                               float *lse, char *ws, hipStream_t s);
+// The same over a segment's first `sinks` rows and its last ones, `limit` rows together.
+hipError_t launch_decode_window(const SeqTab &st, const Dims &dm, int dtype, int headroom, int limit, int sinks,
+                                const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,
+                                int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s);
+// Merges the partial results of a plan's workgroups; new_len: the lengths of a call that appends, else null.
+void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, char *ws, int *new_len, int *overflow, float *out,
+                           float *lse, hipStream_t s);
 hipError_t launch_append(const SeqTab &st, const Dims &dm, int dtype, int headroom,
                          const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,
                          int *seg_len, int *overflow, hipStream_t s);
 
+
+// ---- the cache in 8 bits (decode_q8.hip) -----------------------------------------------------
+struct Q8Cache {
+  char *K, *V;
+  float *k_scale, *v_scale;
+};
+long long q8_scales(const SeqTab &st, const Dims &dm, int headroom);
+hipError_t launch_cache_build_q8(const SeqTab &st, const Dims &dm, int dtype, const void *K, const void *V, const int *indices,
+                                 const int *cu, int headroom, const Q8Cache &c, int *seg_len, hipStream_t s);
+hipError_t launch_append_q8(const SeqTab &st, const Dims &dm, int dtype, int headroom, const void *k_new, const void *v_new,
+                            const int *cu, const Q8Cache &c, int *seg_len, int *overflow, hipStream_t s);
+hipError_t launch_decode_q8(const SeqTab &st, const Dims &dm, int dtype, int headroom, const void *q, const void *k_new,
+                            const void *v_new, const int *cu, const Q8Cache &c, int *seg_len, int *overflow, float *out, float *lse,
+                            char *ws, hipStream_t s);
+
+// ---- sequences of a cache moved (cache_move.hip) ---------------------------------------------
+// row_bytes: of one row of K_cache; the scales are null but for a cache in 8 bits
+hipError_t launch_cache_move(const SeqTab &st, const Dims &dm, int row_bytes, int count, const int *from, const int *cu, int headroom,
+                             const void *K, const void *V, const float *k_scale, const float *v_scale, const int *seg_len,
+                             int headroom_out, int *cu_out, void *K_out, void *V_out, float *ks_out, float *vs_out, int *len_out,
+                             int *overflow, hipStream_t s);
+
+// ---- attention over the prompt (window_attn.hip) ---------------------------------------------
+hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const void *q, long long q_tok, long long q_head,
+                              const void *K, const void *V, int window, int sinks, void *out, float *row_lse, hipStream_t s);
 
 // Profiling aid (adakv_trace_arm): while armed on this host thread, every kernel launch carries
 // a pair of the caller's events that receive the kernel's own start and end timestamps.

@@ -14,22 +14,25 @@
 // of the lengths, writes partial (max, sum, weighted value sum) per query head, and a second kernel
 // merges the parts of each segment.  Where no segment of a layer can be long, one workgroup takes each
 // segment (decode_mfma_kernel, WHOLE) and writes the result itself: no prefix sum, no merge.
+//
+// A call with a window looks at a segment's first rows (the sinks) and its last ones alone: the kernels number the
+// rows it sees and leave a gap where the sinks end (WIN).  Those instantiations are built as a translation unit of
+// their own (ADAKV_DECODE_PART = 2), beside the others and everything else (1).
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
 
-#include "common.h"
+#include "decode_parts.h"
+
+#ifndef ADAKV_DECODE_PART
+#define ADAKV_DECODE_PART 1
+#endif
 
 namespace adakv {
 namespace {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
-constexpr float M_INIT = -1.0e30f;    // finite "no row seen yet" maximum: exp2(-inf - M_INIT) = 0
-
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+constexpr bool WIN_PART = ADAKV_DECODE_PART == 2;
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
@@ -84,97 +87,6 @@ template <> struct Elem<f16_t> {
   }
 };
 
-// Rows of segment s this call works on: the rows held, plus the row the call itself appends
-// (`grow` = 1) if the segment has room for it.
-__device__ __forceinline__ int rows_held(const int *cu, const int *seg_len, int s, int headroom,
-                                         int grow) {
-  const int cap = cu[s + 1] - cu[s] + headroom;
-  const int held = min(max(seg_len[s], 0), cap);   // a corrupt length can never leave the segment
-  return held + (held < cap ? grow : 0);
-}
-
-// What a workgroup works on: part `j` of the `parts` that the `rows` rows of segment s are split into.
-struct Work {
-  int s, j, parts, rows, first_row;
-  bool appended;                               // the last row is the one the call appends
-};
-
-// Finds it from a prefix sum, over the segments, of the parts that their lengths make (blocks of `split` rows).  The
-// same in all lanes.  False: the workgroup has nothing to do (the launch is an upper bound).  The merge kernel finds a
-// segment's partial results through seg_tab; the launch has at least one workgroup per segment, and workgroup s
-// files the entry of segment s.
-//
-// Up to 64 segments every wavefront does it for itself, a segment a lane, without LDS or a barrier (by the other way a
-// workgroup knew its rows 1.5 us after it had started; the kernel over 8 segments of 512 rows 5.4 -> 4.8 us, over 64 of
-// 1500 13.3 -> 12.6).  Beyond, thread t of
-// the workgroup takes segments t*per .. t*per+per-1 and the result goes through sh[0..21].
-template <int NWV = 4>
-__device__ __forceinline__ bool find_work(int nseg, int per, int split, int headroom, int grow, const int *cu,
-                                          const int *seg_len, int *sh, int4 *seg_tab, Work &wk) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, blk = (int)blockIdx.x;
-  if (nseg <= 64) {
-    const int s = min(lane, nseg - 1);
-    const int from = cu[s], cap = cu[s + 1] - from + headroom;
-    const int held = min(max(seg_len[s], 0), cap);       // (as in rows_held)
-    const int now = held + (held < cap ? grow : 0);
-    const int nb = lane < nseg ? (now + split - 1) / split : 0;
-    const int upto = wave_scan_incl(nb), first = upto - nb;
-    if (lane == blk && lane < nseg && wv == 0) seg_tab[s] = make_int4(first, nb, now, now - held);
-    const unsigned long long here = __ballot(blk >= first && blk < upto);
-    if (here == 0) return false;
-    const int L = __ffsll(here) - 1;
-    wk.s = L;
-    wk.j = blk - __builtin_amdgcn_readlane(first, L);
-    wk.parts = __builtin_amdgcn_readlane(nb, L);
-    wk.rows = __builtin_amdgcn_readlane(now, L);
-    wk.first_row = __builtin_amdgcn_readlane(from, L);
-    wk.appended = __builtin_amdgcn_readlane(now - held, L) != 0;
-    return true;
-  }
-  int mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s < nseg) mine += (rows_held(cu, seg_len, s, headroom, grow) + split - 1) / split;
-  }
-  const int inc = wave_scan_incl(mine);
-  if (lane == 63) sh[wv] = inc;
-  __syncthreads();
-  int before = 0, total = 0;
-#pragma unroll
-  for (int i = 0; i < NWV; ++i) {
-    const int v = sh[i];
-    if (i < wv) before += v;
-    total += v;
-  }
-  int first = before + inc - mine;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= nseg) break;
-    const int now = rows_held(cu, seg_len, s, headroom, grow);
-    const int appended = now - rows_held(cu, seg_len, s, headroom, 0);
-    const int nb = (now + split - 1) / split;
-    if (blk >= first && blk < first + nb) {
-      sh[16] = s;
-      sh[17] = blk - first;
-      sh[18] = now;
-      sh[19] = cu[s];
-      sh[20] = appended;
-      sh[21] = nb;
-    }
-    if (s == blk) seg_tab[s] = make_int4(first, nb, now, appended);
-    first += nb;
-  }
-  if (blk >= total) return false;
-  __syncthreads();
-  wk.s = __builtin_amdgcn_readfirstlane(sh[16]);
-  wk.j = __builtin_amdgcn_readfirstlane(sh[17]);
-  wk.rows = __builtin_amdgcn_readfirstlane(sh[18]);
-  wk.first_row = __builtin_amdgcn_readfirstlane(sh[19]);
-  wk.appended = __builtin_amdgcn_readfirstlane(sh[20]) != 0;
-  wk.parts = __builtin_amdgcn_readfirstlane(sh[21]);
-  return true;
-}
-
 // ---------------------------------------------------------------------------------------------
 // Query heads one wavefront carries: at most four (queries and accumulators take 2*GW*EPL
 // registers).  A larger group is split over NGRP sets of four wavefronts that read the
@@ -184,12 +96,12 @@ template <typename T, int G> struct HeadSplit {
   static constexpr int NGRP = G / GW;
 };
 
-template <typename T, int D, int G>
+template <typename T, int D, int G, bool WIN>
 __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_kernel(
     int nseg, int h, int per, int split, int headroom, float c_log2, const T *__restrict__ q,
     const char *__restrict__ k_new, const char *__restrict__ v_new, const int *__restrict__ cu,
     const int *__restrict__ seg_len, char *Kc, char *Vc, float *__restrict__ part_acc,
-    float *__restrict__ part_ml, int4 *__restrict__ seg_tab) {
+    float *__restrict__ part_ml, int4 *__restrict__ seg_tab, Window win) {
   constexpr int EPL = Elem<T>::EPL;
   constexpr int ROWB = D * (int)sizeof(T);
   constexpr int LPR = ROWB / 16;               // lanes per row
@@ -213,7 +125,7 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
   // the row is taken from k_new/v_new by the lanes it falls to, which also store it in the cache.
   const int grow = k_new != nullptr ? 1 : 0;
   Work wk;
-  if (!find_work<NW * NGRP>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, seg_tab, wk)) return;
+  if (!find_work<NW * NGRP, WIN>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, seg_tab, wk, win)) return;
   const int s = wk.s, len = wk.rows;
   const int b = s / h, c = s % h;
   // (equal parts of the segment, as in decode_mfma_kernel, in multiples of the split's own unit)
@@ -253,7 +165,7 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
       const int r = r0 + ((it * U + u) * NW + wv) * RPW + slot;
       ok[u] = r < r1;
       const int rr = min(r, r1 - 1);                           // r1 >= 1: the block exists
-      const long long o = (long long)rr * ROWB;
+      const long long o = (long long)place_of<WIN>(rr, wk.hidden, win) * ROWB;
       // lanes past the end re-read the block's last row (and ignore it): if that is the new row,
       // they too must take it from k_new/v_new, its place in the cache is not written yet
       const bool fresh = rr == new_row;
@@ -371,52 +283,14 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
 // per element and head) issued 130 instructions per four rows at g = 4 and 240 at g = 8, which
 // made it the bound from g = 8 on: a 134 MB cache at g = 8 took 77.2 us, now 29.8 (a plain
 // read of as much: 25); 49 MB at g = 4 19.2, now 12.9 (kernel times, launch included).
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
-typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
-typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
-
-template <bool F16>
-__device__ __forceinline__ floatx4 mfma16(u32x4 a, u32x4 b, floatx4 c) {
-  if constexpr (F16)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
 template <bool F16> constexpr float P_SCALE = F16 ? 0x1p64f : 1.0f;    // (|V| < 2^16, 2^31 rows: below the fp32 range's end)
-constexpr float LOW_MAX = 1024.0f;             // above the lower 3 bits of any finite fp16 value
-
-// The bf16 value that x is cut to, back in 32 bits, where `on`; 0 elsewhere.
-__device__ __forceinline__ float cut(float x, bool on) {
-  return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, x) & (on ? 0xffff0000u : 0u));
-}
-// x0 and x1 cut to bf16, x0 in the lower half of the word.
-__device__ __forceinline__ unsigned pack(float x0, float x1) {
-  return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, x1), __builtin_bit_cast(unsigned, x0), 0x07060302u);
-}
-// The upper (odd) or lower half of a word of two fp16 values.
-__device__ __forceinline__ float half_of(unsigned w, bool odd) {
-  return (float)__builtin_bit_cast(_Float16, (unsigned short)(odd ? w >> 16 : w & 0xffffu));
-}
-// What the cut leaves of an fp16 value in 32 bits.  Of an infinity (whose difference is a NaN) some
-// finite number: the upper part alone makes the product infinite.
-__device__ __forceinline__ float low_part(float x) { return fminf(x - cut(x, true), LOW_MAX); }
-
-// Where a workgroup's result goes: partial results for the merge kernel, or (WHOLE, one workgroup per
-// segment) straight to the caller.
-struct DecodeOut {
-  float *part_acc, *part_ml;
-  int4 *seg_tab;
-  float *out, *lse;
-  int *new_len, *overflow;                     // null unless the call appends
-};
 
 // (seg_len is also written, through res.new_len: after the barrier, by the one workgroup that read it)
-template <bool F16, int D, int G, bool WHOLE>
+template <bool F16, int D, int G, bool WHOLE, bool WIN>
 __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
     int nseg, int h, int per, int split, int headroom, float c_log2, const unsigned short *__restrict__ q,
     const char *__restrict__ k_new, const char *__restrict__ v_new, const int *__restrict__ cu,
-    const int *seg_len, char *Kc, char *Vc, DecodeOut res) {
+    const int *seg_len, char *Kc, char *Vc, DecodeOut res, Window win) {
   constexpr int NW = WHOLE ? 8 : 4;            // wavefronts that share the rows of a split
   constexpr int ROWB = D * 2;
   constexpr int KS = D / 32;                   // k-steps of the logits
@@ -436,19 +310,22 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
 
   // ---- which (segment, split) is this workgroup?  (as in decode_attn_kernel) --------------------
   const int grow = k_new != nullptr ? 1 : 0;
-  int s, len, cu_s, new_row, r0, r1;
+  int s, len, cu_s, new_row, r0, r1, hidden = 0;
   if constexpr (WHOLE) {
     s = blockIdx.x;
     cu_s = cu[s];
-    len = rows_held(cu, seg_len, s, headroom, grow);
-    new_row = len > rows_held(cu, seg_len, s, headroom, 0) ? len - 1 : -1;
+    const int now = rows_held(cu, seg_len, s, headroom, grow);
+    len = seen_rows<WIN>(now, win);
+    hidden = now - len;
+    new_row = now > rows_held(cu, seg_len, s, headroom, 0) ? len - 1 : -1;
     r0 = 0;
     r1 = len;
   } else {
     Work wk;
-    if (!find_work<NW>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, res.seg_tab, wk)) return;
+    if (!find_work<NW, WIN>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, res.seg_tab, wk, win)) return;
     s = wk.s;
     len = wk.rows;
+    hidden = wk.hidden;
     cu_s = wk.first_row;
     new_row = wk.appended ? len - 1 : -1;
     // The segment's rows in equal parts, in whole rounds of the workgroup: the call lasts as long as its
@@ -483,8 +360,10 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
   for (int t0 = r0 + wv * TR; t0 < r1; t0 += NW * TR) {
     u32x4 kk[2][KS];
     vword vv[8];
-    const bool edge = t0 + TR > r1 || (new_row >= t0 && new_row < t0 + TR);
-    const char *kt = Kb + (long long)t0 * ROWB, *vt = Vb + (long long)t0 * ROWB;
+    // (a tile with the last sink and the window's first row in it is none of consecutive rows)
+    const bool edge = t0 + TR > r1 || (new_row >= t0 && new_row < t0 + TR) || (WIN && t0 < win.sinks && win.sinks < t0 + TR);
+    const long long t_at = place_of<WIN>(t0, hidden, win);
+    const char *kt = Kb + t_at * ROWB, *vt = Vb + t_at * ROWB;
     const unsigned vcol = l16 * (VC * 2);
     if (!edge) {
 #pragma unroll
@@ -501,19 +380,21 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int r = t0 + 16 * t + l16, rr = min(r, r1 - 1);
-        const char *src = rr == new_row ? kn : Kb + (long long)rr * ROWB;
+        const long long o = (long long)place_of<WIN>(rr, hidden, win) * ROWB;
+        const char *src = rr == new_row ? kn : Kb + o;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           kk[t][ks] = *reinterpret_cast<const u32x4 *>(src + (4 * ks + lg) * 16);
-          if (r == new_row) *reinterpret_cast<u32x4 *>(Kb + (long long)r * ROWB + (4 * ks + lg) * 16) = kk[t][ks];
+          if (r == new_row) *reinterpret_cast<u32x4 *>(Kb + o + (4 * ks + lg) * 16) = kk[t][ks];
         }
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int r = t0 + 16 * (j / 4) + 4 * lg + j % 4, rr = min(r, r1 - 1);
-        const char *src = rr == new_row ? vn : Vb + (long long)rr * ROWB;
+        const long long o = (long long)place_of<WIN>(rr, hidden, win) * ROWB;
+        const char *src = rr == new_row ? vn : Vb + o;
         vv[j] = *reinterpret_cast<const vword *>(src + vcol);
-        if (r == new_row) *reinterpret_cast<vword *>(Vb + (long long)r * ROWB + vcol) = vv[j];
+        if (r == new_row) *reinterpret_cast<vword *>(Vb + o + vcol) = vv[j];
       }
     }
     float sc[8];                               // row t0 + 16 (j/4) + 4 lg + j%4, not scaled yet
@@ -656,11 +537,12 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
   }
   // (nobody but this workgroup reads the segment's length)
   if (WHOLE && res.new_len && tid == 0) {
-    if (new_row >= 0) res.new_len[s] = len;
+    if (new_row >= 0) res.new_len[s] = len + hidden;
     else if (res.overflow) *res.overflow = 1;  // the segment was full, its new row was dropped
   }
 }
 
+#if ADAKV_DECODE_PART == 1
 // One workgroup per (segment, query head of its group) merges that segment's splits and
 // normalises.  A long segment has hundreds of splits, so they are merged NSLOT side by side
 // (each by D/4 lanes holding a float4 of the value sum), four loads deep, then across slots.
@@ -763,12 +645,13 @@ __global__ __launch_bounds__(256) void append_kernel(
   *reinterpret_cast<uint4 *>(Vc + o) = vv;
   if (col == 0) seg_len[s] = len + 1;
 }
+#endif
 
 template <typename T, int D, int G>
 void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan &pl,
                 const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc,
                 void *Vc, int *seg_len, int *overflow, float *out, float *lse, char *ws,
-                hipStream_t s) {
+                Window win, hipStream_t s) {
   const int nseg = st.batch * dm.h_kv;
   const int per = (nseg + 255) / 256;
   float *part_acc = (float *)(ws + pl.part_acc);
@@ -787,24 +670,23 @@ void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan
   if constexpr (sizeof(T) == 2) {
     const DecodeOut res = {part_acc, part_ml, seg_tab, out, lse, k_new ? seg_len : nullptr, overflow};
     if (pl.whole) {
-      ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, true>), dim3(nseg), dim3(512), s, nseg, dm.h_kv,
+      ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, true, WIN_PART>), dim3(nseg), dim3(512), s, nseg, dm.h_kv,
                    per, pl.split, headroom, dm.scale * LOG2E, (const unsigned short *)q, (const char *)k_new,
-                   (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res);
+                   (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
       return;
     }
     if constexpr (!VECTOR)
-      ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, false>), dim3(pl.nblk), dim3(256), s, nseg,
+      ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, false, WIN_PART>), dim3(pl.nblk), dim3(256), s, nseg,
                    dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const unsigned short *)q, (const char *)k_new,
-                   (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res);
+                   (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
   }
   if constexpr (VECTOR)
-    ADAKV_LAUNCH("decode_attn", (decode_attn_kernel<T, D, G>), dim3(pl.nblk), dim3(256 * HeadSplit<T, G>::NGRP), s,
+    ADAKV_LAUNCH("decode_attn", (decode_attn_kernel<T, D, G, WIN_PART>), dim3(pl.nblk), dim3(256 * HeadSplit<T, G>::NGRP), s,
                  nseg, dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const T *)q, (const char *)k_new,
-                 (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, part_acc, part_ml, seg_tab);
+                 (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, part_acc, part_ml, seg_tab,
+                 win);
   // only a call that appends hands the lengths to the merge kernel for updating
-  ADAKV_LAUNCH("decode_combine", (decode_combine_kernel<D, G>), dim3(nseg, G), dim3(1024), s,
-               (const int4 *)seg_tab, k_new ? seg_len : nullptr, overflow, (const float *)part_acc,
-               (const float *)part_ml, out, lse);
+  launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
 }
 
 struct DecodeArgs {
@@ -814,6 +696,7 @@ struct DecodeArgs {
   int *seg_len, *overflow;
   float *out, *lse;
   char *ws;
+  Window win;
 };
 
 template <typename T, int D>
@@ -821,7 +704,7 @@ bool run_decode_g(const SeqTab &st, const Dims &dm, int headroom, const DecodePl
                   const DecodeArgs &a, hipStream_t s) {
 #define ADAKV_DECODE_G(G)                                                                       \
   run_decode<T, D, G>(st, dm, headroom, pl, a.q, a.k_new, a.v_new, a.cu, a.Kc, a.Vc, a.seg_len,   \
-                      a.overflow, a.out, a.lse, a.ws, s)
+                      a.overflow, a.out, a.lse, a.ws, a.win, s)
   switch (dm.g) {
     case 1: ADAKV_DECODE_G(1); return true;
     case 2: ADAKV_DECODE_G(2); return true;
@@ -832,16 +715,56 @@ bool run_decode_g(const SeqTab &st, const Dims &dm, int headroom, const DecodePl
 #undef ADAKV_DECODE_G
 }
 
+bool run_decode_t(const SeqTab &st, const Dims &dm, int dtype, int headroom, const DecodePlan &pl, const DecodeArgs &a,
+                  hipStream_t s) {
+  if (dtype == ADAKV_BF16)
+    return dm.d == 64 ? run_decode_g<unsigned short, 64>(st, dm, headroom, pl, a, s)
+                      : run_decode_g<unsigned short, 128>(st, dm, headroom, pl, a, s);
+  if (dtype == ADAKV_FP16)
+    return dm.d == 64 ? run_decode_g<f16_t, 64>(st, dm, headroom, pl, a, s)
+                      : run_decode_g<f16_t, 128>(st, dm, headroom, pl, a, s);
+  return dm.d == 64 ? run_decode_g<float, 64>(st, dm, headroom, pl, a, s)
+                    : run_decode_g<float, 128>(st, dm, headroom, pl, a, s);
+}
+
 }  // namespace
+
+#if ADAKV_DECODE_PART == 2
+
+hipError_t launch_decode_window(const SeqTab &st, const Dims &dm, int dtype, int headroom, int limit, int sinks,
+                                const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,
+                                int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s) {
+  const DecodePlan pl = plan_decode(st, dm, dtype, headroom, limit);
+  const DecodeArgs a = {q, k_new, v_new, cu, Kc, Vc, seg_len, overflow, out, lse, ws, {limit, sinks}};
+  return run_decode_t(st, dm, dtype, headroom, pl, a, s) ? hipGetLastError() : hipErrorInvalidValue;
+}
+
+#else
+
+void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, char *ws, int *new_len, int *overflow, float *out,
+                           float *lse, hipStream_t s) {
+  const float *part_acc = (const float *)(ws + pl.part_acc), *part_ml = (const float *)(ws + pl.part_ml);
+  const int4 *seg_tab = (const int4 *)(ws + pl.seg_tab);
+#define ADAKV_COMBINE(D, G)                                                                       \
+  if (d == D && g == G)                                                                           \
+    ADAKV_LAUNCH("decode_combine", (decode_combine_kernel<D, G>), dim3(nseg, G), dim3(1024), s,   \
+                 seg_tab, new_len, overflow, part_acc, part_ml, out, lse)
+#define ADAKV_COMBINE_D(D) ADAKV_COMBINE(D, 1); ADAKV_COMBINE(D, 2); ADAKV_COMBINE(D, 4); ADAKV_COMBINE(D, 8)
+  ADAKV_COMBINE_D(64);
+  ADAKV_COMBINE_D(128);
+#undef ADAKV_COMBINE_D
+#undef ADAKV_COMBINE
+}
 
 bool decode_supported(const Dims &dm) {
   return (dm.g == 1 || dm.g == 2 || dm.g == 4 || dm.g == 8) && (dm.d == 64 || dm.d == 128);
 }
 
-DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom) {
+DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom, int limit) {
   DecodePlan pl;
   const long long nseg = (long long)st.batch * dm.h_kv;
-  const long long cap = (long long)st.out_off[st.batch] + nseg * headroom;
+  long long cap = (long long)st.out_off[st.batch] + nseg * headroom;
+  if (cap > nseg * limit) cap = nseg * limit;               // (what a call with a window looks at)
   // Rows per workgroup: what fills one resident round, so that all workgroups start together and
   // none is left for a thin second round.  Three workgroups fit on a compute unit (768 on the
   // chip), two of the 16-bit kernel for g = 8 at d = 128, whose third part of P takes 32 more
@@ -876,13 +799,24 @@ DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom
     likely = (four < most ? four : most) > likely ? (four < most ? four : most) : likely;
   }
   const long long fixed = dm.w + headroom;
-  pl.whole = mfma && cap <= nseg * 384 && (likely + fixed) * dm.d <= 768 * 128 && (longest + fixed) * dm.d <= 1024 * 128;
+  likely = likely + fixed < limit ? likely + fixed : limit;
+  longest = longest + fixed < limit ? longest + fixed : limit;
+  pl.whole = mfma && cap <= nseg * 384 && likely * dm.d <= 768 * 128 && longest * dm.d <= 1024 * 128;
   pl.split = split;
   pl.nblk = (int)(cap / split + nseg);          // >= sum over segments of ceil(len / split)
   pl.part_acc = 0;
   pl.part_ml = align_up((size_t)pl.nblk * dm.g * dm.d * sizeof(float), 256);
   pl.seg_tab = pl.part_ml + align_up((size_t)pl.nblk * dm.g * 2 * sizeof(float), 256);
   pl.total = pl.seg_tab + align_up((size_t)nseg * sizeof(int4), 256);
+  if (limit < INT_MAX) {
+    // a workspace is as large as the call without a window needs it: fewer rows in shorter parts can be more parts
+    const DecodePlan full = plan_decode(st, dm, dtype, headroom, INT_MAX);
+    if (pl.nblk > full.nblk) {
+      const bool whole = pl.whole;
+      pl = full;                                            // (never fewer parts than the window's rows make)
+      pl.whole = whole;
+    }
+  }
   return pl;
 }
 
@@ -891,20 +825,8 @@ hipError_t launch_decode_attn(const SeqTab &st, const Dims &dm, int dtype, int h
                               void *Kc, void *Vc, int *seg_len, int *overflow, float *out,
                               float *lse, char *ws, hipStream_t s) {
   const DecodePlan pl = plan_decode(st, dm, dtype, headroom);
-  const DecodeArgs a = {q, k_new, v_new, cu, Kc, Vc, seg_len, overflow, out, lse, ws};
-  bool ok;
-  if (dtype == ADAKV_BF16) {
-    ok = dm.d == 64 ? run_decode_g<unsigned short, 64>(st, dm, headroom, pl, a, s)
-                    : run_decode_g<unsigned short, 128>(st, dm, headroom, pl, a, s);
-  } else if (dtype == ADAKV_FP16) {
-    ok = dm.d == 64 ? run_decode_g<f16_t, 64>(st, dm, headroom, pl, a, s)
-                    : run_decode_g<f16_t, 128>(st, dm, headroom, pl, a, s);
-  } else {
-    ok = dm.d == 64 ? run_decode_g<float, 64>(st, dm, headroom, pl, a, s)
-                    : run_decode_g<float, 128>(st, dm, headroom, pl, a, s);
-  }
-  if (!ok) return hipErrorInvalidValue;
-  return hipGetLastError();
+  const DecodeArgs a = {q, k_new, v_new, cu, Kc, Vc, seg_len, overflow, out, lse, ws, {}};
+  return run_decode_t(st, dm, dtype, headroom, pl, a, s) ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 hipError_t launch_append(const SeqTab &st, const Dims &dm, int dtype, int headroom,
@@ -926,5 +848,7 @@ hipError_t launch_append(const SeqTab &st, const Dims &dm, int dtype, int headro
 #undef ADAKV_LAUNCH_APPEND
   return hipGetLastError();
 }
+
+#endif  // ADAKV_DECODE_PART
 
 }  // namespace adakv

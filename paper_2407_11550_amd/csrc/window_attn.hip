@@ -1,0 +1,309 @@
+// Causal attention over a prompt, limited to a window and a few first tokens (the sinks): the softmax of Section 3.1 over
+// all rows of a sequence, in one pass over the keys with a running maximum and sum, and the log-sum-exp of the
+// last w rows, which the scoring call takes.
+//
+// Both products run on the matrix cores, S^T = K Q^T and O^T += V^T P^T, with the keys along the registers of a lane and
+// a query per lane: the maximum and the sum of a row take one exchange between the two halves of a wavefront, the
+// correction of O^T none, and what a lane holds of P is the second product's operand as it is (the contraction
+// runs in the order in which the lanes hold the keys, and V^T is read from LDS in that order).
+//
+// Bound by the matrix instructions: 4 d flops per visible pair.
+#include <math.h>
+
+#include "common.h"
+
+namespace adakv {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float M_INIT = -1.0e30f;             // finite "no key seen yet"
+
+struct BF16 { static constexpr int SIZE = 2; };
+struct FP16 { static constexpr int SIZE = 2; };
+struct FP32 { static constexpr int SIZE = 4; };
+template <typename T> constexpr bool is_f16 = false;
+template <> constexpr bool is_f16<FP16> = true;
+template <typename T> constexpr bool is_f32 = T::SIZE == 4;
+
+// Weights are at most 2^(LAZY + BIAS): the reference they are taken against is moved only when a maximum is 2^LAZY above
+// it.  fp16 weights travel 2^7 times larger, so that the smallest of full precision is 2^-21 of the reference.
+constexpr float LAZY = 8.0f;
+template <typename T> constexpr float BIAS = is_f16<T> ? 7.0f : 0.0f;
+
+struct Shape {
+  int h_q, h_kv, g, w, window, sinks;
+  float c_log2;
+  long long q_tok, q_head, k_tok, k_head, v_tok, v_head;     // bytes
+};
+
+constexpr int ROWS = 128;                      // query rows of a workgroup, 32 per wavefront
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// One element of a row, in 32 bits.
+template <typename T> __device__ __forceinline__ float element(const char *row, int e) {
+  if constexpr (is_f32<T>) return reinterpret_cast<const float *>(row)[e];
+  const unsigned short u = reinterpret_cast<const unsigned short *>(row)[e];
+  if constexpr (is_f16<T>) return (float)__builtin_bit_cast(_Float16, u);
+  return __builtin_bit_cast(float, (unsigned)u << 16);
+}
+template <typename T> __device__ __forceinline__ unsigned short round16(float x) {
+  if constexpr (is_f16<T>) return __builtin_bit_cast(unsigned short, (_Float16)x);
+  return __builtin_bit_cast(unsigned short, (__bf16)x);
+}
+// Two values rounded to the layer's 16-bit type, x0 in the lower half.
+template <typename T> __device__ __forceinline__ unsigned round2(float x0, float x1) {
+  return (unsigned)round16<T>(x0) | (unsigned)round16<T>(x1) << 16;
+}
+
+// Row r of a sequence by one wavefront, key by key and without the matrix cores: for rows that came out infinite or as
+// NaN.  A product over a tile multiplies hidden values by a weight of 0, which is no 0 for those; here hidden
+// keys have no part at all.
+template <typename T, int D>
+__device__ void careful_row(const Shape &sh, const char *q, const char *K, const char *V, int r, char *out, float *lse) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int lo = max(0, r - sh.window + 1), firsts = min(sh.sinks, lo), count = firsts + r - lo + 1;
+  float m = M_INIT, l = 0.0f, acc[E] = {};
+  for (int t0 = 0; t0 < count; t0 += 64) {
+    const int t = t0 + lane;
+    const bool on = t < count;
+    const int tt = min(t, count - 1), j = tt < firsts ? tt : lo + tt - firsts;
+    float s = 0.0f;
+    for (int e = 0; e < D; ++e) s = fmaf(element<T>(q, e), element<T>(K + j * sh.k_tok, e), s);
+    s = on ? s * sh.c_log2 : -INFINITY;
+    float top = s;
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float mn = fmaxf(m, top), corr = exp2f(m - mn), p = on ? exp2f(s - mn) : 0.0f;
+    m = mn;
+    float sum = p;
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    l = l * corr + sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= corr;
+    for (int u = 0; u < min(64, count - t0); ++u) {
+      const float pu = __shfl(p, u);
+      const int ju = __builtin_amdgcn_readfirstlane(__shfl(j, u));
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(pu, element<T>(V + ju * sh.v_tok, lane * E + e), acc[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float x = acc[e] / l;
+    if constexpr (is_f32<T>) reinterpret_cast<float *>(out)[lane * E + e] = x;
+    else reinterpret_cast<unsigned short *>(out)[lane * E + e] = round16<T>(x);
+  }
+  if (lse && lane == 0) *lse = (m + log2f(l)) * LN2;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
+                                                             const char *__restrict__ K, const char *__restrict__ V,
+                                                             char *__restrict__ out, float *__restrict__ row_lse) {
+  constexpr int ROWB = D * T::SIZE, CH = ROWB / 16;            // 16-byte words of a row
+  constexpr int KT = is_f32<T> ? 32 : 64, KB = KT / 32;        // keys of a tile
+  constexpr int CB = D / 32;                                   // column blocks of O^T
+  constexpr int LOADS = KT * CH / 256;                         // words per thread and tensor
+  __shared__ __align__(16) u32x4 shK[KT * CH], shV[KT * CH];
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // ---- which rows of which head ------------------------------------------------------------------------------
+  const int item = blockIdx.x, hh = item % sh.h_q, rank = item / sh.h_q;
+  const int c = hh % sh.h_kv, hq = c * sh.g + hh / sh.h_kv;
+  const int b = find_seq(ct, st.batch, rank);
+  const int n = st.n[b] + sh.w;
+  const int q0 = (ct.off[b + 1] - 1 - rank) * ROWS;            // the longest rows first
+  const char *Kh = K + st.tok_off[b] * sh.k_tok + c * sh.k_head, *Vh = V + st.tok_off[b] * sh.v_tok + c * sh.v_head;
+  const char *Qh = q + st.tok_off[b] * sh.q_tok + hq * sh.q_head;
+  const int w0 = q0 + 32 * wv, r = min(w0 + l32, n - 1);       // the wavefront's first row, this lane's
+
+  u32x4 qf[CH / 2];
+#pragma unroll
+  for (int s = 0; s < CH / 2; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + r * sh.q_tok + (2 * s + half) * 16);
+
+  floatx16 acc[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) acc[cb] = floatx16{0};
+  float m = M_INIT, l = 0.0f;
+
+  const int last = min(q0 + ROWS, n) - 1;                      // the workgroup's last row
+  const int lo = max(0, q0 - sh.window + 1) / KT, hi = last / KT;
+  const int firsts = min((int)(((long long)sh.sinks + KT - 1) / KT), lo), tiles = firsts + hi - lo + 1;
+  for (int t = 0; t < tiles; ++t) {
+    const int j0 = (t < firsts ? t : lo + t - firsts) * KT;
+    u32x4 kk[LOADS], vv[LOADS];
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int word = tid + 256 * u, row = min(j0 + word / CH, n - 1);
+      kk[u] = *reinterpret_cast<const u32x4 *>(Kh + row * sh.k_tok + (word % CH) * 16);
+      vv[u] = *reinterpret_cast<const u32x4 *>(Vh + row * sh.v_tok + (word % CH) * 16);
+    }
+    __syncthreads();                                           // the tile before is done with
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int word = tid + 256 * u, row = word / CH, ch = word % CH;
+      shK[row * CH + (ch ^ (row & (CH < 16 ? CH - 1 : 15)))] = kk[u];
+      shV[row * CH + (is_f32<T> ? ch : ch ^ (2 * (row & (CH / 2 - 1))))] = vv[u];
+    }
+    __syncthreads();
+    // a tile that none of the wavefront's rows sees
+    if (j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window)) continue;
+
+    floatx16 sc[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      sc[kb] = floatx16{0};
+#pragma unroll
+      for (int s = 0; s < CH / 2; ++s) {
+        const int row = 32 * kb + l32;
+        const u32x4 kw = shK[row * CH + ((2 * s + half) ^ (row & (CH < 16 ? CH - 1 : 15)))];
+        if constexpr (is_f32<T>) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const unsigned ka = kw[e], qa = qf[s][e];
+            sc[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc[kb], 0, 0, 0);
+          }
+        } else if constexpr (is_f16<T>) {
+          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kw), __builtin_bit_cast(f16x8, qf[s]), sc[kb], 0, 0, 0);
+        } else {
+          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw), __builtin_bit_cast(bf16x8, qf[s]), sc[kb], 0, 0, 0);
+        }
+      }
+    }
+    const int j1 = j0 + KT - 1;
+    if (j1 > w0 || !(j0 > w0 + 31 - sh.window || j1 < sh.sinks)) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
+          if (j > r || (j <= r - sh.window && j >= sh.sinks)) sc[kb][i] = -INFINITY;
+        }
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+    top = fmaxf(top, other_half(top)) * sh.c_log2;
+    if (__any(top > m + LAZY)) {
+      const float mn = fmaxf(m, top), corr = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) acc[cb] *= corr;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], sh.c_log2, BIAS<T> - m));
+        l += sc[kb][i];
+      }
+
+    if constexpr (is_f32<T>) {
+      const float *vt = reinterpret_cast<const float *>(shV);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const float va = vt[(8 * (i / 4) + 4 * half + i % 4) * D + 32 * cb + l32];
+          const float pa = sc[0][i];
+          acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, pa, acc[cb], 0, 0, 0);
+        }
+    } else {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      typedef __attribute__((address_space(3))) char lds_char;
+      const int sub = lane & 15, row4 = 4 * half + sub / 4, col16 = (lane >> 4) & 1;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          u32x4 pb;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pb[i] = round2<T>(sc[kb][8 * ks + 2 * i], sc[kb][8 * ks + 2 * i + 1]);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            s16x4 v2[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
+              const int row = 32 * kb + 16 * ks + 8 * x + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
+              const int at = (row * CH + (ch ^ (2 * (row & (CH / 2 - 1))))) * 16 + 8 * (sub % 2);
+              v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)shV + at));
+            }
+            const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
+            const u32x4 va = {a0.x, a0.y, a1.x, a1.y};
+            if constexpr (is_f16<T>)
+              acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, va), __builtin_bit_cast(f16x8, pb), acc[cb], 0, 0, 0);
+            else
+              acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), acc[cb], 0, 0, 0);
+          }
+        }
+    }
+  }
+
+  if (w0 >= n) return;
+  l += other_half(l);
+  float *lse = row_lse ? row_lse + ((long long)b * sh.h_q + hq) * sh.w - st.n[b] : nullptr;     // of row 0
+  char *oh = out + (st.tok_off[b] * sh.h_q + hq) * ROWB;
+  const long long o_tok = (long long)sh.h_q * ROWB;
+  float worst = l;                             // infinite or NaN where any of them is
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) worst = fmaf(acc[cb][i], 0.0f, worst);
+  if (__any(!(__builtin_fabsf(worst) < INFINITY))) {
+    for (int i = 0; i < min(32, n - w0); ++i) {
+      const int ri = w0 + i;
+      careful_row<T, D>(sh, Qh + ri * sh.q_tok, Kh, Vh, ri, oh + ri * o_tok, lse && ri >= st.n[b] ? lse + ri : nullptr);
+    }
+    return;
+  }
+  if (w0 + l32 >= n) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  char *dst = oh + r * o_tok;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int col = 32 * cb + 8 * k + 4 * half;
+      const float x0 = acc[cb][4 * k] * inv, x1 = acc[cb][4 * k + 1] * inv, x2 = acc[cb][4 * k + 2] * inv, x3 = acc[cb][4 * k + 3] * inv;
+      if constexpr (is_f32<T>) *reinterpret_cast<float4 *>(dst + col * 4) = make_float4(x0, x1, x2, x3);
+      else *reinterpret_cast<uint2 *>(dst + col * 2) = make_uint2(round2<T>(x0, x1), round2<T>(x2, x3));
+    }
+  if (lse && r >= st.n[b] && half == 0) lse[r] = l > 0.0f ? (m - BIAS<T> + log2f(l)) * LN2 : -INFINITY;
+}
+
+}  // namespace
+
+hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const void *q, long long q_tok, long long q_head,
+                              const void *K, const void *V, int window, int sinks, void *out, float *row_lse, hipStream_t s) {
+  const long long e = dtype == ADAKV_FP32 ? 4 : 2;
+  const Shape sh = {dm.h_q, dm.h_kv, dm.g, dm.w, window, sinks, dm.scale * LOG2E, q_tok * e, q_head * e, dm.k_stride_tok * e,
+                    dm.k_stride_head * e, dm.v_stride_tok * e, dm.v_stride_head * e};
+  ChunkTab ct;
+  ct.off[0] = 0;
+  for (int b = 0; b < st.batch; ++b) ct.off[b + 1] = ct.off[b] + (st.n[b] + dm.w + ROWS - 1) / ROWS;
+  for (int b = st.batch + 1; b <= ADAKV_MAX_BATCH; ++b) ct.off[b] = ct.off[st.batch];
+  const dim3 grid((unsigned)((long long)ct.off[st.batch] * dm.h_q));
+#define ADAKV_WINDOW(T, D)                                                                                              \
+  ADAKV_LAUNCH("window_attn", (window_attn_kernel<T, D>), grid, dim3(256), s, st, ct, sh, (const char *)q, (const char *)K, \
+               (const char *)V, (char *)out, row_lse)
+  if (dtype == ADAKV_BF16) { if (dm.d == 64) ADAKV_WINDOW(BF16, 64); else ADAKV_WINDOW(BF16, 128); }
+  else if (dtype == ADAKV_FP16) { if (dm.d == 64) ADAKV_WINDOW(FP16, 64); else ADAKV_WINDOW(FP16, 128); }
+  else { if (dm.d == 64) ADAKV_WINDOW(FP32, 64); else ADAKV_WINDOW(FP32, 128); }
+#undef ADAKV_WINDOW
+  return hipGetLastError();
+}
+
+}  // namespace adakv
