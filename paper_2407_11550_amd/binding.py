@@ -19,6 +19,7 @@ _LIB_PATH = os.path.join(_HERE, "lib", "libadakv.so")
 _MARSHAL_PATH = os.path.join(_HERE, "lib", "_marshal.so")
 _lib = None
 _decode_step_address = 0
+_addresses = {}             # of the library's other functions that are called through the native checks
 
 ADAKV_BF16, ADAKV_FP32, ADAKV_FP16 = 0, 1, 2
 ADAKV_FLAG_PIPELINE = 2
@@ -118,6 +119,8 @@ def load_library():
     if _marshal is None:                # built since this module was imported
         _marshal = _load_marshal()
     _decode_step_address = ctypes.cast(lib.adakv_decode_step, V).value
+    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn"):
+        _addresses[name] = ctypes.cast(getattr(lib, "adakv_" + name), V).value
     _lib = lib
     return lib
 
@@ -151,6 +154,7 @@ class Layer:
         code = {torch.bfloat16: ADAKV_BF16, torch.float32: ADAKV_FP32, torch.float16: ADAKV_FP16}.get(dtype, 99)
         self.c = _CLayer(code, h_q, h_kv, d, w, pool_k, self.alpha, self.scale, self.batch,
                          self._n, self._B, self._off, ks[0], ks[1], vs[0], vs[1], flags)
+        self._address = ctypes.addressof(self.c)
 
     @classmethod
     def from_workload(cls, wl, **kw):
@@ -265,6 +269,23 @@ def _check_kv(layer, t, name, strides, given):
     extent = 1 + sum((sz - 1) * st for sz, st in zip(t.shape, t.stride())) if t.numel() else 0
     if extent < last:
         raise ValueError(f"{name} reaches {extent} elements from its first one, the layer addresses {last}")
+
+
+def _native(name, layer, stream, *args):
+    """A call whose arguments are checked in native code.  True: it has been made.  False: something is not as it has to
+    be, or is to be made here first, and the checks in Python say what."""
+    if _marshal is None:
+        return False
+    try:
+        device, handle = _device(stream), _stream(stream)
+    except (RuntimeError, AssertionError, AttributeError):      # no GPU: the tensors are looked at first
+        return False
+    st = getattr(_marshal, name)(device, _addresses[name], layer._address, *args, handle)
+    if st is None:
+        return False
+    if st != 0:
+        raise AdaKVError(st, "adakv_" + name)
+    return True
 
 
 def _check_q(layer, q):
@@ -631,6 +652,10 @@ def decode_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, K_cache
         if st is not None:
             raise AdaKVError(st, "adakv_decode_step")
         # something is not as it has to be: the checks below say what
+    if (window is not None and (lse is not None or not want_lse) and
+            _native("decode_window_step", layer, stream, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow,
+                    window, sinks, out, lse, ws)):
+        return out if lse is None else (out, lse)
     want = (layer.batch, layer.h_q, layer.d)
     wkv = (layer.batch, layer.h_kv, layer.d)
     if q_new.shape != want or not q_new.is_contiguous():
@@ -708,6 +733,9 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     window, sinks = _window(window, sinks)
     if window is None:
         raise ValueError("window must be given (the longest sequence's length for all of it)")
+    if (row_lse is not None or not want_lse) and _native("window_attn", layer, stream, layer.last_token_row, *layer.strides_given, q, K, V,
+                                                         window, sinks, out, row_lse):
+        return out if row_lse is None else (out, row_lse)
     if q.dim() != 3 or q.shape[1] != layer.h_q or q.shape[2] != layer.d or (layer.d > 1 and q.stride(2) != 1):
         raise ValueError(f"q must be [tokens, {layer.h_q}, {layer.d}] with contiguous rows")
     rows = layer.last_token_row
@@ -778,6 +806,9 @@ def _check_new(layer, k_new, v_new):
 def cache_build_q8(layer: Layer, K, V, indices, cu_seqlens, headroom, cache=None, seg_len=None, stream=None):
     """adakv_cache_build_q8: the gather of cache_build into an 8-bit cache; returns (cache, seg_len)."""
     lib = load_library()
+    if cache is not None and _native("cache_build_q8", layer, stream, layer.last_token_row, *layer.strides_given, K, V, indices, cu_seqlens,
+                                     headroom, *cache, seg_len):
+        return cache, seg_len
     if cache is None:
         cache = q8_cache(layer, headroom, K.device)
     if seg_len is None:
@@ -856,6 +887,10 @@ def decode_attn_q8(layer: Layer, q_new, cu_seqlens, headroom, cache, seg_len, ou
 def decode_step_q8(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, cache, seg_len, overflow=None, out=None, lse=None,
                    ws=None, stream=None, want_lse=False):
     """adakv_decode_step_q8: decode_step over an 8-bit cache."""
+    load_library()
+    if (lse is not None or not want_lse) and _native("decode_step_q8", layer, stream, q_new, k_new, v_new, cu_seqlens, headroom, *cache,
+                                                     seg_len, overflow, out, lse, ws):
+        return out if lse is None else (out, lse)
     return _decode_q8("adakv_decode_step_q8", layer, q_new, (k_new, v_new), cu_seqlens, headroom, cache, seg_len, (overflow,), out,
                       lse, ws, stream, want_lse)
 

@@ -16,6 +16,7 @@
 namespace adakv {
 namespace {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 
@@ -100,11 +101,12 @@ __global__ __launch_bounds__(256) void cache_build_q8_kernel(
 #pragma unroll
     for (int e = 0; e < EPL; ++e) f[e] = to_range(f[e], inv);
     if (t0 + r < len) {
+      // (past the caches: 96 000 rows of 128 bf16 values 16.8 us, 16.2 with this, 14.1 at the rate of a copy)
       const unsigned w0 = to_codes(f[0], f[1], f[2], f[3]);
       if constexpr (EPL == 8)
-        *reinterpret_cast<uint2 *>(dst + r * D) = make_uint2(w0, to_codes(f[4], f[5], f[6], f[7]));
+        __builtin_nontemporal_store(u32x2{w0, to_codes(f[4], f[5], f[6], f[7])}, reinterpret_cast<u32x2 *>(dst + r * D));
       else
-        *reinterpret_cast<unsigned *>(dst + r * D) = w0;
+        __builtin_nontemporal_store(w0, reinterpret_cast<unsigned *>(dst + r * D));
     }
   }
   if (lane == 0) (values ? v_scale : k_scale)[first_scale(row0, s) + blk] = pow2(k);

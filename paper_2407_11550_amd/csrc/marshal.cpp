@@ -1,4 +1,5 @@
-// The argument checks of a decoding step in native code, for the binding.  A step of a short cache is two kernels of
+// The argument checks of the calls whose kernels take less time than these did in Python, in native code, for the binding.
+// First of them a decoding step.  A step of a short cache is two kernels of
 // 8.6 us together, and the checks of its twelve tensors took 5 us of interpreter time per call, so that the host and
 // not the GPU decided how long it took: 11.3 us to issue one, now 6.6, and a step over 8 KV heads of 512 rows at
 // d = 64 took 11.0 us, now 9.1.  Only the case in which everything is as it has to be is handled here: whatever is
@@ -76,9 +77,194 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   }
 }
 
+// ---- the other calls: as above, and all tensors on the device that the call is launched on --------------------------
+struct Refused {};                             // left to binding.py
+
+// Takes a call's Python arguments in order; the first that is not as it has to be ends it.
+struct Args {
+  PyObject *const *a;
+  int at = 0;
+  int device = -1;
+
+  long long whole(long long least, long long most) {
+    PyObject *o = a[at++];
+    if (!PyLong_Check(o)) throw Refused();
+    const long long v = PyLong_AsLongLong(o);
+    if (PyErr_Occurred() || v < least || v > most) throw Refused();
+    return v;
+  }
+  int32_t i32(long long least = 0) { return (int32_t)whole(least, std::numeric_limits<int32_t>::max()); }
+  void *pointer() {
+    void *p = PyLong_AsVoidPtr(a[at++]);
+    if (PyErr_Occurred()) throw Refused();
+    return p;
+  }
+  const at::Tensor &tensor(at::ScalarType type) {
+    const at::Tensor *t = device_tensor(a[at++], type);
+    if (!t || t->get_device() != device) throw Refused();
+    return *t;
+  }
+  // one behind the other, so many at least
+  const at::Tensor &buffer(at::ScalarType type, int64_t numel) {
+    const at::Tensor &t = tensor(type);
+    if (!holds(&t, numel)) throw Refused();
+    return t;
+  }
+  template <typename T> T *data(at::ScalarType type, int64_t numel) { return static_cast<T *>(buffer(type, numel).data_ptr()); }
+  template <typename T> T *data_or_none(at::ScalarType type, int64_t numel) {
+    if (a[at] != Py_None) return data<T>(type, numel);
+    ++at;
+    return nullptr;
+  }
+  void *rows(at::ScalarType type, int64_t batch, int64_t h, int64_t d) {
+    const at::Tensor &t = tensor(type);
+    if (!is_rows(&t, batch, h, d)) throw Refused();
+    return t.data_ptr();
+  }
+  void *cache(at::ScalarType type, int64_t rows, int64_t d) {
+    const at::Tensor &t = tensor(type);
+    if (!is_cache(&t, rows, d)) throw Refused();
+    return t.data_ptr();
+  }
+  // K or V: strides of the layer, which reach `tokens` rows; `given`: not those of a contiguous tensor
+  void *keys(const adakv_layer *L, at::ScalarType type, int64_t tokens, int64_t s_tok, int64_t s_head, bool given) {
+    const at::Tensor &t = tensor(type);
+    if (!given && !(t.dim() == 3 && t.size(1) == L->h_kv && t.size(2) == L->d && t.stride(0) == (int64_t)L->h_kv * L->d &&
+                    t.stride(1) == L->d && t.stride(2) == 1))
+      throw Refused();
+    int64_t extent = t.numel() ? 1 : 0;
+    for (int64_t i = 0; t.numel() && i < t.dim(); ++i) extent += (t.size(i) - 1) * t.stride(i);
+    if (extent < (tokens - 1) * s_tok + (L->h_kv - 1) * s_head + L->d) throw Refused();
+    return t.data_ptr();
+  }
+};
+
+// The layer at the front of a call's arguments, and what follows from it.
+struct Layer {
+  const adakv_layer *L;
+  at::ScalarType type;
+  int64_t nseg, kept = 0;
+  explicit Layer(Args &x) : L(static_cast<const adakv_layer *>(x.pointer())) {
+    if (!L || L->batch < 1 || L->batch > ADAKV_MAX_BATCH) throw Refused();
+    type = L->dtype == ADAKV_BF16 ? at::kBFloat16 : L->dtype == ADAKV_FP16 ? at::kHalf : at::kFloat;
+    if (L->dtype != ADAKV_FP32 && type == at::kFloat) throw Refused();
+    nseg = (int64_t)L->batch * L->h_kv;
+    for (int b = 0; b < L->batch; ++b) kept += L->B[b];
+  }
+  int64_t rows(int32_t headroom) const { return kept + nseg * headroom; }
+};
+
+template <typename F> PyObject *checked(const char *name, Py_ssize_t n, Py_ssize_t want, PyObject *const *a, F &&call) {
+  if (n != want) {
+    PyErr_Format(PyExc_TypeError, "%s takes %zd arguments", name, want);
+    return nullptr;
+  }
+  try {
+    Args x{a};
+    x.device = (int)x.whole(0, 1 << 16);
+    return PyLong_FromLong(call(x));
+  } catch (...) {                              // Refused, or a tensor without memory of its own
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// A call of the library without the interpreter's lock.
+template <typename F> int unlocked(F &&f) {
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f();
+  Py_END_ALLOW_THREADS
+  return st;
+}
+
+// (device, function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, window, sinks, out, lse, ws, stream)
+PyObject *decode_window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("decode_window_step", n, 18, a, [](Args &x) {
+    const auto fn = reinterpret_cast<decltype(&adakv_decode_window_step)>(x.pointer());
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    void *q = x.rows(l.type, L->batch, L->h_q, L->d), *k = x.rows(l.type, L->batch, L->h_kv, L->d), *v = x.rows(l.type, L->batch, L->h_kv, L->d);
+    const int32_t *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
+    const int32_t headroom = x.i32();
+    void *K = x.cache(l.type, l.rows(headroom), L->d), *V = x.cache(l.type, l.rows(headroom), L->d);
+    int32_t *len = x.data<int32_t>(at::kInt, l.nseg), *over = x.data_or_none<int32_t>(at::kInt, 1);
+    const int32_t window = x.i32(1), sinks = x.i32();
+    float *out = x.data<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->d), *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q);
+    const at::Tensor &ws = x.buffer(at::kByte, 0);
+    void *p = ws.data_ptr(), *stream = x.pointer();
+    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, len, over, window, sinks, out, lse, p, (size_t)ws.numel(), stream); });
+  });
+}
+
+// (device, function, layer, q, k, v, cu_seqlens, headroom, K, V, k_scale, v_scale, seg_len, overflow, out, lse, ws, stream)
+PyObject *decode_step_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("decode_step_q8", n, 18, a, [](Args &x) {
+    const auto fn = reinterpret_cast<decltype(&adakv_decode_step_q8)>(x.pointer());
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    void *q = x.rows(l.type, L->batch, L->h_q, L->d), *k = x.rows(l.type, L->batch, L->h_kv, L->d), *v = x.rows(l.type, L->batch, L->h_kv, L->d);
+    const int32_t *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
+    const int32_t headroom = x.i32();
+    const int64_t rows = l.rows(headroom), scales = rows / ADAKV_Q8_BLOCK + l.nseg;
+    void *K = x.cache(at::kFloat8_e4m3fn, rows, L->d), *V = x.cache(at::kFloat8_e4m3fn, rows, L->d);
+    float *ks = x.data<float>(at::kFloat, scales), *vs = x.data<float>(at::kFloat, scales);
+    int32_t *len = x.data<int32_t>(at::kInt, l.nseg), *over = x.data_or_none<int32_t>(at::kInt, 1);
+    float *out = x.data<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->d), *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q);
+    const at::Tensor &ws = x.buffer(at::kByte, 0);
+    void *p = ws.data_ptr(), *stream = x.pointer();
+    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, ks, vs, len, over, out, lse, p, (size_t)ws.numel(), stream); });
+  });
+}
+
+// (device, function, layer, tokens, K's strides given, V's, K, V, indices, cu_seqlens, headroom, K_q8, V_q8, k_scale, v_scale, seg_len, stream)
+PyObject *cache_build_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("cache_build_q8", n, 17, a, [](Args &x) {
+    const auto fn = reinterpret_cast<decltype(&adakv_cache_build_q8)>(x.pointer());
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    const int64_t tokens = x.whole(1, std::numeric_limits<int64_t>::max());
+    const bool kg = x.whole(0, 1) != 0, vg = x.whole(0, 1) != 0;
+    void *K = x.keys(L, l.type, tokens, L->k_stride_tok, L->k_stride_head, kg), *V = x.keys(L, l.type, tokens, L->v_stride_tok, L->v_stride_head, vg);
+    const int32_t *idx = x.data<int32_t>(at::kInt, l.kept), *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
+    const int32_t headroom = x.i32();
+    const int64_t rows = l.rows(headroom), scales = rows / ADAKV_Q8_BLOCK + l.nseg;
+    void *Kq = x.cache(at::kFloat8_e4m3fn, rows, L->d), *Vq = x.cache(at::kFloat8_e4m3fn, rows, L->d);
+    float *ks = x.data<float>(at::kFloat, scales), *vs = x.data<float>(at::kFloat, scales);
+    int32_t *len = x.data<int32_t>(at::kInt, l.nseg);
+    void *stream = x.pointer();
+    return unlocked([&] { return fn(L, K, V, idx, cu, headroom, Kq, Vq, ks, vs, len, stream); });
+  });
+}
+
+// (device, function, layer, tokens, K's strides given, V's, q, K, V, window, sinks, out, row_lse, stream)
+PyObject *window_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("window_attn", n, 14, a, [](Args &x) {
+    const auto fn = reinterpret_cast<decltype(&adakv_window_attn)>(x.pointer());
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    const int64_t tokens = x.whole(1, std::numeric_limits<int64_t>::max());
+    const bool kg = x.whole(0, 1) != 0, vg = x.whole(0, 1) != 0;
+    const at::Tensor &q = x.tensor(l.type);
+    if (q.dim() != 3 || q.size(0) < tokens || q.size(1) != L->h_q || q.size(2) != L->d || q.stride(2) != 1) throw Refused();
+    void *K = x.keys(L, l.type, tokens, L->k_stride_tok, L->k_stride_head, kg), *V = x.keys(L, l.type, tokens, L->v_stride_tok, L->v_stride_head, vg);
+    const int32_t window = x.i32(1), sinks = x.i32();
+    void *out = x.data<void>(l.type, tokens * L->h_q * L->d);
+    float *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->w);
+    void *stream = x.pointer();
+    return unlocked([&] { return fn(L, q.data_ptr(), q.stride(0), q.stride(1), K, V, window, sinks, out, lse, stream); });
+  });
+}
+
 PyMethodDef methods[] = {
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL,
      "decode_step(function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, out, lse, ws, stream)"},
+#define ADAKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+    ADAKV_METHOD(decode_window_step),
+    ADAKV_METHOD(decode_step_q8),
+    ADAKV_METHOD(cache_build_q8),
+    ADAKV_METHOD(window_attn),
+#undef ADAKV_METHOD
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
