@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import itertools
 import os
 from typing import NamedTuple
 
@@ -119,7 +120,7 @@ def load_library():
     if _marshal is None:                # built since this module was imported
         _marshal = _load_marshal()
     _decode_step_address = ctypes.cast(lib.adakv_decode_step, V).value
-    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn"):
+    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8"):
         _addresses[name] = ctypes.cast(getattr(lib, "adakv_" + name), V).value
     _lib = lib
     return lib
@@ -166,9 +167,19 @@ class Layer:
         packed one after the other)."""
         if not picks or any(not 0 <= int(b) < self.batch for b in picks):
             raise ValueError(f"picks must name sequences of the layer, 0 to {self.batch - 1}, one at least")
-        ks, vs = (s if given else None for s, given in zip((self.k_strides, self.v_strides), self.strides_given))
-        return Layer(self.torch_dtype, self.h_q, self.h_kv, self.d, self.w, self.pool_k, self.alpha, [self.n[b] for b in picks],
-                     [self.B[b] for b in picks], scale=self.scale, k_strides=ks, v_strides=vs, flags=int(self.c.flags))
+        # (a copy with other sequences: made anew it took longer than moving a small cache)
+        new = object.__new__(type(self))
+        new.__dict__.update(self.__dict__)
+        new.n, new.B = [self.n[b] for b in picks], [self.B[b] for b in picks]
+        new.batch = len(new.n)
+        new.tok_off = [0, *itertools.accumulate(nb + self.w for nb in new.n)]
+        new._rows_out, new._segments, new._scores, new._last_row = sum(new.B), new.batch * self.h_kv, self.h_kv * sum(new.n), None
+        new._n, new._B = (ctypes.c_int32 * new.batch)(*new.n), (ctypes.c_int32 * new.batch)(*new.B)
+        new._off = (ctypes.c_int64 * (new.batch + 1))(*new.tok_off)
+        new.c = _CLayer.from_buffer_copy(self.c)
+        new.c.batch, new.c.n, new.c.B, new.c.tok_off = new.batch, new._n, new._B, new._off
+        new._address = ctypes.addressof(new.c)
+        return new
 
     @property
     def last_token_row(self):
@@ -271,16 +282,17 @@ def _check_kv(layer, t, name, strides, given):
         raise ValueError(f"{name} reaches {extent} elements from its first one, the layer addresses {last}")
 
 
-def _native(name, layer, stream, *args):
+def _native(name, layer, stream, *args, check=None):
     """A call whose arguments are checked in native code.  True: it has been made.  False: something is not as it has to
     be, or is to be made here first, and the checks in Python say what."""
+    load_library()
     if _marshal is None:
         return False
     try:
         device, handle = _device(stream), _stream(stream)
     except (RuntimeError, AssertionError, AttributeError):      # no GPU: the tensors are looked at first
         return False
-    st = getattr(_marshal, name)(device, _addresses[name], layer._address, *args, handle)
+    st = getattr(_marshal, check or name)(device, _addresses[name], layer._address, *args, handle)
     if st is None:
         return False
     if st != 0:
@@ -887,7 +899,6 @@ def decode_attn_q8(layer: Layer, q_new, cu_seqlens, headroom, cache, seg_len, ou
 def decode_step_q8(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, cache, seg_len, overflow=None, out=None, lse=None,
                    ws=None, stream=None, want_lse=False):
     """adakv_decode_step_q8: decode_step over an 8-bit cache."""
-    load_library()
     if (lse is not None or not want_lse) and _native("decode_step_q8", layer, stream, q_new, k_new, v_new, cu_seqlens, headroom, *cache,
                                                      seg_len, overflow, out, lse, ws):
         return out if lse is None else (out, lse)
@@ -931,6 +942,9 @@ def cache_move(layer: Layer, picks, cu_seqlens, headroom, K_cache, V_cache, seg_
             return tuple(_ptr(t, nm, lay.torch_dtype) for t, nm in ((K, "K_cache"), (V, "V_cache"))), dict(K=K, V=V)
         return at
 
+    if _native("cache_move", layer, stream, picks, cu_seqlens, headroom, K_cache, V_cache, None, None, seg_len, headroom_out, cu_out, K_out,
+               V_out, None, None, len_out, overflow):
+        return layer.pick(picks), cu_out, K_out, V_out, len_out
     rows = cache_rows(layer.pick(picks), headroom_out)
     if K_out is None:
         K_out = torch.zeros((rows, layer.d), dtype=layer.torch_dtype, device=K_cache.device)
@@ -944,6 +958,9 @@ def cache_move(layer: Layer, picks, cu_seqlens, headroom, K_cache, V_cache, seg_
 def cache_move_q8(layer: Layer, picks, cu_seqlens, headroom, cache, seg_len, headroom_out, cu_out=None, out=None, len_out=None,
                   overflow=None, stream=None):
     """adakv_cache_move_q8: cache_move for an 8-bit cache.  Returns (layer.pick(picks), cu_out, out, len_out)."""
+    if out is not None and _native("cache_move_q8", layer, stream, picks, cu_seqlens, headroom, *cache, seg_len, headroom_out, cu_out, *out,
+                                   len_out, overflow, check="cache_move"):
+        return layer.pick(picks), cu_out, out, len_out
     if out is None:
         out = q8_cache(layer.pick(picks), headroom_out, cache.K.device)
     to, cu_out, len_out = _move("adakv_cache_move_q8", layer, picks, cu_seqlens, headroom, lambda lay, hr: _q8_ptrs(lay, hr, cache), seg_len,

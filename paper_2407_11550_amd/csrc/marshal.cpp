@@ -256,6 +256,55 @@ PyObject *window_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (device, function, layer, picks, cu_seqlens, headroom, K, V, k_scale, v_scale, seg_len, headroom_out, cu_out, K_out, V_out, k_scale_out,
+// v_scale_out, len_out, overflow, stream); scales of a cache in 8 bits, else None: the function is the one for it
+PyObject *cache_move(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("cache_move", n, 20, a, [](Args &x) {
+    void *fn = x.pointer();
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    PyObject *picks = x.a[x.at++];
+    if (!PyList_CheckExact(picks) || PyList_GET_SIZE(picks) < 1 || PyList_GET_SIZE(picks) > ADAKV_MAX_BATCH) throw Refused();
+    const int32_t count = (int32_t)PyList_GET_SIZE(picks);
+    int32_t from[ADAKV_MAX_BATCH];
+    int64_t kept = 0;
+    for (int32_t i = 0; i < count; ++i) {
+      PyObject *o = PyList_GET_ITEM(picks, i);
+      const long long b = PyLong_CheckExact(o) ? PyLong_AsLongLong(o) : -1;
+      if (PyErr_Occurred() || b < 0 || b >= L->batch) throw Refused();
+      from[i] = (int32_t)b;
+      kept += L->B[b];
+    }
+    const int32_t *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
+    const bool q8 = x.a[x.at + 3] != Py_None;
+    const at::ScalarType type = q8 ? at::kFloat8_e4m3fn : l.type;
+    struct { void *K, *V; float *ks, *vs; } c[2];
+    int32_t headroom[2], *cu_out = nullptr;
+    const int32_t *len = nullptr;
+    for (int o = 0; o < 2; ++o) {              // the source, the destination
+      const int64_t nseg = o ? (int64_t)count * L->h_kv : l.nseg;
+      headroom[o] = x.i32();
+      if (o) cu_out = x.data<int32_t>(at::kInt, nseg + 1);
+      const int64_t rows = (o ? kept : l.kept) + nseg * headroom[o], scales = rows / ADAKV_Q8_BLOCK + nseg;
+      c[o].K = x.cache(type, rows, L->d);
+      c[o].V = x.cache(type, rows, L->d);
+      c[o].ks = x.data_or_none<float>(at::kFloat, scales);
+      c[o].vs = x.data_or_none<float>(at::kFloat, scales);
+      if ((c[o].ks != nullptr) != q8 || (c[o].vs != nullptr) != q8) throw Refused();
+      if (!o) len = x.data<int32_t>(at::kInt, nseg);
+    }
+    int32_t *len_out = x.data<int32_t>(at::kInt, (int64_t)count * L->h_kv), *over = x.data_or_none<int32_t>(at::kInt, 1);
+    void *stream = x.pointer();
+    return unlocked([&] {
+      if (q8)
+        return reinterpret_cast<decltype(&adakv_cache_move_q8)>(fn)(L, count, from, cu, headroom[0], c[0].K, c[0].V, c[0].ks, c[0].vs, len, headroom[1],
+                                                                   cu_out, c[1].K, c[1].V, c[1].ks, c[1].vs, len_out, over, stream);
+      return reinterpret_cast<decltype(&adakv_cache_move)>(fn)(L, count, from, cu, headroom[0], c[0].K, c[0].V, len, headroom[1], cu_out, c[1].K,
+                                                              c[1].V, len_out, over, stream);
+    });
+  });
+}
+
 PyMethodDef methods[] = {
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL,
      "decode_step(function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, out, lse, ws, stream)"},
@@ -264,6 +313,7 @@ PyMethodDef methods[] = {
     ADAKV_METHOD(decode_step_q8),
     ADAKV_METHOD(cache_build_q8),
     ADAKV_METHOD(window_attn),
+    ADAKV_METHOD(cache_move),
 #undef ADAKV_METHOD
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -26,13 +26,22 @@ def arguments(name, dev):
     if name == "decode_step_q8":
         return layer, dict(step, cache=q8, **rest)
     K, V = f(tokens, H, D), f(tokens, H, D)
+    if name.startswith("cache_move"):
+        to = layer.pick([1, 1, 0])
+        more = dict(len_out=i(*[0] * 6), overflow=i(0))
+        front = dict(picks=[1, 1, 0], cu_seqlens=cu, headroom=HR)
+        if name == "cache_move_q8":
+            return layer, dict(front, cache=q8, seg_len=lens, headroom_out=9, cu_out=i(*[0] * 7), out=adakv.q8_cache(to, 9, dev), **more)
+        rows_out = adakv.cache_rows(to, 9)
+        return layer, dict(front, K_cache=f(rows, D), V_cache=f(rows, D), seg_len=lens, headroom_out=9, cu_out=i(*[0] * 7),
+                           K_out=f(rows_out, D), V_out=f(rows_out, D), **more)
     if name == "cache_build_q8":
         idx = torch.cat([torch.arange(n, dtype=torch.int32) for n in (20, 20, 24, 24)]).to(dev)
         return layer, dict(K=K, V=V, indices=idx, cu_seqlens=cu, headroom=HR, cache=q8, seg_len=lens)
     return layer, dict(q=f(tokens, H_Q, D), K=K, V=V, window=9, sinks=1, out=f(tokens, H_Q, D), row_lse=torch.zeros(2, H_Q, W, device=dev))
 
 
-NAMES = ("decode_step", "decode_step_q8", "cache_build_q8", "window_attn")
+NAMES = ("decode_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8")
 strided = lambda t: torch.stack([t, t], dim=-1)[..., 0]
 
 
@@ -52,9 +61,14 @@ def spoiled(a):
                 yield f"{k} with gaps", dict(a, **{k: strided(v)})
         elif k == "headroom":
             yield "headroom", dict(a, headroom=HR + 1)
+        elif k == "headroom_out":
+            yield "headroom_out", dict(a, headroom_out=10)
+        elif k == "picks":
+            yield "picks of no sequence", dict(a, picks=[1, 2, 0])
+            yield "no picks", dict(a, picks=[])
 
 
-def leaves(x):
+def leaves(x):                              # (a picked layer, its numbers)
     for t in x if isinstance(x, (tuple, list)) else [x]:
         yield from (leaves(t) if isinstance(t, (tuple, list)) else [t])
 
@@ -69,7 +83,7 @@ def test_host_tensors_are_left_to_python(name, lib, monkeypatch):
 
 
 def test_wrong_argument_counts(lib):
-    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn"):
+    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move"):
         with pytest.raises(TypeError, match="takes"):
             getattr(binding._marshal, name)(1, 2)
 
@@ -85,7 +99,7 @@ def test_both_checks_make_the_same_call(name, without, monkeypatch):
         calls = []
         if native:
             native_fn = binding._native
-            monkeypatch.setattr(binding, "_native", lambda *args: calls.append(native_fn(*args)) or calls[-1])
+            monkeypatch.setattr(binding, "_native", lambda *args, **kw: calls.append(native_fn(*args, **kw)) or calls[-1])
         else:
             monkeypatch.setattr(binding, "_marshal", None)
         out = getattr(adakv, name)(layer, **a)
