@@ -18,6 +18,9 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
@@ -46,6 +49,42 @@ constexpr int ROWS = 128;                      // query rows of a workgroup, 32 
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
+// 64 x 16 bytes from base + at + the lane's off, straight into 1 KB of LDS, behind the compiler's back: the tiles take
+// turns in LDS, and it would wait for every load before it reads any.  (In front of the load stand the wait states that
+// follow a write of m0, one, and a scalar register's write by the vector unit, five.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"        // m0 among the clobbers
+__device__ __forceinline__ void load_to_lds(const char *base, unsigned off, unsigned at, const u32x4 *dst) {
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+                   (unsigned)(size_t)(__attribute__((address_space(3))) const void *)dst),
+               "v"(off), "s"(rs), "s"(at)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// What this wavefront has asked for is in LDS, it has read what it read, and so has every other wavefront.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ const char *scalar_address(const char *p) {
+  const unsigned long long a = (unsigned long long)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  return (const char *)((unsigned long long)hi << 32 | lo);
+}
+
+// Tiles in LDS: KT rows of CH 16-byte words, of which the words of a row change places with the row so that the lanes of a
+// read fall on different banks.  Keys: 32 lanes read a word each of neighbouring rows.  Values, 16 bits: 32 lanes read 32
+// columns of four rows; 32 bits: 32 lanes read 32 columns of a row and the others those of the row four further on.
+template <typename T, int D> struct Tile {
+  static constexpr int ROWB = D * T::SIZE, CH = ROWB / 16;
+  static constexpr int KT = T::SIZE == 4 ? 32 : 64;
+  static constexpr int WORDS = KT * CH;
+  static constexpr int RPI = 64 / CH;                          // rows per load instruction
+  static constexpr int LOADS = WORDS / 256;                    // load instructions per wavefront and tensor
+  static __device__ __forceinline__ int swz_k(int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int swz_v(int row) {
+    return T::SIZE == 4 ? 8 * ((row >> 2) & 1) : CH == 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+  }
+};
+
 // One element of a row, in 32 bits.
 template <typename T> __device__ __forceinline__ float element(const char *row, int e) {
   if constexpr (is_f32<T>) return reinterpret_cast<const float *>(row)[e];
@@ -59,7 +98,8 @@ template <typename T> __device__ __forceinline__ unsigned short round16(float x)
 }
 // Two values rounded to the layer's 16-bit type, x0 in the lower half.
 template <typename T> __device__ __forceinline__ unsigned round2(float x0, float x1) {
-  return (unsigned)round16<T>(x0) | (unsigned)round16<T>(x1) << 16;
+  if constexpr (is_f16<T>) return __builtin_bit_cast(unsigned, __builtin_convertvector(floatx2{x0, x1}, f16x2));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(floatx2{x0, x1}, bf16x2));
 }
 
 // Row r of a sequence by one wavefront, key by key and without the matrix cores: for rows that came out infinite or as
@@ -107,11 +147,10 @@ template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
                                                              const char *__restrict__ K, const char *__restrict__ V,
                                                              char *__restrict__ out, float *__restrict__ row_lse) {
-  constexpr int ROWB = D * T::SIZE, CH = ROWB / 16;            // 16-byte words of a row
-  constexpr int KT = is_f32<T> ? 32 : 64, KB = KT / 32;        // keys of a tile
+  typedef Tile<T, D> TL;
+  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32;
   constexpr int CB = D / 32;                                   // column blocks of O^T
-  constexpr int LOADS = KT * CH / 256;                         // words per thread and tensor
-  __shared__ __align__(16) u32x4 shK[KT * CH], shV[KT * CH];
+  __shared__ __align__(16) u32x4 shK[2][TL::WORDS], shV[2][TL::WORDS];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -138,23 +177,40 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
   const int last = min(q0 + ROWS, n) - 1;                      // the workgroup's last row
   const int lo = max(0, q0 - sh.window + 1) / KT, hi = last / KT;
   const int firsts = min((int)(((long long)sh.sinks + KT - 1) / KT), lo), tiles = firsts + hi - lo + 1;
+  // the wavefront's share of a tile: rows on (wv * LOADS + i) * RPI + lane / CH
+  unsigned off_k[TL::LOADS], off_v[TL::LOADS];
+#pragma unroll
+  for (int i = 0; i < TL::LOADS; ++i) {
+    const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
+    off_k[i] = row * (unsigned)sh.k_tok + ((lane % CH) ^ TL::swz_k(row)) * 16;
+    off_v[i] = row * (unsigned)sh.v_tok + ((lane % CH) ^ TL::swz_v(row)) * 16;
+  }
+  auto first_key = [&](int t) { return (t < firsts ? t : lo + t - firsts) * KT; };
+  auto load = [&](int t) {
+    const int j0 = first_key(t);
+    const char *kb = scalar_address(Kh + j0 * sh.k_tok), *vb = scalar_address(Vh + j0 * sh.v_tok);
+    const u32x4 *dk = shK[t & 1] + wv * TL::LOADS * 64, *dv = shV[t & 1] + wv * TL::LOADS * 64;
+    if (j0 + KT <= n) {
+#pragma unroll
+      for (int i = 0; i < TL::LOADS; ++i) load_to_lds(kb, off_k[i], 0u, dk + i * 64);
+#pragma unroll
+      for (int i = 0; i < TL::LOADS; ++i) load_to_lds(vb, off_v[i], 0u, dv + i * 64);
+    } else {                                                   // rows past the sequence's end repeat its last one
+#pragma unroll
+      for (int i = 0; i < TL::LOADS; ++i) {
+        const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH, back = max(row - (n - 1 - j0), 0);
+        load_to_lds(kb, off_k[i] - back * (unsigned)sh.k_tok, 0u, dk + i * 64);
+        load_to_lds(vb, off_v[i] - back * (unsigned)sh.v_tok, 0u, dv + i * 64);
+      }
+    }
+  };
+
+  load(0);
   for (int t = 0; t < tiles; ++t) {
-    const int j0 = (t < firsts ? t : lo + t - firsts) * KT;
-    u32x4 kk[LOADS], vv[LOADS];
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int word = tid + 256 * u, row = min(j0 + word / CH, n - 1);
-      kk[u] = *reinterpret_cast<const u32x4 *>(Kh + row * sh.k_tok + (word % CH) * 16);
-      vv[u] = *reinterpret_cast<const u32x4 *>(Vh + row * sh.v_tok + (word % CH) * 16);
-    }
-    __syncthreads();                                           // the tile before is done with
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int word = tid + 256 * u, row = word / CH, ch = word % CH;
-      shK[row * CH + (ch ^ (row & (CH < 16 ? CH - 1 : 15)))] = kk[u];
-      shV[row * CH + (is_f32<T> ? ch : ch ^ (2 * (row & (CH / 2 - 1))))] = vv[u];
-    }
-    __syncthreads();
+    const int j0 = first_key(t);
+    const u32x4 *tk = shK[t & 1], *tv = shV[t & 1];
+    meet();
+    if (t + 1 < tiles) load(t + 1);
     // a tile that none of the wavefront's rows sees
     if (j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window)) continue;
 
@@ -165,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
 #pragma unroll
       for (int s = 0; s < CH / 2; ++s) {
         const int row = 32 * kb + l32;
-        const u32x4 kw = shK[row * CH + ((2 * s + half) ^ (row & (CH < 16 ? CH - 1 : 15)))];
+        const u32x4 kw = tk[row * CH + ((2 * s + half) ^ TL::swz_k(row))];
         if constexpr (is_f32<T>) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -186,7 +242,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
-          if (j > r || (j <= r - sh.window && j >= sh.sinks)) sc[kb][i] = -INFINITY;
+          const bool hidden = (j > r) | ((j <= r - sh.window) & (j >= sh.sinks));
+          sc[kb][i] = hidden ? -INFINITY : sc[kb][i];
         }
     }
     float top = sc[0][0];
@@ -211,12 +268,13 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
       }
 
     if constexpr (is_f32<T>) {
-      const float *vt = reinterpret_cast<const float *>(shV);
+      const float *vt = reinterpret_cast<const float *>(tv);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          const float va = vt[(8 * (i / 4) + 4 * half + i % 4) * D + 32 * cb + l32];
+          const int row = 8 * (i / 4) + 4 * half + i % 4;
+          const float va = vt[row * D + ((8 * cb + l32 / 4) ^ TL::swz_v(row)) * 4 + l32 % 4];
           const float pa = sc[0][i];
           acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, pa, acc[cb], 0, 0, 0);
         }
@@ -238,8 +296,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
             for (int x = 0; x < 2; ++x) {
               // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
               const int row = 32 * kb + 16 * ks + 8 * x + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
-              const int at = (row * CH + (ch ^ (2 * (row & (CH / 2 - 1))))) * 16 + 8 * (sub % 2);
-              v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)shV + at));
+              const int at = (row * CH + (ch ^ TL::swz_v(row))) * 16 + 8 * (sub % 2);
+              v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const lds_char *)tv + at));
             }
             const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
             const u32x4 va = {a0.x, a0.y, a1.x, a1.y};
