@@ -320,6 +320,14 @@ def _stream(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
+def _zeros(shape, dtype, device, stream):
+    """Zeros that a call on `stream` writes over: cleared on that stream, not on the current one beside it."""
+    if stream is None:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.zeros(shape, dtype=dtype, device=device)
+
+
 def _workspace(layer, ws):
     if ws is None:
         ws = torch.empty(max(workspace_bytes(layer), 16), dtype=torch.uint8, device="cuda")
@@ -756,7 +764,7 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
     _check_kv(layer, V, "V", layer.v_strides, layer.strides_given[1])
     if out is None:
-        out = torch.zeros((q.shape[0], layer.h_q, layer.d), dtype=layer.torch_dtype, device=q.device)
+        out = _zeros((q.shape[0], layer.h_q, layer.d), layer.torch_dtype, q.device, stream)
     if row_lse is None and want_lse:
         row_lse = torch.empty((layer.batch, layer.h_q, layer.w), dtype=torch.float32, device=q.device)
     _need(out, rows * layer.h_q * layer.d, "out")
@@ -788,13 +796,13 @@ def q8_scales(layer: Layer, headroom: int) -> int:
     return int(load_library().adakv_q8_scales(ctypes.byref(layer.c), int(headroom)))
 
 
-def q8_cache(layer: Layer, headroom: int, device="cuda") -> Q8Cache:
-    """Memory for a cache in 8 bits: zeros."""
+def q8_cache(layer: Layer, headroom: int, device="cuda", stream=None) -> Q8Cache:
+    """Memory for a cache in 8 bits: zeros (cleared on `stream`, or on the current one)."""
     scales = q8_scales(layer, headroom)
     if scales == 0:
         raise ValueError("the layer or the head-room is not valid")
-    codes = [torch.zeros((cache_rows(layer, headroom), layer.d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
-    return Q8Cache(*codes, *(torch.zeros(scales, dtype=torch.float32, device=device) for _ in range(2)))
+    codes = [_zeros((cache_rows(layer, headroom), layer.d), torch.uint8, device, stream).view(torch.float8_e4m3fn) for _ in range(2)]
+    return Q8Cache(*codes, *(_zeros(scales, torch.float32, device, stream) for _ in range(2)))
 
 
 def _q8_ptrs(layer, headroom, cache):
@@ -822,7 +830,7 @@ def cache_build_q8(layer: Layer, K, V, indices, cu_seqlens, headroom, cache=None
                                      headroom, *cache, seg_len):
         return cache, seg_len
     if cache is None:
-        cache = q8_cache(layer, headroom, K.device)
+        cache = q8_cache(layer, headroom, K.device, stream)
     if seg_len is None:
         seg_len = torch.empty(layer._segments, dtype=torch.int32, device=K.device)
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
@@ -947,9 +955,9 @@ def cache_move(layer: Layer, picks, cu_seqlens, headroom, K_cache, V_cache, seg_
         return layer.pick(picks), cu_out, K_out, V_out, len_out
     rows = cache_rows(layer.pick(picks), headroom_out)
     if K_out is None:
-        K_out = torch.zeros((rows, layer.d), dtype=layer.torch_dtype, device=K_cache.device)
+        K_out = _zeros((rows, layer.d), layer.torch_dtype, K_cache.device, stream)
     if V_out is None:
-        V_out = torch.zeros((rows, layer.d), dtype=layer.torch_dtype, device=V_cache.device)
+        V_out = _zeros((rows, layer.d), layer.torch_dtype, V_cache.device, stream)
     to, cu_out, len_out = _move("adakv_cache_move", layer, picks, cu_seqlens, headroom, cache(K_cache, V_cache), seg_len, headroom_out,
                                 cu_out, cache(K_out, V_out), len_out, overflow, stream)
     return to, cu_out, K_out, V_out, len_out
@@ -962,7 +970,7 @@ def cache_move_q8(layer: Layer, picks, cu_seqlens, headroom, cache, seg_len, hea
                                    len_out, overflow, check="cache_move"):
         return layer.pick(picks), cu_out, out, len_out
     if out is None:
-        out = q8_cache(layer.pick(picks), headroom_out, cache.K.device)
+        out = q8_cache(layer.pick(picks), headroom_out, cache.K.device, stream)
     to, cu_out, len_out = _move("adakv_cache_move_q8", layer, picks, cu_seqlens, headroom, lambda lay, hr: _q8_ptrs(lay, hr, cache), seg_len,
                                 headroom_out, cu_out, lambda lay, hr: _q8_ptrs(lay, hr, out), len_out, overflow, stream)
     return to, cu_out, out, len_out

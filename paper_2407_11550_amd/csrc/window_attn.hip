@@ -47,7 +47,11 @@ struct Shape {
 
 constexpr int ROWS = 128;                      // query rows of a workgroup, 32 per wavefront
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The value of the lane 32 further on.
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
 
 // 64 x 16 bytes from base + at + the lane's off, straight into 1 KB of LDS, behind the compiler's back: the tiles take
 // turns in LDS, and it would wait for every load before it reads any.  (In front of the load stand the wait states that
