@@ -34,9 +34,11 @@ template <typename T> constexpr bool is_f16 = false;
 template <> constexpr bool is_f16<FP16> = true;
 template <typename T> constexpr bool is_f32 = T::SIZE == 4;
 
-// Weights are at most 2^(LAZY + BIAS): the reference they are taken against is moved only when a maximum is 2^LAZY above
-// it.  fp16 weights travel 2^7 times larger, so that the smallest of full precision is 2^-21 of the reference.
-constexpr float LAZY = 8.0f;
+// Weights are taken against a kept reference, which costs no search for a maximum: it is moved, to the maximum of all so far,
+// only where the sum of a lane's 16 weights of a tile is beyond MOST (which holds for the first tile, whose reference lies
+// below every number).  fp16 weights travel 2^7 times larger, so that the smallest of full precision is 2^-21 of the reference;
+// none is beyond the type's range.
+constexpr float MOST = 0x1p15f;
 template <typename T> constexpr float BIAS = is_f16<T> ? 7.0f : 0.0f;
 
 struct Shape {
@@ -147,11 +149,100 @@ __device__ void careful_row(const Shape &sh, const char *q, const char *K, const
   if (lse && lane == 0) *lse = (m + log2f(l)) * LN2;
 }
 
+// What a wavefront does with 32 keys, a query per lane (twice: the halves of the wavefront hold different keys, lane `half`
+// of a query those numbered 8 (i / 4) + 4 half + i % 4).
+template <typename T, int D> struct Step {
+  typedef Tile<T, D> TL;
+  static constexpr int CH = TL::CH, CB = D / 32;
+  static constexpr int PW = is_f32<T> ? 16 : 8;                // registers of a tile's weights
+  typedef unsigned Weights __attribute__((ext_vector_type(PW)));
+
+  static __device__ __forceinline__ floatx16 logits(const u32x4 *tk, const u32x4 (&qf)[CH / 2], int l32, int half) {
+    floatx16 sc = floatx16{0};
+#pragma unroll
+    for (int s = 0; s < CH / 2; ++s) {
+      const u32x4 kw = tk[l32 * CH + ((2 * s + half) ^ TL::swz_k(l32))];
+      if constexpr (is_f32<T>) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned ka = kw[e], qa = qf[s][e];
+          sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc, 0, 0, 0);
+        }
+      } else if constexpr (is_f16<T>) {
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kw), __builtin_bit_cast(f16x8, qf[s]), sc, 0, 0, 0);
+      } else {
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw), __builtin_bit_cast(bf16x8, qf[s]), sc, 0, 0, 0);
+      }
+    }
+    return sc;
+  }
+
+  // Weights against the reference m, and their sum.
+  static __device__ __forceinline__ Weights weights(const floatx16 &sc, float c_log2, float m, float &sum) {
+    float p[16];
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_log2, BIAS<T> - m));
+      sum += p[i];
+    }
+    Weights w;
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      if constexpr (is_f32<T>) w[i] = __builtin_bit_cast(unsigned, p[i]);
+      else w[i] = round2<T>(p[2 * i], p[2 * i + 1]);
+    }
+    return w;
+  }
+
+  static __device__ __forceinline__ void add_values(floatx16 (&acc)[CB], const u32x4 *tv, const Weights &w, int lane) {
+    const int l32 = lane & 31, half = lane >> 5;
+    if constexpr (is_f32<T>) {
+      const float *vt = reinterpret_cast<const float *>(tv);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const int row = 8 * (i / 4) + 4 * half + i % 4;
+          const float va = vt[row * D + ((8 * cb + l32 / 4) ^ TL::swz_v(row)) * 4 + l32 % 4];
+          const unsigned pa = w[i];
+          acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, __builtin_bit_cast(float, pa), acc[cb], 0, 0, 0);
+        }
+    } else {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      typedef __attribute__((address_space(3))) char lds_char;
+      const int sub = lane & 15, row4 = 4 * half + sub / 4, col16 = (lane >> 4) & 1;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const u32x4 pb = {w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3]};
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          s16x4 v2[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
+            const int row = 16 * ks + 8 * x + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
+            const int at = (row * CH + (ch ^ TL::swz_v(row))) * 16 + 8 * (sub % 2);
+            v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const lds_char *)tv + at));
+          }
+          const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
+          const u32x4 va = {a0.x, a0.y, a1.x, a1.y};
+          if constexpr (is_f16<T>)
+            acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, va), __builtin_bit_cast(f16x8, pb), acc[cb], 0, 0, 0);
+          else
+            acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), acc[cb], 0, 0, 0);
+        }
+      }
+    }
+  }
+};
+
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
                                                              const char *__restrict__ K, const char *__restrict__ V,
                                                              char *__restrict__ out, float *__restrict__ row_lse) {
   typedef Tile<T, D> TL;
+  typedef Step<T, D> S;
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32;
   constexpr int CB = D / 32;                                   // column blocks of O^T
   __shared__ __align__(16) u32x4 shK[2][TL::WORDS], shV[2][TL::WORDS];
@@ -218,29 +309,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
     // a tile that none of the wavefront's rows sees
     if (j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window)) continue;
 
+    const bool edge = j0 + KT - 1 > w0 || !(j0 > w0 + 31 - sh.window || j0 + KT - 1 < sh.sinks);
     floatx16 sc[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      sc[kb] = floatx16{0};
-#pragma unroll
-      for (int s = 0; s < CH / 2; ++s) {
-        const int row = 32 * kb + l32;
-        const u32x4 kw = tk[row * CH + ((2 * s + half) ^ TL::swz_k(row))];
-        if constexpr (is_f32<T>) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const unsigned ka = kw[e], qa = qf[s][e];
-            sc[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc[kb], 0, 0, 0);
-          }
-        } else if constexpr (is_f16<T>) {
-          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kw), __builtin_bit_cast(f16x8, qf[s]), sc[kb], 0, 0, 0);
-        } else {
-          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw), __builtin_bit_cast(bf16x8, qf[s]), sc[kb], 0, 0, 0);
-        }
-      }
-    }
-    const int j1 = j0 + KT - 1;
-    if (j1 > w0 || !(j0 > w0 + 31 - sh.window || j1 < sh.sinks)) {
+    for (int kb = 0; kb < KB; ++kb) sc[kb] = S::logits(tk + kb * 32 * CH, qf, l32, half);
+    if (edge) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -250,67 +323,23 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
           sc[kb][i] = hidden ? -INFINITY : sc[kb][i];
         }
     }
-    float top = sc[0][0];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb) {
+      float sum;
+      typename S::Weights w = S::weights(sc[kb], sh.c_log2, m, sum);
+      if (__builtin_expect(__any(!(sum <= MOST)), 0)) {        // too far above the reference (or no number): a new one
+        float top = sc[kb][0];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-    top = fmaxf(top, other_half(top)) * sh.c_log2;
-    if (__any(top > m + LAZY)) {
-      const float mn = fmaxf(m, top), corr = __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= corr;
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+        const float mn = fmaxf(m, fmaxf(top, other_half(top)) * sh.c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= corr;
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) acc[cb] *= corr;
-    }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], sh.c_log2, BIAS<T> - m));
-        l += sc[kb][i];
+        for (int cb = 0; cb < CB; ++cb) acc[cb] *= corr;
+        w = S::weights(sc[kb], sh.c_log2, m, sum);
       }
-
-    if constexpr (is_f32<T>) {
-      const float *vt = reinterpret_cast<const float *>(tv);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          const int row = 8 * (i / 4) + 4 * half + i % 4;
-          const float va = vt[row * D + ((8 * cb + l32 / 4) ^ TL::swz_v(row)) * 4 + l32 % 4];
-          const float pa = sc[0][i];
-          acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, pa, acc[cb], 0, 0, 0);
-        }
-    } else {
-      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-      typedef __attribute__((address_space(3))) char lds_char;
-      const int sub = lane & 15, row4 = 4 * half + sub / 4, col16 = (lane >> 4) & 1;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          u32x4 pb;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) pb[i] = round2<T>(sc[kb][8 * ks + 2 * i], sc[kb][8 * ks + 2 * i + 1]);
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb) {
-            s16x4 v2[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
-              const int row = 32 * kb + 16 * ks + 8 * x + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
-              const int at = (row * CH + (ch ^ TL::swz_v(row))) * 16 + 8 * (sub % 2);
-              v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const lds_char *)tv + at));
-            }
-            const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
-            const u32x4 va = {a0.x, a0.y, a1.x, a1.y};
-            if constexpr (is_f16<T>)
-              acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, va), __builtin_bit_cast(f16x8, pb), acc[cb], 0, 0, 0);
-            else
-              acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), acc[cb], 0, 0, 0);
-          }
-        }
+      l += sum;
+      S::add_values(acc, tv + kb * 32 * CH, w, lane);
     }
   }
 
