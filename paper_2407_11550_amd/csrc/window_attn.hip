@@ -47,8 +47,6 @@ struct Shape {
   long long q_tok, q_head, k_tok, k_head, v_tok, v_head;     // bytes
 };
 
-constexpr int ROWS = 128;                      // query rows of a workgroup, 32 per wavefront
-
 // The value of the lane 32 further on.
 __device__ __forceinline__ float other_half(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -79,9 +77,9 @@ __device__ __forceinline__ const char *scalar_address(const char *p) {
 // Tiles in LDS: KT rows of CH 16-byte words, of which the words of a row change places with the row so that the lanes of a
 // read fall on different banks.  Keys: 32 lanes read a word each of neighbouring rows.  Values, 16 bits: 32 lanes read 32
 // columns of four rows; 32 bits: 32 lanes read 32 columns of a row and the others those of the row four further on.
-template <typename T, int D> struct Tile {
+template <typename T, int D, int KS> struct Tile {
   static constexpr int ROWB = D * T::SIZE, CH = ROWB / 16;
-  static constexpr int KT = T::SIZE == 4 ? 32 : 64;
+  static constexpr int KT = KS > 1 ? 32 * KS : T::SIZE == 4 ? 32 : 64;
   static constexpr int WORDS = KT * CH;
   static constexpr int RPI = 64 / CH;                          // rows per load instruction
   static constexpr int LOADS = WORDS / 256;                    // load instructions per wavefront and tensor
@@ -151,8 +149,8 @@ __device__ void careful_row(const Shape &sh, const char *q, const char *K, const
 
 // What a wavefront does with 32 keys, a query per lane (twice: the halves of the wavefront hold different keys, lane `half`
 // of a query those numbered 8 (i / 4) + 4 half + i % 4).
-template <typename T, int D> struct Step {
-  typedef Tile<T, D> TL;
+template <typename T, int D, int KS> struct Step {
+  typedef Tile<T, D, KS> TL;
   static constexpr int CH = TL::CH, CB = D / 32;
   static constexpr int PW = is_f32<T> ? 16 : 8;                // registers of a tile's weights
   typedef unsigned Weights __attribute__((ext_vector_type(PW)));
@@ -179,13 +177,13 @@ template <typename T, int D> struct Step {
 
   // Weights against the reference m, and their sum.
   static __device__ __forceinline__ Weights weights(const floatx16 &sc, float c_log2, float m, float &sum) {
-    float p[16];
-    sum = 0.0f;
+    float p[16], part[4];                      // (four sums: one after the other would be a chain of 16 additions)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_log2, BIAS<T> - m));
-      sum += p[i];
+      part[i % 4] = i < 4 ? p[i] : part[i % 4] + p[i];
     }
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
     Weights w;
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
@@ -237,13 +235,16 @@ template <typename T, int D> struct Step {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
+// KS wavefronts share 32 rows and take 32 keys of a tile each: 1, four times 32 rows in a workgroup; 2 or 4, a half or a quarter of
+// the rows and as much of the way, and the sums meet at the end.
+template <typename T, int D, int KS>
+__global__ __launch_bounds__(256, KS > 1 && D == 128 && (KS == 4 || T::SIZE == 4) ? 1 : 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
                                                              const char *__restrict__ K, const char *__restrict__ V,
                                                              char *__restrict__ out, float *__restrict__ row_lse) {
-  typedef Tile<T, D> TL;
-  typedef Step<T, D> S;
-  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32;
+  typedef Tile<T, D, KS> TL;
+  typedef Step<T, D, KS> S;
+  constexpr int ROWS = 128 / KS;                               // query rows of the workgroup
+  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32 / KS;
   constexpr int CB = D / 32;                                   // column blocks of O^T
   __shared__ __align__(16) u32x4 shK[2][TL::WORDS], shV[2][TL::WORDS];
 
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
   const int q0 = (ct.off[b + 1] - 1 - rank) * ROWS;            // the longest rows first
   const char *Kh = K + st.tok_off[b] * sh.k_tok + c * sh.k_head, *Vh = V + st.tok_off[b] * sh.v_tok + c * sh.v_head;
   const char *Qh = q + st.tok_off[b] * sh.q_tok + hq * sh.q_head;
-  const int w0 = q0 + 32 * wv, r = min(w0 + l32, n - 1);       // the wavefront's first row, this lane's
+  const int w0 = q0 + 32 * (wv / KS), r = min(w0 + l32, n - 1);       // the wavefront's first row, this lane's
 
   u32x4 qf[CH / 2];
 #pragma unroll
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
   auto load = [&](int t) {
     const int j0 = first_key(t);
     const char *kb = scalar_address(Kh + j0 * sh.k_tok), *vb = scalar_address(Vh + j0 * sh.v_tok);
-    const u32x4 *dk = shK[t & 1] + wv * TL::LOADS * 64, *dv = shV[t & 1] + wv * TL::LOADS * 64;
+    const u32x4 *dk = shK[t % 2] + wv * TL::LOADS * 64, *dv = shV[t % 2] + wv * TL::LOADS * 64;
     if (j0 + KT <= n) {
 #pragma unroll
       for (int i = 0; i < TL::LOADS; ++i) load_to_lds(kb, off_k[i], 0u, dk + i * 64);
@@ -303,22 +304,23 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
   load(0);
   for (int t = 0; t < tiles; ++t) {
     const int j0 = first_key(t);
-    const u32x4 *tk = shK[t & 1], *tv = shV[t & 1];
+    const u32x4 *tk = shK[t % 2], *tv = shV[t % 2];
     meet();
     if (t + 1 < tiles) load(t + 1);
     // a tile that none of the wavefront's rows sees
     if (j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window)) continue;
 
+    const int kb0 = wv % KS;                                    // this wavefront's keys of the tile
     const bool edge = j0 + KT - 1 > w0 || !(j0 > w0 + 31 - sh.window || j0 + KT - 1 < sh.sinks);
     floatx16 sc[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) sc[kb] = S::logits(tk + kb * 32 * CH, qf, l32, half);
+    for (int kb = 0; kb < KB; ++kb) sc[kb] = S::logits(tk + (kb0 + kb) * 32 * CH, qf, l32, half);
     if (edge) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
+          const int j = j0 + 32 * (kb0 + kb) + 8 * (i / 4) + 4 * half + i % 4;
           const bool hidden = (j > r) | ((j <= r - sh.window) & (j >= sh.sinks));
           sc[kb][i] = hidden ? -INFINITY : sc[kb][i];
         }
@@ -339,12 +341,41 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(SeqTab st, ChunkTab
         w = S::weights(sc[kb], sh.c_log2, m, sum);
       }
       l += sum;
-      S::add_values(acc, tv + kb * 32 * CH, w, lane);
+      S::add_values(acc, tv + (kb0 + kb) * 32 * CH, w, lane);
     }
   }
 
-  if (w0 >= n) return;
   l += other_half(l);
+  if constexpr (KS > 1) {
+    // the first of those that share their rows takes the others' sums, through the tiles' place
+    typedef float Sums[CB * 16][64];
+    static_assert((4 - 4 / KS) * sizeof(Sums) <= sizeof(shK), "the sums have room");
+    Sums *sums = reinterpret_cast<Sums *>(&shK[0][0]);
+    float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(&shV[0][0]);
+    const int place = wv / KS * (KS - 1) - 1;                  // + 1 .. KS - 1
+    meet();
+    if (wv % KS) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[place + wv % KS][cb * 16 + i][lane] = acc[cb][i];
+      ml[place + wv % KS][lane] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (wv % KS) return;
+#pragma unroll
+    for (int k = 1; k < KS; ++k) {
+      const float2 other = ml[place + k][lane];
+      const float mn = fmaxf(m, other.x), f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(other.x - mn);
+      m = mn;
+      l = l * f0 + other.y * f1;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[cb][i] = acc[cb][i] * f0 + sums[place + k][cb * 16 + i][lane] * f1;
+    }
+  }
+  if (w0 >= n) return;
   float *lse = row_lse ? row_lse + ((long long)b * sh.h_q + hq) * sh.w - st.n[b] : nullptr;     // of row 0
   char *oh = out + (st.tok_off[b] * sh.h_q + hq) * ROWB;
   const long long o_tok = (long long)sh.h_q * ROWB;
@@ -382,18 +413,43 @@ hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const
   const long long e = dtype == ADAKV_FP32 ? 4 : 2;
   const Shape sh = {dm.h_q, dm.h_kv, dm.g, dm.w, window, sinks, dm.scale * LOG2E, q_tok * e, q_head * e, dm.k_stride_tok * e,
                     dm.k_stride_head * e, dm.v_stride_tok * e, dm.v_stride_head * e};
-  ChunkTab ct;
-  ct.off[0] = 0;
-  for (int b = 0; b < st.batch; ++b) ct.off[b + 1] = ct.off[b] + (st.n[b] + dm.w + ROWS - 1) / ROWS;
-  for (int b = st.batch + 1; b <= ADAKV_MAX_BATCH; ++b) ct.off[b] = ct.off[st.batch];
+  const auto chunks = [&](int rows) {
+    ChunkTab ct;
+    ct.off[0] = 0;
+    for (int b = 0; b < st.batch; ++b) ct.off[b + 1] = ct.off[b] + (st.n[b] + dm.w + rows - 1) / rows;
+    for (int b = st.batch + 1; b <= ADAKV_MAX_BATCH; ++b) ct.off[b] = ct.off[st.batch];
+    return ct;
+  };
+  // A wavefront takes 0.9 us for 32 keys whatever else there is to do, so with few workgroups (two fit on each of 256 compute
+  // units) wavefronts share rows.  us, 128 | 64 | 32 rows a workgroup, by the number that 128 rows make; all keys visible, d = 128
+  // but for the last two: 64 workgroups, 256 keys 10.6 | 9.7 | 8.8; 128, 2048 keys 43.5 | 31.0 | 28.9; 160, 541 keys
+  // 17.1 | 14.7 | 22.0; 256, 1024 keys 27.3 | 22.8 | 40.0; 384, 1536 keys 40.8 | 35.9; 512, 2043 keys 54.9 | 53.2; 512, 8192 keys
+  // 191 | 173; 1024, 4096 keys 159 | 182; d = 64: 128, 2048 keys 30.6 | 22.7 | 16.4; 256, 1024 keys 18.4 | 15.2 | 17.2.  Where a
+  // window makes all rows' ways equally short there is no longest one to shorten: 300 keys, 256 workgroups 19.1 | 18.4, 384
+  // 24.7 | 28.1, 512 26.8 | 33.3.  Nothing is there to share in 64 keys: 6.6 | 7.3.
+  ChunkTab ct = chunks(128);
+  const long long wgs = (long long)ct.off[st.batch] * dm.h_q;
+  long long reach = 0;                         // keys that the last rows see
+  for (int b = 0; b < st.batch; ++b) reach = st.n[b] + dm.w > reach ? st.n[b] + dm.w : reach;
+  if ((long long)window + sinks < reach) reach = (long long)window + sinks;
+  const bool room_for_four = !(dtype == ADAKV_FP32 && dm.d == 128);      // (tiles of 128 keys, twice, in a compute unit's LDS)
+  const int share = reach <= 128 ? 1 : wgs <= 128 && room_for_four ? 4 : wgs <= 256 || (wgs <= 512 && reach >= 1024) ? 2 : 1;
+  if (share > 1) ct = chunks(128 / share);
   const dim3 grid((unsigned)((long long)ct.off[st.batch] * dm.h_q));
-#define ADAKV_WINDOW(T, D)                                                                                              \
-  ADAKV_LAUNCH("window_attn", (window_attn_kernel<T, D>), grid, dim3(256), s, st, ct, sh, (const char *)q, (const char *)K, \
+#define ADAKV_WINDOW_KS(T, D, KS)                                                                                           \
+  ADAKV_LAUNCH("window_attn", (window_attn_kernel<T, D, KS>), grid, dim3(256), s, st, ct, sh, (const char *)q, (const char *)K, \
                (const char *)V, (char *)out, row_lse)
+#define ADAKV_WINDOW(T, D)                                                                                                  \
+  do {                                                                                                                      \
+    if constexpr (T::SIZE == 2 || D == 64)                                                                                  \
+      if (share == 4) { ADAKV_WINDOW_KS(T, D, 4); break; }                                                                  \
+    if (share == 2) ADAKV_WINDOW_KS(T, D, 2); else ADAKV_WINDOW_KS(T, D, 1);                                                \
+  } while (0)
   if (dtype == ADAKV_BF16) { if (dm.d == 64) ADAKV_WINDOW(BF16, 64); else ADAKV_WINDOW(BF16, 128); }
   else if (dtype == ADAKV_FP16) { if (dm.d == 64) ADAKV_WINDOW(FP16, 64); else ADAKV_WINDOW(FP16, 128); }
   else { if (dm.d == 64) ADAKV_WINDOW(FP32, 64); else ADAKV_WINDOW(FP32, 128); }
 #undef ADAKV_WINDOW
+#undef ADAKV_WINDOW_KS
   return hipGetLastError();
 }
 

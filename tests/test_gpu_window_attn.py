@@ -54,6 +54,17 @@ CASES = [
     (FS, 4, 1, 128, [161], 16, 1, 33),
     (BF, 5, 5, 128, [200], 7, 1, 0),             # a row sees itself alone
     (BF, 2, 1, 128, [1500], 32, 65, 5),          # far rows: tiles between sinks and window are not visited
+    # rows shared by one, two and four wavefronts, in every type and width (which of them goes by the number of workgroups)
+    (BF, 64, 64, 128, [330, 33], 32, 200, 3),    # 256 workgroups of 128 rows
+    (FH, 64, 64, 64, [330, 33], 32, 200, 3),
+    (BF, 64, 64, 64, [300, 160], 7, 129, 0),     # 320
+    (FH, 64, 64, 128, [300, 160], 7, 129, 0),
+    (FS, 64, 64, 64, [140, 260], 3, 129, 0),
+    (FS, 64, 64, 128, [140, 260], 3, 131, 33),
+    (FS, 32, 32, 128, [161], 3, 131, 33),
+    (BF, 64, 32, 128, [150], 3, 150, 0),         # 128
+    (BF, 64, 32, 64, [150], 3, 150, 0),
+    (FH, 60, 30, 128, [129, 5], 3, 2 ** 31 - 1, 0),
 ]
 
 
@@ -65,7 +76,7 @@ def test_prompts_against_64_bits(case):
     q, K, V = inputs(dtype, h_q, h, d, sum(lens))
     out, lse = adakv.window_attn(layer, q, K, V, window, sinks, want_lse=True)
     torch.cuda.synchronize()
-    check(layer, q, K, V, window, sinks, out, lse)
+    check(layer, q, K, V, window, sinks, out, lse, heads=None if h_q < 16 else (0, 1, h_q // 2, h_q - 1))
 
 
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 64), (FS, 64)])
@@ -94,13 +105,15 @@ def test_strided_tensors_loose_sequences_and_a_scale(dtype, d):
 
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 128), (FS, 64)])
 @pytest.mark.parametrize("what", [float("inf"), float("-inf"), float("nan")])
-def test_hidden_keys_and_values_have_no_part(dtype, d, what):
+@pytest.mark.parametrize("window", [40, 130])
+@pytest.mark.parametrize("h_q", [2, 70])
+def test_hidden_keys_and_values_have_no_part(dtype, d, what, window, h_q):
     """Rows before a broken key or value, and rows whose window has left it behind, come out as if it were not there; the
     rows that see a broken value are not finite."""
-    print(dtype, d, what, flush=True)
-    n, w, window, sinks, at = 210, 4, 40, 2, 101
-    layer = layer_of(dtype, 2, 1, d, [n], w)
-    q, K, V = inputs(dtype, 2, 1, d, n)
+    print(dtype, d, what, window, h_q, flush=True)
+    n, w, sinks, at = 260, 4, 2, 101
+    layer = layer_of(dtype, h_q, 1, d, [n], w)
+    q, K, V = inputs(dtype, h_q, 1, d, n)
     clean = adakv.window_attn(layer, q, K, V, window, sinks)
     Vb, Kb = V.clone(), K.clone()
     Vb[at] = what
