@@ -319,9 +319,10 @@ int adakv_decode_step(const adakv_layer *L, const void *q_new, const void *k_new
  *   q        (device) rows as K's; element (row, i, e) at row*q_stride_tok + i*q_stride_head + e, both
  *                     strides >= d and rows 16-byte aligned
  *   K, V     (device) strided as in the layer, rows 16-byte aligned
- *   out      (device) [rows][h_q][d] contiguous, L->dtype, 16-byte aligned; rows of no sequence stay as they are
+ *   out      (device) [rows][h_q][d] contiguous, L->dtype, 16-byte aligned, no part of q, K or V; rows of no
+ *                     sequence stay as they are
  *   row_lse  (device) [batch][h_q][w] fp32, written; may be NULL
- * Supported (else ADAKV_EUNSUPPORTED): up to 2^28 rows a sequence; rows of K and of V less than 32 MiB apart; at most 2^32 rows times query heads in
+ * Supported (else ADAKV_EUNSUPPORTED): up to 2^28 rows a sequence; rows of K and of V less than 16 MiB apart; at most 2^32 rows times query heads in
  * all, each sequence's rows counted in 64s.
  */
 int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,

@@ -406,7 +406,8 @@ int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
   const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
   if (q_stride_tok * esz % 16 != 0 || q_stride_head * esz % 16 != 0) return ADAKV_EUNSUPPORTED;
   if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return ADAKV_EUNSUPPORTED;
-  if (L->k_stride_tok >= (1 << 25) / esz || L->v_stride_tok >= (1 << 25) / esz) return ADAKV_EUNSUPPORTED;   // (32-bit offsets in a tile)
+  // (a tile has up to 128 rows, whose offsets are below 2^31)
+  if (L->k_stride_tok >= (1 << 24) / esz || L->v_stride_tok >= (1 << 24) / esz) return ADAKV_EUNSUPPORTED;
   long long blocks = 0;
   for (int b = 0; b < st.batch; ++b) {
     const long long rows = (long long)st.n[b] + dm.w;

@@ -33,7 +33,7 @@ def test_window_attn_refusals(lib):
     for bad in (dict(window=0), dict(window=-3), dict(sinks=-1), dict(tok=127), dict(head=64), dict(q=None), dict(K=None), dict(V=None),
                 dict(out=None), dict(L=layer(w=0)), dict(L=layer(h_q=30))):
         assert call(**bad) == -1, bad
-    for bad in (dict(q=ODD), dict(K=ODD), dict(V=ODD), dict(out=ODD), dict(tok=4100), dict(head=132), dict(L=layer(d=96)), dict(L=layer(k_strides=(1 << 24, 128))), dict(L=layer(v_strides=(1 << 24, 128))),
+    for bad in (dict(q=ODD), dict(K=ODD), dict(V=ODD), dict(out=ODD), dict(tok=4100), dict(head=132), dict(L=layer(d=96)), dict(L=layer(k_strides=(1 << 23, 128))), dict(L=layer(v_strides=(1 << 23, 128))),
                 dict(L=layer(n=[(1 << 28) - 31], h_q=1, h_kv=1, B=[64])), dict(L=layer(n=[(1 << 27)] * 2, h_q=32, h_kv=1, B=[64] * 2))):
         assert call(**bad) == -2, bad
 
