@@ -10,6 +10,8 @@
 // Bound by the matrix instructions: 4 d flops per visible pair.
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace adakv {
@@ -33,6 +35,18 @@ struct FP32 { static constexpr int SIZE = 4; };
 template <typename T> constexpr bool is_f16 = false;
 template <> constexpr bool is_f16<FP16> = true;
 template <typename T> constexpr bool is_f32 = T::SIZE == 4;
+
+template <typename T> __device__ __forceinline__ float half_of(unsigned u) {
+  if constexpr (is_f16<T>) return (float)__builtin_bit_cast(_Float16, (unsigned short)u);
+  else return __builtin_bit_cast(float, u << 16);
+}
+template <typename T> constexpr unsigned EXPONENT = is_f16<T> ? 0x7c00u : 0x7f80u;     // all ones: infinite or NaN
+template <typename T> __device__ __forceinline__ floatx16 product(const u32x4 &a, const u32x4 &b, const floatx16 &c) {
+  if constexpr (is_f16<T>)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
 
 // Weights are taken against a kept reference, which costs no search for a maximum: it is moved, to the maximum of all so far,
 // only where the sum of a lane's 16 weights of a tile is beyond MOST (which holds for the first tile, whose reference lies
@@ -89,62 +103,10 @@ template <typename T, int D, int KS> struct Tile {
   }
 };
 
-// One element of a row, in 32 bits.
-template <typename T> __device__ __forceinline__ float element(const char *row, int e) {
-  if constexpr (is_f32<T>) return reinterpret_cast<const float *>(row)[e];
-  const unsigned short u = reinterpret_cast<const unsigned short *>(row)[e];
-  if constexpr (is_f16<T>) return (float)__builtin_bit_cast(_Float16, u);
-  return __builtin_bit_cast(float, (unsigned)u << 16);
-}
-template <typename T> __device__ __forceinline__ unsigned short round16(float x) {
-  if constexpr (is_f16<T>) return __builtin_bit_cast(unsigned short, (_Float16)x);
-  return __builtin_bit_cast(unsigned short, (__bf16)x);
-}
 // Two values rounded to the layer's 16-bit type, x0 in the lower half.
 template <typename T> __device__ __forceinline__ unsigned round2(float x0, float x1) {
   if constexpr (is_f16<T>) return __builtin_bit_cast(unsigned, __builtin_convertvector(floatx2{x0, x1}, f16x2));
   return __builtin_bit_cast(unsigned, __builtin_convertvector(floatx2{x0, x1}, bf16x2));
-}
-
-// Row r of a sequence by one wavefront, key by key and without the matrix cores: for rows that came out infinite or as
-// NaN.  A product over a tile multiplies hidden values by a weight of 0, which is no 0 for those; here hidden
-// keys have no part at all.
-template <typename T, int D>
-__device__ void careful_row(const Shape &sh, const char *q, const char *K, const char *V, int r, char *out, float *lse) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int lo = max(0, r - sh.window + 1), firsts = min(sh.sinks, lo), count = firsts + r - lo + 1;
-  float m = M_INIT, l = 0.0f, acc[E] = {};
-  for (int t0 = 0; t0 < count; t0 += 64) {
-    const int t = t0 + lane;
-    const bool on = t < count;
-    const int tt = min(t, count - 1), j = tt < firsts ? tt : lo + tt - firsts;
-    float s = 0.0f;
-    for (int e = 0; e < D; ++e) s = fmaf(element<T>(q, e), element<T>(K + j * sh.k_tok, e), s);
-    s = on ? s * sh.c_log2 : -INFINITY;
-    float top = s;
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float mn = fmaxf(m, top), corr = exp2f(m - mn), p = on ? exp2f(s - mn) : 0.0f;
-    m = mn;
-    float sum = p;
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    l = l * corr + sum;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] *= corr;
-    for (int u = 0; u < min(64, count - t0); ++u) {
-      const float pu = __shfl(p, u);
-      const int ju = __builtin_amdgcn_readfirstlane(__shfl(j, u));
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(pu, element<T>(V + ju * sh.v_tok, lane * E + e), acc[e]);
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float x = acc[e] / l;
-    if constexpr (is_f32<T>) reinterpret_cast<float *>(out)[lane * E + e] = x;
-    else reinterpret_cast<unsigned short *>(out)[lane * E + e] = round16<T>(x);
-  }
-  if (lse && lane == 0) *lse = (m + log2f(l)) * LN2;
 }
 
 // What a wavefront does with 32 keys, a query per lane (twice: the halves of the wavefront hold different keys, lane `half`
@@ -154,6 +116,7 @@ template <typename T, int D, int KS> struct Step {
   static constexpr int CH = TL::CH, CB = D / 32;
   static constexpr int PW = is_f32<T> ? 16 : 8;                // registers of a tile's weights
   typedef unsigned Weights __attribute__((ext_vector_type(PW)));
+  typedef floatx16 Sums[CB];
 
   static __device__ __forceinline__ floatx16 logits(const u32x4 *tk, const u32x4 (&qf)[CH / 2], int l32, int half) {
     floatx16 sc = floatx16{0};
@@ -166,10 +129,8 @@ template <typename T, int D, int KS> struct Step {
           const unsigned ka = kw[e], qa = qf[s][e];
           sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc, 0, 0, 0);
         }
-      } else if constexpr (is_f16<T>) {
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kw), __builtin_bit_cast(f16x8, qf[s]), sc, 0, 0, 0);
       } else {
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw), __builtin_bit_cast(bf16x8, qf[s]), sc, 0, 0, 0);
+        sc = product<T>(kw, qf[s], sc);
       }
     }
     return sc;
@@ -193,43 +154,78 @@ template <typename T, int D, int KS> struct Step {
     return w;
   }
 
-  static __device__ __forceinline__ void add_values(floatx16 (&acc)[CB], const u32x4 *tv, const Weights &w, int lane) {
+  // A weight as the matrix units get it.
+  static __device__ __forceinline__ float weight(const Weights &w, int i) {
+    if constexpr (is_f32<T>) return __builtin_bit_cast(float, (unsigned)w[i]);
+    else return half_of<T>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu);
+  }
+
+  // o += the products of 32 keys' weights and the values of columns 32 cb on.  FINITE: infinities and NaN count as 0.
+  template <bool FINITE> static __device__ __forceinline__ void add_block(floatx16 &o, const u32x4 *tv, const Weights &w, int lane, int ks, int cb) {
     const int l32 = lane & 31, half = lane >> 5;
     if constexpr (is_f32<T>) {
       const float *vt = reinterpret_cast<const float *>(tv);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          const int row = 8 * (i / 4) + 4 * half + i % 4;
-          const float va = vt[row * D + ((8 * cb + l32 / 4) ^ TL::swz_v(row)) * 4 + l32 % 4];
-          const unsigned pa = w[i];
-          acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, __builtin_bit_cast(float, pa), acc[cb], 0, 0, 0);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int row = 8 * (2 * ks + i / 4) + 4 * half + i % 4;
+        float va = vt[row * D + ((8 * cb + l32 / 4) ^ TL::swz_v(row)) * 4 + l32 % 4];
+        if (FINITE) va = __builtin_fabsf(va) < INFINITY ? va : 0.0f;
+        const unsigned pa = w[8 * ks + i];
+        o = __builtin_amdgcn_mfma_f32_32x32x2f32(va, __builtin_bit_cast(float, pa), o, 0, 0, 0);
+      }
     } else {
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
       typedef __attribute__((address_space(3))) char lds_char;
       const int sub = lane & 15, row4 = 4 * half + sub / 4, col16 = (lane >> 4) & 1;
+      s16x4 v2[2];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const u32x4 pb = {w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3]};
+      for (int y = 0; y < 2; ++y) {
+        // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
+        const int row = 16 * ks + 8 * y + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
+        const int at = (row * CH + (ch ^ TL::swz_v(row))) * 16 + 8 * (sub % 2);
+        v2[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const lds_char *)tv + at));
+      }
+      const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
+      u32x4 va = {a0.x, a0.y, a1.x, a1.y};
+      if constexpr (FINITE) {
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          s16x4 v2[2];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            // 4 rows x 16 columns by 16 lanes: a lane gets a column of them
-            const int row = 16 * ks + 8 * x + row4, ch = 4 * cb + 2 * col16 + (sub % 4) / 2;
-            const int at = (row * CH + (ch ^ TL::swz_v(row))) * 16 + 8 * (sub % 2);
-            v2[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const lds_char *)tv + at));
-          }
-          const uint2 a0 = __builtin_bit_cast(uint2, v2[0]), a1 = __builtin_bit_cast(uint2, v2[1]);
-          const u32x4 va = {a0.x, a0.y, a1.x, a1.y};
-          if constexpr (is_f16<T>)
-            acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, va), __builtin_bit_cast(f16x8, pb), acc[cb], 0, 0, 0);
-          else
-            acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), acc[cb], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          const unsigned u = va[i], top = EXPONENT<T>;
+          va[i] = ((u & top) == top ? 0u : u & 0xffffu) | ((u >> 16 & top) == top ? 0u : u & 0xffff0000u);
         }
+      }
+      o = product<T>(va, u32x4{w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3]}, o);
+    }
+  }
+  static __device__ __forceinline__ void add_values(floatx16 (&acc)[CB], const u32x4 *tv, const Weights &w, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) add_block<false>(acc[cb], tv, w, lane, ks, cb);
+  }
+
+  // The infinities and NaN that add_block<true> left out, for the rows that see them.
+  template <typename Sees> static __device__ __forceinline__ void add_seen(floatx16 &o, const u32x4 *tv, const Weights &w, int lane, int cb, Sees &&sees) {
+#pragma nounroll
+    for (int row = 0; row < 32; ++row) {
+      asm volatile("" : "+v"(lane));                           // (addresses are made here, not kept in registers for this rare loop)
+      const int l32 = lane & 31, half = lane >> 5;
+      const int reg = 4 * (row / 8) + row % 4, there = l32 + 32 * (row / 4 % 2);       // where the row's weights are
+      float p = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p = i == reg ? weight(w, i) : p;
+      p = __shfl(p, there);
+      const bool seen = sees(row);
+      const char *bytes = reinterpret_cast<const char *>(tv) + row * TL::ROWB;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int col = 32 * cb + 8 * (i / 4) + 4 * half + i % 4;
+        const char *at = bytes + (col * T::SIZE / 16 ^ TL::swz_v(row)) * 16 + col * T::SIZE % 16;
+        float v;
+        if constexpr (is_f32<T>) v = *reinterpret_cast<const float *>(at);
+        else v = half_of<T>(*reinterpret_cast<const unsigned short *>(at));
+        o[i] += seen && !(__builtin_fabsf(v) < INFINITY) ? p * v : 0.0f;
+        __builtin_amdgcn_sched_barrier(0);                     // (one at a time: this is rare)
       }
     }
   }
@@ -238,15 +234,16 @@ template <typename T, int D, int KS> struct Step {
 // KS wavefronts share 32 rows and take 32 keys of a tile each: 1, four times 32 rows in a workgroup; 2 or 4, a half or a quarter of
 // the rows and as much of the way, and the sums meet at the end.
 template <typename T, int D, int KS>
-__global__ __launch_bounds__(256, KS > 1 && D == 128 && (KS == 4 || T::SIZE == 4) ? 1 : 2) void window_attn_kernel(SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q,
-                                                             const char *__restrict__ K, const char *__restrict__ V,
-                                                             char *__restrict__ out, float *__restrict__ row_lse) {
+__global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 4) ? 1 : 2) : KS == 4 ? 2 : T::SIZE == 4 ? 3 : 4) void window_attn_kernel(
+    SeqTab st, ChunkTab ct, Shape sh, const char *__restrict__ q, const char *__restrict__ K, const char *__restrict__ V,
+    char *__restrict__ out, float *__restrict__ row_lse) {
   typedef Tile<T, D, KS> TL;
   typedef Step<T, D, KS> S;
-  constexpr int ROWS = 128 / KS;                               // query rows of the workgroup
+  constexpr int ROWS = 128 / KS;                          // query rows of the workgroup
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32 / KS;
   constexpr int CB = D / 32;                                   // column blocks of O^T
   __shared__ __align__(16) u32x4 shK[2][TL::WORDS], shV[2][TL::WORDS];
+  __shared__ int sh_bad[4];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -259,16 +256,11 @@ __global__ __launch_bounds__(256, KS > 1 && D == 128 && (KS == 4 || T::SIZE == 4
   const int q0 = (ct.off[b + 1] - 1 - rank) * ROWS;            // the longest rows first
   const char *Kh = K + st.tok_off[b] * sh.k_tok + c * sh.k_head, *Vh = V + st.tok_off[b] * sh.v_tok + c * sh.v_head;
   const char *Qh = q + st.tok_off[b] * sh.q_tok + hq * sh.q_head;
-  const int w0 = q0 + 32 * (wv / KS), r = min(w0 + l32, n - 1);       // the wavefront's first row, this lane's
+  const int w0 = q0 + 32 * (wv / KS), r = min(w0 + l32, n - 1);        // the wavefront's first row, this lane's
 
   u32x4 qf[CH / 2];
 #pragma unroll
   for (int s = 0; s < CH / 2; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + r * sh.q_tok + (2 * s + half) * 16);
-
-  floatx16 acc[CB];
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) acc[cb] = floatx16{0};
-  float m = M_INIT, l = 0.0f;
 
   const int last = min(q0 + ROWS, n) - 1;                      // the workgroup's last row
   const int lo = max(0, q0 - sh.window + 1) / KT, hi = last / KT;
@@ -301,56 +293,142 @@ __global__ __launch_bounds__(256, KS > 1 && D == 128 && (KS == 4 || T::SIZE == 4
     }
   };
 
+  floatx16 acc[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) acc[cb] = floatx16{0};
+  float m = M_INIT, l = 0.0f;
+  // Logits of 32 keys, hidden ones -inf where there are any, and their weights against the running reference; where that has to
+  // move, `move` multiplies what was summed against it.
+  auto hide = [&](floatx16 &sc, int first, int half) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j = first + 8 * (i / 4) + 4 * half + i % 4;
+      const bool hidden = (j > r) | ((j <= r - sh.window) & (j >= sh.sinks));
+      sc[i] = hidden ? -INFINITY : sc[i];
+    }
+  };
+  auto weigh = [&](const floatx16 &sc, auto &&move) {
+    float sum;
+    typename S::Weights w = S::weights(sc, sh.c_log2, m, sum);
+    if (__builtin_expect(__any(!(sum <= MOST)), 0)) {          // too far above the reference (or no number): a new one
+      float top = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+      const float mn = fmaxf(m, fmaxf(top, other_half(top)) * sh.c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= corr;
+      move(corr);
+      w = S::weights(sc, sh.c_log2, m, sum);
+    }
+    l += sum;
+    return w;
+  };
+  // whether none of the wavefront's rows sees a key of the tile, and whether some see only some
+  auto unseen = [&](int j0) { return j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window); };
+  auto edge = [&](int j0) { return j0 + KT - 1 > w0 || !(j0 > w0 + 31 - sh.window || j0 + KT - 1 < sh.sinks); };
+
   load(0);
   for (int t = 0; t < tiles; ++t) {
     const int j0 = first_key(t);
     const u32x4 *tk = shK[t % 2], *tv = shV[t % 2];
     meet();
     if (t + 1 < tiles) load(t + 1);
-    // a tile that none of the wavefront's rows sees
-    if (j0 > w0 + 31 || (j0 >= sh.sinks && j0 + KT - 1 <= w0 - sh.window)) continue;
-
-    const int kb0 = wv % KS;                                    // this wavefront's keys of the tile
-    const bool edge = j0 + KT - 1 > w0 || !(j0 > w0 + 31 - sh.window || j0 + KT - 1 < sh.sinks);
+    if (unseen(j0)) continue;
+    const int kb0 = wv % KS;                                   // this wavefront's keys of the tile
     floatx16 sc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) sc[kb] = S::logits(tk + (kb0 + kb) * 32 * CH, qf, l32, half);
-    if (edge) {
+    if (edge(j0)) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = j0 + 32 * (kb0 + kb) + 8 * (i / 4) + 4 * half + i % 4;
-          const bool hidden = (j > r) | ((j <= r - sh.window) & (j >= sh.sinks));
-          sc[kb][i] = hidden ? -INFINITY : sc[kb][i];
-        }
+      for (int kb = 0; kb < KB; ++kb) hide(sc[kb], j0 + 32 * (kb0 + kb), half);
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      float sum;
-      typename S::Weights w = S::weights(sc[kb], sh.c_log2, m, sum);
-      if (__builtin_expect(__any(!(sum <= MOST)), 0)) {        // too far above the reference (or no number): a new one
-        float top = sc[kb][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-        const float mn = fmaxf(m, fmaxf(top, other_half(top)) * sh.c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= corr;
+      const typename S::Weights w = weigh(sc[kb], [&](float corr) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) acc[cb] *= corr;
-        w = S::weights(sc[kb], sh.c_log2, m, sum);
-      }
-      l += sum;
+      });
       S::add_values(acc, tv + (kb0 + kb) * 32 * CH, w, lane);
     }
   }
 
+  float *lse = row_lse ? row_lse + ((long long)b * sh.h_q + hq) * sh.w - st.n[b] : nullptr;     // of row 0
+  char *dst = out + (st.tok_off[b] * sh.h_q + hq) * ROWB + r * ((long long)sh.h_q * ROWB);
+  auto store = [&](const floatx16 &o, int cb, float inv) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int col = 32 * cb + 8 * k + 4 * half;
+      const float x0 = o[4 * k] * inv, x1 = o[4 * k + 1] * inv, x2 = o[4 * k + 2] * inv, x3 = o[4 * k + 3] * inv;
+      if constexpr (is_f32<T>) *reinterpret_cast<float4 *>(dst + col * 4) = make_float4(x0, x1, x2, x3);
+      else *reinterpret_cast<uint2 *>(dst + col * 2) = make_uint2(round2<T>(x0, x1), round2<T>(x2, x3));
+    }
+  };
+  auto store_lse = [&]() {
+    if (lse && r >= st.n[b] && half == 0) lse[r] = l == 0.0f ? -INFINITY : (m - BIAS<T> + log2f(l)) * LN2;
+  };
+
+  // Where something came out infinite or as NaN, a value that none should have seen may be the reason (a weight of 0 does not
+  // cancel it): once more, 32 columns at a time, with a look at every value of the tiles that hold hidden keys.  (In the
+  // others every row sees every key.)
+  float worst = l * 0.0f;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) worst = fmaf(acc[cb][i], 0.0f, worst);
+  const bool bad = __any(!(worst == 0.0f));
+  if (lane == 0) sh_bad[wv] = bad;
+  __syncthreads();
+  if (sh_bad[0] | sh_bad[1] | sh_bad[2] | sh_bad[3]) {
+#pragma nounroll
+    for (int cb = 0; cb < CB; ++cb) {
+      floatx16 o = floatx16{0};
+      m = M_INIT;
+      l = 0.0f;
+      __syncthreads();
+      load(0);
+#pragma nounroll
+      for (int t = 0; t < tiles; ++t) {
+        const int j0 = first_key(t);
+        meet();
+        if (t + 1 < tiles) load(t + 1);
+        if (wv % KS || unseen(j0)) continue;                   // (one wavefront for all of its rows' keys)
+#pragma nounroll
+        for (int kb = 0; kb < KT / 32; ++kb) {
+          int here = lane;
+          asm volatile("" : "+v"(here));                       // (as in add_seen)
+          const int first = j0 + 32 * kb;
+          const u32x4 *values = shV[t % 2] + kb * 32 * CH;
+          floatx16 sc = S::logits(shK[t % 2] + kb * 32 * CH, qf, here & 31, here >> 5);
+          hide(sc, first, here >> 5);
+          const typename S::Weights w = weigh(sc, [&](float corr) { o *= corr; });
+          if (edge(j0)) {
+            S::template add_block<true>(o, values, w, here, 0, cb);
+            S::template add_block<true>(o, values, w, here, 1, cb);
+            S::add_seen(o, values, w, here, cb, [&](int row) {
+              const int j = first + row;
+              return (j <= r) & ((j > r - sh.window) | (j < sh.sinks));
+            });
+          } else {
+            S::template add_block<false>(o, values, w, here, 0, cb);
+            S::template add_block<false>(o, values, w, here, 1, cb);
+          }
+        }
+      }
+      l += other_half(l);
+      if (wv % KS == 0 && w0 + l32 < n) {
+        store(o, cb, l == 0.0f ? 0.0f : 1.0f / l);
+        if (cb == 0) store_lse();
+      }
+    }
+    return;
+  }
   l += other_half(l);
+
   if constexpr (KS > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place
-    typedef float Sums[CB * 16][64];
-    static_assert((4 - 4 / KS) * sizeof(Sums) <= sizeof(shK), "the sums have room");
-    Sums *sums = reinterpret_cast<Sums *>(&shK[0][0]);
+    typedef float Shared[CB * 16][64];
+    static_assert((4 - 4 / KS) * sizeof(Shared) <= sizeof(shK), "the sums have room");
+    Shared *sums = reinterpret_cast<Shared *>(&shK[0][0]);
     float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(&shV[0][0]);
     const int place = wv / KS * (KS - 1) - 1;                  // + 1 .. KS - 1
     meet();
@@ -375,35 +453,12 @@ __global__ __launch_bounds__(256, KS > 1 && D == 128 && (KS == 4 || T::SIZE == 4
         for (int i = 0; i < 16; ++i) acc[cb][i] = acc[cb][i] * f0 + sums[place + k][cb * 16 + i][lane] * f1;
     }
   }
-  if (w0 >= n) return;
-  float *lse = row_lse ? row_lse + ((long long)b * sh.h_q + hq) * sh.w - st.n[b] : nullptr;     // of row 0
-  char *oh = out + (st.tok_off[b] * sh.h_q + hq) * ROWB;
-  const long long o_tok = (long long)sh.h_q * ROWB;
-  float worst = l;                             // infinite or NaN where any of them is
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) worst = fmaf(acc[cb][i], 0.0f, worst);
-  if (__any(!(__builtin_fabsf(worst) < INFINITY))) {
-    for (int i = 0; i < min(32, n - w0); ++i) {
-      const int ri = w0 + i;
-      careful_row<T, D>(sh, Qh + ri * sh.q_tok, Kh, Vh, ri, oh + ri * o_tok, lse && ri >= st.n[b] ? lse + ri : nullptr);
-    }
-    return;
-  }
+
   if (w0 + l32 >= n) return;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  char *dst = oh + r * o_tok;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int col = 32 * cb + 8 * k + 4 * half;
-      const float x0 = acc[cb][4 * k] * inv, x1 = acc[cb][4 * k + 1] * inv, x2 = acc[cb][4 * k + 2] * inv, x3 = acc[cb][4 * k + 3] * inv;
-      if constexpr (is_f32<T>) *reinterpret_cast<float4 *>(dst + col * 4) = make_float4(x0, x1, x2, x3);
-      else *reinterpret_cast<uint2 *>(dst + col * 2) = make_uint2(round2<T>(x0, x1), round2<T>(x2, x3));
-    }
-  if (lse && r >= st.n[b] && half == 0) lse[r] = l > 0.0f ? (m - BIAS<T> + log2f(l)) * LN2 : -INFINITY;
+  for (int cb = 0; cb < CB; ++cb) store(acc[cb], cb, inv);
+  store_lse();
 }
 
 }  // namespace
