@@ -6,6 +6,8 @@
 // Attention is HBM-bound: 2 d bytes a row and 8 bytes a block for 4 g d flops a row, half of what a 16-bit cache reads.
 // Codes are turned into 16-bit operands in registers (exact: 4 significant bits), two per instruction; fp16 queries
 // meet fp16 keys, all others bf16.  fp32 queries are three bf16 parts, the products of which are added in 32 bits.
+// 64 segments of 8192 rows on average, 64 query heads, d = 128, bf16: 27 us (4.8 TB/s) and 4.4 for the merge kernel (half as many rows in
+// 16 bits: 30 and 4.2).
 #include <math.h>
 
 #include <type_traits>
