@@ -164,6 +164,7 @@ int probe_waves_per_block();
 // ---- decode side of the flattened layout (decode.hip) -----------------------------------------
 struct DecodePlan {
   bool whole;                       // one workgroup per segment, results written directly
+  long long likely, longest;        // rows of the longest segment: at four times the average budget, and at the most
   int split;                        // rows of a segment per workgroup
   int nblk;                         // workgroups launched: an upper bound on what the lengths need
   size_t part_acc, part_ml;         // byte offsets of the per-workgroup partial results

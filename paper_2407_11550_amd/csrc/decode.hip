@@ -791,7 +791,7 @@ DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom
   // layer allows, one head with all of its sequence's prefix budget, 1024; and 384 rows of capacity on average.  (768
   // is where both took the same while the split form's workgroups found their rows 1.5 us later.  They meet near 400
   // rows now: a layer at the line, with half to all of its 768 rows in use, takes up to 2.6 us more than in parts.)
-  long long likely = 0, longest = 0;
+  long long &likely = pl.likely = 0, &longest = pl.longest = 0;
   for (int b = 0; b < st.batch; ++b) {
     const long long most = st.Bp[b] < st.n[b] ? st.Bp[b] : st.n[b];
     const long long four = 4ll * ((st.Bp[b] + dm.h_kv - 1) / dm.h_kv);
@@ -812,9 +812,9 @@ DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom
     // a workspace is as large as the call without a window needs it: fewer rows in shorter parts can be more parts
     const DecodePlan full = plan_decode(st, dm, dtype, headroom, INT_MAX);
     if (pl.nblk > full.nblk) {
-      const bool whole = pl.whole;
+      const DecodePlan window = pl;
       pl = full;                                            // (never fewer parts than the window's rows make)
-      pl.whole = whole;
+      pl.whole = window.whole, pl.likely = window.likely, pl.longest = window.longest;
     }
   }
   return pl;

@@ -191,6 +191,10 @@ template <bool F16> __device__ __forceinline__ unsigned two(unsigned w, bool upp
   }
 }
 
+// Wavefronts of a workgroup that takes a whole segment: as many as its registers (100 to 120 at d = 64, 140 to 160 at
+// d = 128, 213 with eight fp32 queries) and LDS (a wavefront's results, 6 or 12 KB with eight queries) allow.
+template <int D, int G> constexpr int WHOLE_WAVES = D == 64 ? 16 : G == 8 ? 8 : 12;
+
 // As decode_mfma_kernel, tile by tile of 32 rows, one block each:
 //   logits   a lane loads 16 codes of a row at a time, which are two operands of 8; the queries' operands are loaded
 //            in that order of the columns.
@@ -198,12 +202,12 @@ template <bool F16> __device__ __forceinline__ unsigned two(unsigned w, bool upp
 //            side by side, and converts them with the block's scale on the way.
 // The row that the call appends is stored by the wavefront whose tile it belongs to, before it loads that tile.
 template <typename T, int D, int G, bool WHOLE>
-__global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_q8_kernel(
+__global__ __launch_bounds__((WHOLE ? 64 * WHOLE_WAVES<D, G> : 256)) void decode_q8_kernel(
     int nseg, int h, int per, int split, int headroom, float c_log2, const char *__restrict__ q, const char *__restrict__ k_new,
     const char *__restrict__ v_new, const int *__restrict__ cu, const int *seg_len, char *Kc, char *Vc, float *k_scale,
     float *v_scale, DecodeOut res) {
   constexpr bool F16 = Same<T>::f16, F32 = Same<T>::f32;
-  constexpr int NW = WHOLE ? 8 : 4;
+  constexpr int NW = WHOLE ? WHOLE_WAVES<D, G> : 4;
   constexpr int KC = D / 64;                   // 16-byte words of a K row per lane
   constexpr int KS = D / 32;                   // k-steps of the logits
   constexpr int QP = F32 ? 3 : 1;              // parts of a query
@@ -462,7 +466,7 @@ void run_decode_q8(const SeqTab &st, const Dims &dm, int headroom, const DecodeP
                headroom, dm.scale *LOG2E, (const char *)q, (const char *)k_new, (const char *)v_new, cu, (const int *)seg_len, \
                c.K, c.V, c.k_scale, c.v_scale, res)
   if (pl.whole) {
-    ADAKV_DECODE_Q8(true, nseg, 512);
+    ADAKV_DECODE_Q8(true, nseg, (64 * WHOLE_WAVES<D, G>));
     return;
   }
   ADAKV_DECODE_Q8(false, pl.nblk, 256);
@@ -513,12 +517,20 @@ hipError_t launch_append_q8(const SeqTab &st, const Dims &dm, int dtype, int hea
 
 DecodePlan plan_decode_q8(const SeqTab &st, const Dims &dm, int dtype, int headroom) {
   // the 16-bit kernels' division (the same tiles and registers); the workspace is as large as the layer's own type has it
-  const DecodePlan full = plan_decode(st, dm, dtype, headroom);
   DecodePlan pl = plan_decode(st, dm, ADAKV_BF16, headroom);
-  if (pl.nblk <= full.nblk) return pl;
-  const bool whole = pl.whole;
-  pl = full;
-  pl.whole = whole;
+  const DecodePlan full = plan_decode(st, dm, dtype, headroom);
+  if (pl.nblk > full.nblk) pl = full;
+  // One workgroup per segment and no merge kernel up to a longest segment of, in bytes of codes, 768 rows of 128 (512
+  // with fp32 queries, which take three products for one).  us per step, parts | whole, by rows of the longest segment
+  // (the others a third of it): 8 segments, d = 128, g = 4, bf16: 64 8.1 | 5.5, 256 8.5 | 7.0, 512 8.4 | 8.1, 768 8.7 |
+  // 9.2, 1024 8.9 | 11.3; g = 8: 9.1 | 6.1, 9.3 | 7.2, 9.5 | 8.4, 9.5 | 9.8, 9.7 | 11.1; d = 64, fp16: 8.0 | 5.0, 8.1 |
+  // 5.2, 8.2 | 5.8, 8.3 | 6.6, 8.4 | 6.8, 1536 8.5 | 8.3, 2048 8.7 | 9.5; fp32, d = 128: 256 9.3 | 8.2, 512 9.3 | 9.9,
+  // 768 9.7 | 11.0.  From half as many segments as compute units on the parts fill the chip less evenly, and the merge
+  // takes longer: segments of 512 and of 1024 rows, d = 128, g = 4, bf16: 64 segments 9.7 | 8.3 and 10.8 | 11.4, 256
+  // 14.5 | 9.3 and 19.4 | 14.5, 512 24.3 | 18.4 and 33.2 | 27.3; fp32, 256: 15.6 | 10.6 and 20.2 | 15.9.
+  const long long nseg = (long long)st.batch * dm.h_kv;
+  const long long line = 128ll * (nseg >= 128 ? 1024 : dtype == ADAKV_FP32 ? 512 : 768);
+  pl.whole = pl.likely * dm.d <= line && pl.longest * dm.d <= line + line / 3;
   return pl;
 }
 

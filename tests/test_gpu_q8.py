@@ -135,6 +135,41 @@ def test_build_steps_and_attention(case):
                 check(layer, q, want, held, out, lse, f"step {t}")
 
 
+@pytest.mark.parametrize("lens, kernels", [([250, 61], 1), ([1700, 40], 2)], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g", [1, 2, 4, 8])
+@pytest.mark.parametrize("dtype", [BF, FH, FS])
+def test_a_segment_by_one_workgroup_and_in_parts(dtype, g, d, lens, kernels):
+    """Both divisions of the work, for every kernel there is: a step that begins a block, and one that does not."""
+    layer, cache, cu, seg_len, want = build(dtype, g, 2, d, lens, 4)
+    q = rows(dtype, 1, 2 * g, d, 0, 2.0 ** -4)
+    for t in range(4):
+        kn, vn = rows(dtype, 1, 2, d, 2 * t + 1), rows(dtype, 1, 2, d, 2 * t + 2)
+        trace = adakv.KernelTrace(8)
+        with trace:
+            out, lse = adakv.decode_step_q8(layer, q, kn, vn, cu, 4, cache, seg_len, want_lse=True)
+        torch.cuda.synchronize()
+        assert len(trace.durations_us()) == kernels
+        for name, x in (("K", f64(kn)), ("V", f64(vn))):
+            want[name] = [S.append(*want[name][s], x.reshape(-1, d)[s]) for s in range(2)]
+        held = [n + t + 1 for n in lens]
+        assert_cache(cache, cu, 4, held, want, f"step {t}")
+        check(layer, q, want, held, out, lse, f"step {t}")
+
+
+def test_many_segments_up_to_a_thousand_rows():
+    lens = [(900, 7, 480, 33, 2, 256, 1)[i % 7] for i in range(136)]
+    layer, cache, cu, seg_len, want = build(BF, 4, 34, 128, lens, 3)
+    q, kn, vn = rows(BF, 4, 4 * 34, 128, 0, 2.0 ** -4), rows(BF, 4, 34, 128, 1), rows(BF, 4, 34, 128, 2)
+    out, lse = adakv.decode_step_q8(layer, q, kn, vn, cu, 3, cache, seg_len, want_lse=True)
+    torch.cuda.synchronize()
+    for name, x in (("K", f64(kn)), ("V", f64(vn))):
+        want[name] = [S.append(*want[name][s], x.reshape(-1, 128)[s]) for s in range(136)]
+    held = [n + 1 for n in lens]
+    assert_cache(cache, cu, 3, held, want, "step")
+    check(layer, q, want, held, out, lse, "step")
+
+
 @pytest.mark.parametrize("dtype", [BF, FH, FS])
 def test_values_at_the_ends_of_the_range(dtype):
     """Zeros, halves between codes, what no code can hold, and what is no number."""
