@@ -96,19 +96,19 @@ template <typename T, int G> struct HeadSplit {
   static constexpr int NGRP = G / GW;
 };
 
-template <typename T, int D, int G, bool WIN>
-__global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_kernel(
+// WHOLE: one workgroup of 16 wavefronts takes a segment and writes the result itself (fp32 windows).
+template <typename T, int D, int G, bool WHOLE, bool WIN>
+__global__ __launch_bounds__((WHOLE ? 1024 : 256 * HeadSplit<T, G>::NGRP)) void decode_attn_kernel(
     int nseg, int h, int per, int split, int headroom, float c_log2, const T *__restrict__ q,
     const char *__restrict__ k_new, const char *__restrict__ v_new, const int *__restrict__ cu,
-    const int *__restrict__ seg_len, char *Kc, char *Vc, float *__restrict__ part_acc,
-    float *__restrict__ part_ml, int4 *__restrict__ seg_tab, Window win) {
+    const int *seg_len, char *Kc, char *Vc, DecodeOut res, Window win) {
   constexpr int EPL = Elem<T>::EPL;
   constexpr int ROWB = D * (int)sizeof(T);
   constexpr int LPR = ROWB / 16;               // lanes per row
   constexpr int RPW = 64 / LPR;                // rows per wavefront load
-  constexpr int NW = 4;                        // wavefronts that share the rows of a split
   constexpr int GW = HeadSplit<T, G>::GW, NGRP = HeadSplit<T, G>::NGRP;
-  constexpr int NT = 256 * NGRP;
+  constexpr int NW = WHOLE ? 16 / NGRP : 4;    // wavefronts that share the rows of a split
+  constexpr int NT = 64 * NW * NGRP;
   constexpr int U = 4;                         // row loads in flight per lane, for K and for V
 
   __shared__ int sh_scan[24];                  // [0..15] the prefix sum's wavefront totals, [16..21] results
@@ -124,15 +124,31 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
   // With k_new/v_new the call appends one row per segment (Eq. 1) and attends over it as well:
   // the row is taken from k_new/v_new by the lanes it falls to, which also store it in the cache.
   const int grow = k_new != nullptr ? 1 : 0;
-  Work wk;
-  if (!find_work<NW * NGRP, WIN>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, seg_tab, wk, win)) return;
-  const int s = wk.s, len = wk.rows;
+  int s, len, hidden, cu_s, new_row, r0, r1;
+  if constexpr (WHOLE) {
+    s = blockIdx.x;
+    cu_s = cu[s];
+    const int now = rows_held(cu, seg_len, s, headroom, grow);
+    len = seen_rows<WIN>(now, win);
+    hidden = now - len;
+    new_row = now > rows_held(cu, seg_len, s, headroom, 0) ? len - 1 : -1;
+    r0 = 0;
+    r1 = len;
+  } else {
+    Work wk;
+    if (!find_work<NW * NGRP, WIN>(nseg, per, split, headroom, grow, cu, seg_len, sh_scan, res.seg_tab, wk, win)) return;
+    s = wk.s;
+    len = wk.rows;
+    hidden = wk.hidden;
+    cu_s = wk.first_row;
+    new_row = wk.appended ? len - 1 : -1;
+    // (equal parts of the segment, as in decode_mfma_kernel, in multiples of the split's own unit)
+    const int part = ((len + wk.parts - 1) / wk.parts + 63) / 64 * 64;
+    r0 = wk.j * part;
+    r1 = min(len, r0 + part);
+  }
   const int b = s / h, c = s % h;
-  // (equal parts of the segment, as in decode_mfma_kernel, in multiples of the split's own unit)
-  const int part = ((len + wk.parts - 1) / wk.parts + 63) / 64 * 64;
-  const int r0 = wk.j * part, r1 = min(len, r0 + part);
-  const int new_row = wk.appended ? len - 1 : -1;
-  const long long seg_byte = ((long long)wk.first_row + (long long)s * headroom) * ROWB + col * 16;
+  const long long seg_byte = ((long long)cu_s + (long long)s * headroom) * ROWB + col * 16;
   char *Kb = Kc + seg_byte;
   char *Vb = Vc + seg_byte;
   const long long new_byte = (long long)s * ROWB + col * 16;
@@ -165,7 +181,7 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
       const int r = r0 + ((it * U + u) * NW + wv) * RPW + slot;
       ok[u] = r < r1;
       const int rr = min(r, r1 - 1);                           // r1 >= 1: the block exists
-      const long long o = (long long)place_of<WIN>(rr, wk.hidden, win) * ROWB;
+      const long long o = (long long)place_of<WIN>(rr, hidden, win) * ROWB;
       // lanes past the end re-read the block's last row (and ignore it): if that is the new row,
       // they too must take it from k_new/v_new, its place in the cache is not written yet
       const bool fresh = rr == new_row;
@@ -251,11 +267,22 @@ __global__ __launch_bounds__((256 * HeadSplit<T, G>::NGRP)) void decode_attn_ker
       a = fmaf(sh_acc[w2][gi][e], f, a);
       ll = fmaf(sh_l[w2][gi], f, ll);
     }
-    part_acc[((long long)blockIdx.x * G + gi) * D + e] = a;
-    if (e == 0) {
-      part_ml[((long long)blockIdx.x * G + gi) * 2] = M;
-      part_ml[((long long)blockIdx.x * G + gi) * 2 + 1] = ll;
+    if constexpr (WHOLE) {
+      const long long row = (long long)s * G + gi;
+      res.out[row * D + e] = ll > 0.0f ? a / ll : 0.0f;
+      if (res.lse && e == 0) res.lse[row] = ll > 0.0f ? (M + log2f(ll)) * LN2 : -INFINITY;
+    } else {
+      res.part_acc[((long long)blockIdx.x * G + gi) * D + e] = a;
+      if (e == 0) {
+        res.part_ml[((long long)blockIdx.x * G + gi) * 2] = M;
+        res.part_ml[((long long)blockIdx.x * G + gi) * 2 + 1] = ll;
+      }
     }
+  }
+  // (nobody but this workgroup reads the segment's length, and all of it has: a barrier lies between)
+  if (WHOLE && res.new_len && tid == 0) {
+    if (new_row >= 0) res.new_len[s] = len + hidden;
+    else if (res.overflow) *res.overflow = 1;  // the segment was full, its new row was dropped
   }
 }
 
@@ -667,8 +694,8 @@ void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan
   // bf16, g = 1, d = 64 (kernels alone): 64 segments of 1500 rows 11.6 | 12.1, 256 of 6000 81.4 | 87.9, but 256
   // of 1500 26.0 | 23.8, the one shape measured that the matrix kernel does faster.
   constexpr bool VECTOR = sizeof(T) == 4 || G == 1 || (F16 && G == 2 && D == 128);
+  const DecodeOut res = {part_acc, part_ml, seg_tab, out, lse, k_new ? seg_len : nullptr, overflow};
   if constexpr (sizeof(T) == 2) {
-    const DecodeOut res = {part_acc, part_ml, seg_tab, out, lse, k_new ? seg_len : nullptr, overflow};
     if (pl.whole) {
       ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, true, WIN_PART>), dim3(nseg), dim3(512), s, nseg, dm.h_kv,
                    per, pl.split, headroom, dm.scale * LOG2E, (const unsigned short *)q, (const char *)k_new,
@@ -679,12 +706,18 @@ void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan
       ADAKV_LAUNCH("decode_attn", (decode_mfma_kernel<F16, D, G, false, WIN_PART>), dim3(pl.nblk), dim3(256), s, nseg,
                    dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const unsigned short *)q, (const char *)k_new,
                    (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
+  } else if constexpr (WIN_PART) {
+    if (pl.whole) {
+      ADAKV_LAUNCH("decode_attn", (decode_attn_kernel<T, D, G, true, true>), dim3(nseg), dim3(1024), s, nseg, dm.h_kv, per,
+                   pl.split, headroom, dm.scale * LOG2E, (const T *)q, (const char *)k_new, (const char *)v_new, cu,
+                   (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
+      return;
+    }
   }
   if constexpr (VECTOR)
-    ADAKV_LAUNCH("decode_attn", (decode_attn_kernel<T, D, G, WIN_PART>), dim3(pl.nblk), dim3(256 * HeadSplit<T, G>::NGRP), s,
+    ADAKV_LAUNCH("decode_attn", (decode_attn_kernel<T, D, G, false, WIN_PART>), dim3(pl.nblk), dim3(256 * HeadSplit<T, G>::NGRP), s,
                  nseg, dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const T *)q, (const char *)k_new,
-                 (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, part_acc, part_ml, seg_tab,
-                 win);
+                 (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
   // only a call that appends hands the lengths to the merge kernel for updating
   launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
 }
@@ -809,6 +842,22 @@ DecodePlan plan_decode(const SeqTab &st, const Dims &dm, int dtype, int headroom
   pl.seg_tab = pl.part_ml + align_up((size_t)pl.nblk * dm.g * 2 * sizeof(float), 256);
   pl.total = pl.seg_tab + align_up((size_t)nseg * sizeof(int4), 256);
   if (limit < INT_MAX) {
+    // With a window segments are about as long as each other, so that one workgroup per segment pays further: with as
+    // many segments as half the compute units or all of them (if they hold the window on average), longer ones too.
+    // us per call, parts | whole, by rows that it looks at, 16-bit, d = 128, g = 4:
+    //   8 segments     64 10.6 | 8.1   256 10.6 | 8.1   512 10.5 | 8.6   768 10.3 | 11.2   1024 10.4 | 13.1
+    //   128 segments   64 10.1 | 8.0   256 10.3 | 7.8   512 11.5 | 9.1   768 15.3 | 12.8   1024 17.4 | 15.1   2048 26.2 | 25.0
+    //   256 segments   64 10.3 | 8.0   256 12.4 | 8.2   512 19.2 | 13.9  768 23.5 | 18.2   1024 28.0 | 22.6   2048 46.2 | 40.6
+    // (d = 64, 8 segments: 1024 10.4 | 9.6).  The fp32 kernel is bound by its vector instructions, which follow the rows, d and g
+    // (d = 128, g = 4: 8 segments 128 12.1 | 8.8, 256 11.7 | 11.3, 512 11.9 | 18.5, 256 segments 15.1 | 8.8, 19.7 |
+    // 15.2, 28.7 | 24.7, 1024 47.1 | 44.1; g = 8: 8 segments 128 11.5 | 11.4, 256 segments 20.8 | 12.1, 1024 82.5 | 77.6).
+    const long long even = st.out_off[st.batch] >= nseg * limit ? nseg : 0, seen = longest * dm.d;
+    if (longest < limit) {                                  // (it hides nothing: as without a window)
+    } else if (mfma) {
+      pl.whole |= seen <= 128 * (even >= 256 ? 2048 : even >= 128 ? 1024 : 640);
+    } else {
+      pl.whole = even >= 256 ? seen <= 128 * 1024 : seen * dm.g <= 128 * 4 * 256 && seen <= 128 * 512;
+    }
     // a workspace is as large as the call without a window needs it: fewer rows in shorter parts can be more parts
     const DecodePlan full = plan_decode(st, dm, dtype, headroom, INT_MAX);
     if (pl.nblk > full.nblk) {

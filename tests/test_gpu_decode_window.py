@@ -92,6 +92,37 @@ def test_attention_and_steps_against_64_bits(case):
             check(layer, q, K, V, cu, hr, held, window, sinks, out, lse, f"step {t}")
 
 
+@pytest.mark.parametrize("lens, window, kernels", [([900, 61], 100, 1), ([2500, 61], 1500, 2)], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g", [1, 2, 4, 8])
+@pytest.mark.parametrize("dtype", [BF, FH, FS])
+def test_a_segment_by_one_workgroup_and_in_parts(dtype, g, d, lens, window, kernels):
+    """Both divisions of the work, for every kernel there is; the last step finds no room."""
+    layer, K, V, cu, seg_len, q, kn, vn = cache(dtype, g, 2, d, lens, 1)
+    over = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for t in range(2):
+        trace = adakv.KernelTrace(8)
+        with trace:
+            out, lse = adakv.decode_step(layer, q, kn, vn, cu, 1, K, V, seg_len, overflow=over, want_lse=True, window=window, sinks=3)
+        torch.cuda.synchronize()
+        assert len(trace.durations_us()) == kernels
+        held = np.array(lens) + 1
+        assert np.array_equal(seg_len.cpu().numpy(), held) and int(over) == t
+        check(layer, q, K, V, cu, 1, held, window, 3, out, lse, f"step {t}")
+
+
+@pytest.mark.parametrize("dtype", [BF, FS])
+def test_many_segments_that_hold_their_window(dtype):
+    lens = [1010 + i % 5 for i in range(256)]
+    layer, K, V, cu, seg_len, q, _, _ = cache(dtype, 4, 32, 128, lens, 2)
+    trace = adakv.KernelTrace(8)
+    with trace:
+        out, lse = adakv.decode_attn(layer, q, cu, 2, K, V, seg_len, want_lse=True, window=1000, sinks=4)
+    torch.cuda.synchronize()
+    assert len(trace.durations_us()) == 1
+    check(layer, q, K, V, cu, 2, np.array(lens), 1000, 4, out, lse)
+
+
 @pytest.mark.parametrize("dtype", [BF, FH, FS])
 def test_hidden_rows_have_no_part(dtype):
     layer, K, V, cu, seg_len, q, _, _ = cache(dtype, 4, 2, 64, [500, 260], 3)
