@@ -79,7 +79,7 @@ __device__ __forceinline__ float other_half(float x) {
 __device__ __forceinline__ void load_to_lds(const char *base, unsigned off, unsigned at, const u32x4 *dst) {
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
-                   (unsigned)(size_t)(__attribute__((address_space(3))) const void *)dst),
+                   __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const void *)dst)),
                "v"(off), "s"(rs), "s"(at)
                : "memory", "m0");
 }
@@ -99,6 +99,7 @@ template <typename T, int D, int KS> struct Tile {
   static constexpr int ROWB = D * T::SIZE, CH = ROWB / 16;
   static constexpr int KT = KS > 1 ? 32 * KS : T::SIZE == 4 ? 32 : 64;
   static constexpr int WORDS = KT * CH;
+  static constexpr int TURNS = 4 * WORDS * 16 <= 160 * 1024 ? 2 : 1;      // tiles of each tensor in LDS at a time
   static constexpr int RPI = 64 / CH;                          // rows per load instruction
   static constexpr int LOADS = WORDS / 256;                    // load instructions per wavefront and tensor
   static __device__ __forceinline__ int swz_k(int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; }
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
   constexpr int ROWS = 128 / KS;                          // query rows of the workgroup
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32 / KS;
   constexpr int CB = D / 32;                                   // column blocks of O^T
-  __shared__ __align__(16) u32x4 shK[2][TL::WORDS], shV[2][TL::WORDS];
+  __shared__ __align__(16) u32x4 shK[TL::TURNS][TL::WORDS], shV[TL::TURNS][TL::WORDS];
   __shared__ int sh_bad[4];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -270,30 +271,56 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
   const int lo = max(0, q0 - sh.window + 1) / KT, hi = last / KT;
   const int firsts = min((int)(((long long)sh.sinks + KT - 1) / KT), lo), tiles = firsts + hi - lo + 1;
   // the wavefront's share of a tile: rows on (wv * LOADS + i) * RPI + lane / CH
+  auto at_k = [&](int row, int lane) { return row * (unsigned)sh.k_tok + ((lane % CH) ^ TL::swz_k(row)) * 16; };
+  auto at_v = [&](int row, int lane) { return row * (unsigned)sh.v_tok + ((lane % CH) ^ TL::swz_v(row)) * 16; };
   unsigned off_k[TL::LOADS], off_v[TL::LOADS];
 #pragma unroll
   for (int i = 0; i < TL::LOADS; ++i) {
     const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
-    off_k[i] = row * (unsigned)sh.k_tok + ((lane % CH) ^ TL::swz_k(row)) * 16;
-    off_v[i] = row * (unsigned)sh.v_tok + ((lane % CH) ^ TL::swz_v(row)) * 16;
+    off_k[i] = at_k(row, lane);
+    off_v[i] = at_v(row, lane);
   }
   auto first_key = [&](int t) { return (t < firsts ? t : lo + t - firsts) * KT; };
-  auto load = [&](int t) {
+  auto load = [&](int t) __attribute__((always_inline)) {
     const int j0 = first_key(t);
     const char *kb = scalar_address(Kh + j0 * sh.k_tok), *vb = scalar_address(Vh + j0 * sh.v_tok);
-    const u32x4 *dk = shK[t % 2] + wv * TL::LOADS * 64, *dv = shV[t % 2] + wv * TL::LOADS * 64;
-    if (j0 + KT <= n) {
+    const u32x4 *dk = shK[t % TL::TURNS] + wv * TL::LOADS * 64, *dv = shV[t % TL::TURNS] + wv * TL::LOADS * 64;
+    if (TL::LOADS > 8) {                                       // (so many places do not fit in registers)
+      int here = lane;
+      asm volatile("" : "+v"(here));
+      const int end = n - 1 - j0;                              // rows past the sequence's end repeat its last one
+#pragma unroll
+      for (int i = 0; i < TL::LOADS; ++i) {
+        const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH, back = max(row - end, 0);
+        load_to_lds(kb, at_k(row, here) - back * (unsigned)sh.k_tok, 0u, dk + i * 64);
+        load_to_lds(vb, at_v(row, here) - back * (unsigned)sh.v_tok, 0u, dv + i * 64);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else if (j0 + KT <= n) {
 #pragma unroll
       for (int i = 0; i < TL::LOADS; ++i) load_to_lds(kb, off_k[i], 0u, dk + i * 64);
 #pragma unroll
       for (int i = 0; i < TL::LOADS; ++i) load_to_lds(vb, off_v[i], 0u, dv + i * 64);
-    } else {                                                   // rows past the sequence's end repeat its last one
+    } else {
 #pragma unroll
       for (int i = 0; i < TL::LOADS; ++i) {
         const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH, back = max(row - (n - 1 - j0), 0);
         load_to_lds(kb, off_k[i] - back * (unsigned)sh.k_tok, 0u, dk + i * 64);
         load_to_lds(vb, off_v[i] - back * (unsigned)sh.v_tok, 0u, dv + i * 64);
       }
+    }
+  };
+  // tile t is there, and the next one on its way where it has a place of its own
+  auto await = [&](int t) __attribute__((always_inline)) {
+    if constexpr (TL::TURNS == 2) {
+      meet();
+      if (t + 1 < tiles) load(t + 1);
+    } else {
+      if (t > 0) {
+        meet();
+        load(t);
+      }
+      meet();
     }
   };
 
@@ -334,9 +361,8 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
   load(0);
   for (int t = 0; t < tiles; ++t) {
     const int j0 = first_key(t);
-    const u32x4 *tk = shK[t % 2], *tv = shV[t % 2];
-    meet();
-    if (t + 1 < tiles) load(t + 1);
+    const u32x4 *tk = shK[t % TL::TURNS], *tv = shV[t % TL::TURNS];
+    await(t);
     if (unseen(j0)) continue;
     const int kb0 = wv % KS;                                   // this wavefront's keys of the tile
     floatx16 sc[KB];
@@ -393,16 +419,15 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
 #pragma nounroll
       for (int t = 0; t < tiles; ++t) {
         const int j0 = first_key(t);
-        meet();
-        if (t + 1 < tiles) load(t + 1);
+        await(t);
         if (wv % KS || unseen(j0)) continue;                   // (one wavefront for all of its rows' keys)
 #pragma nounroll
         for (int kb = 0; kb < KT / 32; ++kb) {
           int here = lane;
           asm volatile("" : "+v"(here));                       // (as in add_seen)
           const int first = j0 + 32 * kb;
-          const u32x4 *values = shV[t % 2] + kb * 32 * CH;
-          floatx16 sc = S::logits(shK[t % 2] + kb * 32 * CH, qf, here & 31, here >> 5);
+          const u32x4 *values = shV[t % TL::TURNS] + kb * 32 * CH;
+          floatx16 sc = S::logits(shK[t % TL::TURNS] + kb * 32 * CH, qf, here & 31, here >> 5);
           hide(sc, first, here >> 5);
           const typename S::Weights w = weigh(sc, [&](float corr) { o *= corr; });
           if (edge(j0)) {
@@ -488,11 +513,19 @@ hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const
   // 24.7 | 28.1, 512 26.8 | 33.3.  Nothing is there to share in 64 keys: 6.6 | 7.3.
   ChunkTab ct = chunks(128);
   const long long wgs = (long long)ct.off[st.batch] * dm.h_q;
-  long long reach = 0;                         // keys that the last rows see
-  for (int b = 0; b < st.batch; ++b) reach = st.n[b] + dm.w > reach ? st.n[b] + dm.w : reach;
-  if ((long long)window + sinks < reach) reach = (long long)window + sinks;
-  const bool room_for_four = !(dtype == ADAKV_FP32 && dm.d == 128);      // (tiles of 128 keys, twice, in a compute unit's LDS)
-  const int share = reach <= 128 ? 1 : wgs <= 128 && room_for_four ? 4 : wgs <= 256 || (wgs <= 512 && reach >= 1024) ? 2 : 1;
+  long long longest = 0;
+  for (int b = 0; b < st.batch; ++b) longest = st.n[b] + dm.w > longest ? st.n[b] + dm.w : longest;
+  const long long reach = (long long)window + sinks < longest ? (long long)window + sinks : longest;   // keys that the last rows see
+  int share = reach <= 128 ? 1 : wgs <= 128 ? 4 : wgs <= 256 || (wgs <= 512 && reach >= 1024) ? 2 : 1;
+  // fp32: 32 keys take 1.7 us at d = 64 and 3.4 at d = 128, so sharing pays from the second 32 on.  d = 128: 4 workgroups, 40
+  // keys 13.1 | 9.8 | 11.6, 100 keys 22.8 | 14.4 | 12.0; 24, 729 keys 101 | 57 | 38; 96, 1500 keys 201 | 110 | 72; 192, 1500 keys
+  // 203 | 115 | 129; 384, 1500 keys 250 | 194 | 231; 768, 1500 keys 342 | 356 | 454; a window of 200 of 1500 keys: 48 workgroups 59
+  // | 34 | 31, 96 58 | 35 | 59, 192 59 | 67 | 86.  d = 64, where two of the workgroups of half the rows fit on a unit: 768, 3000 keys
+  // 381 | 317 | 416, a window of 200: 384 56 | 51 | 91, 768 79 | 95 | 165.
+  if (dtype == ADAKV_FP32) {
+    const bool even = reach < longest / 2;                 // most rows have ways of the same length
+    share = reach <= 64 ? (wgs <= 256 ? 2 : 1) : wgs <= (even ? 64 : 128) ? 4 : wgs * dm.d <= (even ? 192 : 384) * 128 ? 2 : 1;
+  }
   if (share > 1) ct = chunks(128 / share);
   const dim3 grid((unsigned)((long long)ct.off[st.batch] * dm.h_q));
 #define ADAKV_WINDOW_KS(T, D, KS)                                                                                           \
@@ -500,9 +533,9 @@ hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const
                (const char *)V, (char *)out, row_lse)
 #define ADAKV_WINDOW(T, D)                                                                                                  \
   do {                                                                                                                      \
-    if constexpr (T::SIZE == 2 || D == 64)                                                                                  \
-      if (share == 4) { ADAKV_WINDOW_KS(T, D, 4); break; }                                                                  \
-    if (share == 2) ADAKV_WINDOW_KS(T, D, 2); else ADAKV_WINDOW_KS(T, D, 1);                                                \
+    if (share == 4) ADAKV_WINDOW_KS(T, D, 4);                                                                               \
+    else if (share == 2) ADAKV_WINDOW_KS(T, D, 2);                                                                          \
+    else ADAKV_WINDOW_KS(T, D, 1);                                                                                          \
   } while (0)
   if (dtype == ADAKV_BF16) { if (dm.d == 64) ADAKV_WINDOW(BF16, 64); else ADAKV_WINDOW(BF16, 128); }
   else if (dtype == ADAKV_FP16) { if (dm.d == 64) ADAKV_WINDOW(FP16, 64); else ADAKV_WINDOW(FP16, 128); }

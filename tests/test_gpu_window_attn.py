@@ -79,6 +79,25 @@ def test_prompts_against_64_bits(case):
     check(layer, q, K, V, window, sinks, out, lse, heads=None if h_q < 16 else (0, 1, h_q // 2, h_q - 1))
 
 
+# fp32: rows shared by one, two and four wavefronts (by the number of workgroups and what the rows see)
+FP32_CASES = [
+    (FS, 2, 1, 128, [3, 129, 257], 2, 2 ** 31 - 1, 0),
+    (FS, 3, 3, 128, [700], 32, 2 ** 31 - 1, 0),
+    (FS, 3, 3, 64, [700, 640], 32, 300, 40),
+    (FS, 2, 2, 128, [900], 5, 65, 200),
+    (FS, 16, 4, 128, [600, 130, 2], 1, 120, 1),
+    (FS, 48, 6, 128, [500], 9, 2 ** 31 - 1, 0),
+    (FS, 40, 10, 128, [40, 64, 33], 1, 64, 0),
+    (FS, 64, 8, 128, [500, 400], 3, 50, 3),
+    (FS, 64, 8, 64, [500, 400, 390], 3, 100, 3),
+]
+
+
+@pytest.mark.parametrize("case", FP32_CASES, ids=lambda c: "%d_%d_d%d_n%s_w%d_win%d_s%d" % (c[1], c[2], c[3], "_".join(map(str, c[4])), *c[5:]))
+def test_fp32_prompts_against_64_bits(case):
+    test_prompts_against_64_bits(case)
+
+
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 64), (FS, 64)])
 def test_strided_tensors_loose_sequences_and_a_scale(dtype, d):
     """q, K and V as views into one fused buffer, NaN rows between the sequences, `out` rows of no sequence as they were."""
@@ -131,6 +150,13 @@ def test_hidden_keys_and_values_have_no_part(dtype, d, what, window, h_q):
             bound = attention_bound(dtype, d, ref, mag, big, lse, keys, rounded=True)
             assert_within(f64(got[:, hq])[check_rows], ref[check_rows], bound[check_rows], f"head {hq}")
     assert torch.isfinite(clean.float()).all()
+
+
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+@pytest.mark.parametrize("window", [40, 230])
+def test_hidden_values_in_fp32_rows_of_128(what, window):
+    """As above, where four wavefronts share rows and a tile has no second place to be loaded to."""
+    test_hidden_keys_and_values_have_no_part(FS, 128, what, window, 2)
 
 
 def test_logits_far_apart_and_growing_along_the_keys():
