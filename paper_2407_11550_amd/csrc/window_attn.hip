@@ -504,28 +504,33 @@ hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const
     for (int b = st.batch + 1; b <= ADAKV_MAX_BATCH; ++b) ct.off[b] = ct.off[st.batch];
     return ct;
   };
-  // A wavefront takes 0.9 us for 32 keys whatever else there is to do, so with few workgroups (two fit on each of 256 compute
-  // units) wavefronts share rows.  us, 128 | 64 | 32 rows a workgroup, by the number that 128 rows make; all keys visible, d = 128
-  // but for the last two: 64 workgroups, 256 keys 10.6 | 9.7 | 8.8; 128, 2048 keys 43.5 | 31.0 | 28.9; 160, 541 keys
-  // 17.1 | 14.7 | 22.0; 256, 1024 keys 27.3 | 22.8 | 40.0; 384, 1536 keys 40.8 | 35.9; 512, 2043 keys 54.9 | 53.2; 512, 8192 keys
-  // 191 | 173; 1024, 4096 keys 159 | 182; d = 64: 128, 2048 keys 30.6 | 22.7 | 16.4; 256, 1024 keys 18.4 | 15.2 | 17.2.  Where a
-  // window makes all rows' ways equally short there is no longest one to shorten: 300 keys, 256 workgroups 19.1 | 18.4, 384
-  // 24.7 | 28.1, 512 26.8 | 33.3.  Nothing is there to share in 64 keys: 6.6 | 7.3.
+  // A wavefront takes 0.9 us for 32 keys whatever else there is to do, so with few workgroups (two of 128 or 64 rows fit on each
+  // of 256 compute units, one of 32; at d = 64 twice as many of those that share) wavefronts share rows.  us, 128 | 64 | 32 rows a
+  // workgroup, by the number that 128 rows make; all keys visible, d = 128: 4 workgroups, 64 keys 6.0 | 6.6 | 7.6, 100 keys
+  // 8.6 | 6.8 | 7.4; 64, 256 keys 10.6 | 9.7 | 8.8; 96, 1500 keys 37.7 | 24.6 | 21.1; 128, 2048 keys 43.5 | 31.0 | 28.9; 160, 541
+  // keys 17.1 | 14.7 | 22.0; 192, 3000 keys 69 | 49 | 60; 256, 1024 keys 27.3 | 22.8 | 40.0; 384, 1500 keys 42 | 35 | 70; 512, 2043
+  // keys 54.9 | 53.2; 512, 8192 keys 191 | 173; 1024, 4096 keys 159 | 182; d = 64: 192, 729 keys 18.2 | 13.0 | 14.3, 3000 keys
+  // 52 | 34 | 26; 384, 1500 keys 32 | 23 | 31.  Where a window makes most rows' ways equally short there is no longest one to shorten;
+  // 60 and 500 keys, d = 128: 48 workgroups 12.8 | 9.4 | 10.5 and 23.0 | 15.5 | 13.9, 96 13.1 | 9.7 | 19.4 and 23.6 | 16.0 | 21.9,
+  // 192 13.7 | 12.5 | 28.5 and 24.1 | 21.4 | 38.9, 376 17.8 | 21.1 | 57.0 and 33.1 | 35.2 | 77.6; d = 64: 96 10.8 | 7.5 | 9.0 and
+  // 18.8 | 11.9 | 12.4, 384 14.4 | 11.6 | 21.8 and 20.7 | 16.7 | 27.3.
   ChunkTab ct = chunks(128);
   const long long wgs = (long long)ct.off[st.batch] * dm.h_q;
   long long longest = 0;
   for (int b = 0; b < st.batch; ++b) longest = st.n[b] + dm.w > longest ? st.n[b] + dm.w : longest;
   const long long reach = (long long)window + sinks < longest ? (long long)window + sinks : longest;   // keys that the last rows see
-  int share = reach <= 128 ? 1 : wgs <= 128 ? 4 : wgs <= 256 || (wgs <= 512 && reach >= 1024) ? 2 : 1;
+  const bool even = reach < longest / 2;       // most rows have ways of the same length
+  const int by_d = 128 / dm.d;
+  const long long four = even ? (reach > 128 ? 64 : 0) : by_d == 2 && reach >= 1024 ? 192 : 128;
+  const long long two = !even && reach >= 1024 ? 512 : 256 * by_d;
+  int share = longest <= 64 ? 1 : wgs <= four ? 4 : wgs <= two ? 2 : 1;
   // fp32: 32 keys take 1.7 us at d = 64 and 3.4 at d = 128, so sharing pays from the second 32 on.  d = 128: 4 workgroups, 40
   // keys 13.1 | 9.8 | 11.6, 100 keys 22.8 | 14.4 | 12.0; 24, 729 keys 101 | 57 | 38; 96, 1500 keys 201 | 110 | 72; 192, 1500 keys
   // 203 | 115 | 129; 384, 1500 keys 250 | 194 | 231; 768, 1500 keys 342 | 356 | 454; a window of 200 of 1500 keys: 48 workgroups 59
   // | 34 | 31, 96 58 | 35 | 59, 192 59 | 67 | 86.  d = 64, where two of the workgroups of half the rows fit on a unit: 768, 3000 keys
   // 381 | 317 | 416, a window of 200: 384 56 | 51 | 91, 768 79 | 95 | 165.
-  if (dtype == ADAKV_FP32) {
-    const bool even = reach < longest / 2;                 // most rows have ways of the same length
-    share = reach <= 64 ? (wgs <= 256 ? 2 : 1) : wgs <= (even ? 64 : 128) ? 4 : wgs * dm.d <= (even ? 192 : 384) * 128 ? 2 : 1;
-  }
+  if (dtype == ADAKV_FP32)
+    share = reach <= 64 ? (wgs <= 256 ? 2 : 1) : wgs <= (even ? 64 : 128) ? 4 : wgs <= (even ? 192 : 384) * by_d ? 2 : 1;
   if (share > 1) ct = chunks(128 / share);
   const dim3 grid((unsigned)((long long)ct.off[st.batch] * dm.h_q));
 #define ADAKV_WINDOW_KS(T, D, KS)                                                                                           \
