@@ -79,7 +79,7 @@ __device__ __forceinline__ float other_half(float x) {
 __device__ __forceinline__ void load_to_lds(const char *base, unsigned off, unsigned at, const u32x4 *dst) {
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
-                   __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const void *)dst)),
+                   (unsigned)(size_t)(__attribute__((address_space(3))) const void *)dst),
                "v"(off), "s"(rs), "s"(at)
                : "memory", "m0");
 }
