@@ -135,6 +135,19 @@ def test_hidden_rows_have_no_part(dtype):
     assert torch.equal(got, want) and torch.isfinite(got).all()
 
 
+@pytest.mark.parametrize("lens, window", [([900, 61], 100), ([2500, 61], 1500)], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("dtype, g, d", [(BF, 4, 128), (BF, 1, 64), (FH, 8, 64), (FS, 4, 128)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_a_key_that_is_no_number_is_not_passed_over(dtype, g, d, lens, window, what):
+    """A visible row of NaN or infinite keys, as the last appended one: the group's results are no numbers, the others are."""
+    layer, K, V, cu, seg_len, q, _, _ = cache(dtype, g, 2, d, lens, 3)
+    K[lens[0] - 1] = what
+    out, lse = adakv.decode_attn(layer, q.abs() + 1.0, cu, 3, K, V, seg_len, want_lse=True, window=window, sinks=2)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0, :g]).all() and torch.isnan(lse[0, :g]).all()
+    assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
+
+
 def test_empty_and_corrupt_lengths():
     layer, K, V, cu, seg_len, q, kn, vn = cache(BF, 4, 3, 128, [60, 50, 40], 3)
     seg_len[1] = 0

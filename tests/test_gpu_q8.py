@@ -236,6 +236,17 @@ def test_nan_rows_spoil_their_head_alone_and_empty_segments():
     assert torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("lens", [[250, 61], [1700, 40]], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("dtype, g, d", [(BF, 4, 128), (FH, 8, 64), (FS, 1, 128)])
+def test_a_key_that_is_no_number_is_not_passed_over(dtype, g, d, lens):
+    layer, cache, cu, seg_len, _ = build(dtype, g, 2, d, lens, 4)
+    cache.K.view(torch.uint8)[lens[0] - 1, d // 2] = 0x7f
+    out, lse = adakv.decode_attn_q8(layer, rows(dtype, 1, 2 * g, d, 0, 2.0 ** -4), cu, 4, cache, seg_len, want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0, :g]).all() and torch.isnan(lse[0, :g]).all()
+    assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
+
+
 def test_strides_loose_sequences_and_another_stream():
     """K and V as views into one buffer with gaps between the sequences."""
     h, d, w, lens, hr = 2, 128, 4, [40, 70, 33, 9], 5
