@@ -333,6 +333,7 @@ int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
  * adakv_decode_attn and adakv_decode_step over a segment's visible rows: with len rows held (the
  * appended one included) those are t < sinks and t >= len - window.  Arguments as for the two calls; a
  * workspace of adakv_decode_workspace_bytes(L, headroom) bytes does.
+ * A visible key that is no finite number makes its heads' results NaN; hidden rows are not read.
  */
 int adakv_decode_window_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
                              int32_t headroom, const void *K_cache, const void *V_cache,
