@@ -13,7 +13,8 @@
 // (capacity / split + segments); each workgroup finds its segment and its part of it from a prefix sum
 // of the lengths, writes partial (max, sum, weighted value sum) per query head, and a second kernel
 // merges the parts of each segment.  Where no segment of a layer can be long, one workgroup takes each
-// segment (decode_mfma_kernel, WHOLE) and writes the result itself: no prefix sum, no merge.
+// segment (WHOLE: decode_mfma_kernel, and decode_attn_kernel for fp32 windows) and writes the result itself: no
+// prefix sum, no merge.
 //
 // A call with a window looks at a segment's first rows (the sinks) and its last ones alone: the kernels number the
 // rows it sees and leave a gap where the sinks end (WIN).  Those instantiations are built as a translation unit of
