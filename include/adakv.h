@@ -273,6 +273,10 @@ size_t adakv_decode_workspace_bytes(const adakv_layer *L, int32_t headroom);
  *
  * Logits, the softmax and the weighted sum are accumulated in fp32.  A segment of length 0
  * gives a zero row and lse = -inf.  The projection by W^O is not part of this call.
+ * A logit that is NaN or +inf makes its head's out and lse NaN.  One of -inf has weight 0; where there
+ * are no others out is NaN and lse -inf.  Logits beyond 2^26 in magnitude, whose rounding to fp32 alone is up
+ * to 4, can make their head's results NaN.  A weighted sum beyond the fp32 range is infinite or NaN: values times
+ * the number of rows stay below 2^127.
  *
  *   q_new (device) [batch][h_q][d] contiguous, L->dtype, 16-byte aligned
  *   out   (device) [batch][h_q][d] fp32, written
@@ -333,7 +337,7 @@ int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
  * adakv_decode_attn and adakv_decode_step over a segment's visible rows: with len rows held (the
  * appended one included) those are t < sinks and t >= len - window.  Arguments as for the two calls; a
  * workspace of adakv_decode_workspace_bytes(L, headroom) bytes does.
- * A visible key that is no finite number makes its heads' results NaN; hidden rows are not read.
+ * Hidden rows are not read.
  */
 int adakv_decode_window_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
                              int32_t headroom, const void *K_cache, const void *V_cache,

@@ -183,7 +183,7 @@ hipError_t launch_decode_window(const SeqTab &st, const Dims &dm, int dtype, int
                                 const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,
                                 int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s);
 // Merges the partial results of a plan's workgroups; new_len: the lengths of a call that appends, else null.
-void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, bool keep_nan, char *ws, int *new_len, int *overflow,
+void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, char *ws, int *new_len, int *overflow,
                            float *out, float *lse, hipStream_t s);
 hipError_t launch_append(const SeqTab &st, const Dims &dm, int dtype, int headroom,
                          const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,

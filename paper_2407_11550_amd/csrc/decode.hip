@@ -270,9 +270,8 @@ __global__ __launch_bounds__((WHOLE ? 1024 : 256 * HeadSplit<T, G>::NGRP)) void 
     }
     if constexpr (WHOLE) {
       const long long row = (long long)s * G + gi;
-      const bool none = no_weight<WIN>(ll);
-      res.out[row * D + e] = none ? 0.0f : a / ll;
-      if (res.lse && e == 0) res.lse[row] = none ? -INFINITY : (M + log2f(ll)) * LN2;
+      res.out[row * D + e] = len > 0 ? a / ll : 0.0f;
+      if (res.lse && e == 0) res.lse[row] = (M + log2f(ll)) * LN2;
     } else {
       res.part_acc[((long long)blockIdx.x * G + gi) * D + e] = a;
       if (e == 0) {
@@ -554,9 +553,8 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
     }
     if constexpr (WHOLE) {
       const long long row = (long long)s * G + gi;
-      const bool none = no_weight<WIN>(ll);
-      res.out[row * D + e] = none ? 0.0f : a / ll;
-      if (res.lse && e == 0) res.lse[row] = none ? -INFINITY : (M + log2f(ll)) * LN2;
+      res.out[row * D + e] = len > 0 ? a / ll : 0.0f;
+      if (res.lse && e == 0) res.lse[row] = (M + log2f(ll)) * LN2;
     } else {
       res.part_acc[((long long)blockIdx.x * G + gi) * D + e] = a;
       if (e == 0) {
@@ -578,7 +576,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256) void decode_mfma_kernel(
 // (each by D/4 lanes holding a float4 of the value sum), four loads deep, then across slots.
 template <int D, int G>
 __global__ __launch_bounds__(1024) void decode_combine_kernel(
-    bool keep_nan, const int4 *__restrict__ seg_tab, int *__restrict__ seg_len, int *__restrict__ overflow,
+    const int4 *__restrict__ seg_tab, int *__restrict__ seg_len, int *__restrict__ overflow,
     const float *__restrict__ part_acc, const float *__restrict__ part_ml,
     float *__restrict__ out, float *__restrict__ lse) {
   constexpr int LPE = D / 4;
@@ -648,9 +646,8 @@ __global__ __launch_bounds__(1024) void decode_combine_kernel(
       for (int k = 0; k < live; ++k) add(k);
     }
     const long long row = (long long)s * G + gi;       // = (b*h + c)*G + gi
-    const bool none = keep_nan ? no_weight<true>(ll) : no_weight<false>(ll);
-    out[row * D + tid] = none ? 0.0f : acc / ll;
-    if (lse && tid == 0) lse[row] = none ? -INFINITY : (M + log2f(ll)) * LN2;
+    out[row * D + tid] = cnt > 0 ? acc / ll : 0.0f;
+    if (lse && tid == 0) lse[row] = (M + log2f(ll)) * LN2;
   }
 }
 
@@ -723,7 +720,7 @@ void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan
                  nseg, dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const T *)q, (const char *)k_new,
                  (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
   // only a call that appends hands the lengths to the merge kernel for updating
-  launch_decode_combine(nseg, D, G, pl, WIN_PART, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
+  launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
 }
 
 struct DecodeArgs {
@@ -778,14 +775,14 @@ hipError_t launch_decode_window(const SeqTab &st, const Dims &dm, int dtype, int
 
 #else
 
-void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, bool keep_nan, char *ws, int *new_len, int *overflow,
+void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, char *ws, int *new_len, int *overflow,
                            float *out, float *lse, hipStream_t s) {
   const float *part_acc = (const float *)(ws + pl.part_acc), *part_ml = (const float *)(ws + pl.part_ml);
   const int4 *seg_tab = (const int4 *)(ws + pl.seg_tab);
 #define ADAKV_COMBINE(D, G)                                                                       \
   if (d == D && g == G)                                                                           \
     ADAKV_LAUNCH("decode_combine", (decode_combine_kernel<D, G>), dim3(nseg, G), dim3(1024), s,   \
-                 keep_nan, seg_tab, new_len, overflow, part_acc, part_ml, out, lse)
+                 seg_tab, new_len, overflow, part_acc, part_ml, out, lse)
 #define ADAKV_COMBINE_D(D) ADAKV_COMBINE(D, 1); ADAKV_COMBINE(D, 2); ADAKV_COMBINE(D, 4); ADAKV_COMBINE(D, 8)
   ADAKV_COMBINE_D(64);
   ADAKV_COMBINE_D(128);

@@ -151,12 +151,9 @@ __device__ __forceinline__ float half_of(unsigned w, bool odd) {
 // finite number: the upper part alone makes the product infinite.
 __device__ __forceinline__ float low_part(float x) { return fminf(x - cut(x, true), LOW_MAX); }
 
-// Whether a sum of weights is that of no rows.  A key that is no number makes the sum one too: calls with a window and of 8-bit
-// caches pass it on (KEEP_NAN), those without give zeros.
-template <bool KEEP_NAN> __device__ __forceinline__ bool no_weight(float sum) { return KEEP_NAN ? sum == 0.0f : !(sum > 0.0f); }
-
 // Where a workgroup's result goes: partial results for the merge kernel, or (WHOLE, one workgroup per
-// segment) straight to the caller.
+// segment) straight to the caller.  Only a segment of no rows has zeros for a result: a sum of weights that is no
+// number, or 0 because every logit is -inf, makes it NaN.
 struct DecodeOut {
   float *part_acc, *part_ml;
   int4 *seg_tab;

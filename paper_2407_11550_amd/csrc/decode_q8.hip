@@ -438,9 +438,8 @@ __global__ __launch_bounds__((WHOLE ? 64 * WHOLE_WAVES<D, G> : 256)) void decode
     }
     if constexpr (WHOLE) {
       const long long row = (long long)s * G + gi;
-      const bool none = no_weight<true>(ll);
-      res.out[row * D + e] = none ? 0.0f : a / ll;
-      if (res.lse && e == 0) res.lse[row] = none ? -INFINITY : (M + log2f(ll)) * LN2;
+      res.out[row * D + e] = len > 0 ? a / ll : 0.0f;
+      if (res.lse && e == 0) res.lse[row] = (M + log2f(ll)) * LN2;
     } else {
       res.part_acc[((long long)blockIdx.x * G + gi) * D + e] = a;
       if (e == 0) {
@@ -472,7 +471,7 @@ void run_decode_q8(const SeqTab &st, const Dims &dm, int headroom, const DecodeP
   }
   ADAKV_DECODE_Q8(false, pl.nblk, 256);
 #undef ADAKV_DECODE_Q8
-  launch_decode_combine(nseg, D, G, pl, true, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
+  launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
 }
 
 // A template's call by the layer's type, d (and g): `false` where there is none.

@@ -1,0 +1,73 @@
+"""Attention where the numbers end: logits that are no numbers or infinite, rows that no weight is left for."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_11550_amd as adakv
+from oracle import serve_oracle as S
+from serve_util import DEV, assert_within, attention_bound, f64, lse_bound
+from test_gpu_decode_window import cache
+from test_gpu_q8 import build
+
+pytestmark = pytest.mark.gpu
+BF, FH, FS = torch.bfloat16, torch.float16, torch.float32
+
+# (lengths, window): a segment by one workgroup, in parts; the same two without a window
+DIVISIONS = {"one_workgroup": ([900, 61], 100), "parts": ([2500, 61], 1500), "short": ([150, 61], None), "long": ([2500, 61], None)}
+
+
+@pytest.mark.parametrize("div", DIVISIONS, ids=str)
+@pytest.mark.parametrize("dtype, g, d", [(BF, 4, 128), (BF, 1, 64), (FH, 8, 64), (FS, 4, 128)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_a_step_over_infinite_keys(div, dtype, g, d, sign):
+    """A logit of -inf has weight 0; where the visible rows have no other the result is none: NaN, and ln 0."""
+    lens, window = DIVISIONS[div]
+    kw = {} if window is None else dict(window=window, sinks=2)
+    layer, K, V, cu, seg_len, q, _, _ = cache(dtype, g, 2, d, lens, 3)
+    q = sign * (q.abs() + 1.0)
+    K[lens[0] - 7] = -sign * float("inf")
+    out, lse = adakv.decode_attn(layer, q, cu, 3, K, V, seg_len, want_lse=True, **kw)
+    torch.cuda.synchronize()
+    see = S.step_rows(lens[0], window or lens[0], 2)
+    see = see[see != lens[0] - 7]
+    for i in range(g):
+        ref, z, mag, big = S.attend(f64(q[0, i]), f64(K[see]), f64(V[see]), 1 / math.sqrt(d))
+        keys = np.array(len(see))
+        assert_within(f64(out[0, i]), ref, attention_bound(dtype, d, ref, mag, np.array(big), np.array(z), keys, rounded=False), f"head {i}")
+        assert_within(f64(lse[0, i]), z, lse_bound(d, np.array(big), np.array(z), keys), f"lse {i}")
+    K[:lens[0]] = -sign * float("inf")
+    out, lse = adakv.decode_attn(layer, q, cu, 3, K, V, seg_len, want_lse=True, **kw)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0, :g]).all() and torch.isneginf(lse[0, :g]).all()
+    assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
+
+
+@pytest.mark.parametrize("lens", [[150, 61], [2500, 61]], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("dtype, g, d", [(BF, 4, 128), (BF, 1, 64), (FH, 8, 64), (FS, 4, 128)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_a_key_that_is_no_number_is_not_passed_over_without_a_window(dtype, g, d, lens, what):
+    layer, K, V, cu, seg_len, q, _, _ = cache(dtype, g, 2, d, lens, 3)
+    K[lens[0] - 1] = what
+    out, lse = adakv.decode_attn(layer, q.abs() + 1.0, cu, 3, K, V, seg_len, want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0, :g]).all() and torch.isnan(lse[0, :g]).all()
+    assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
+
+
+@pytest.mark.parametrize("lens", [[250, 61], [1700, 40]], ids=["one_workgroup", "parts"])
+@pytest.mark.parametrize("dtype, g, d", [(BF, 4, 128), (FH, 8, 64)])
+def test_an_8_bit_step_whose_logits_are_all_minus_infinity(dtype, g, d, lens):
+    layer, cache8, cu, seg_len, _ = build(dtype, g, 2, d, lens, 4)
+    codes = cache8.K.view(torch.uint8)
+    codes[:lens[0], 5] = 0x38                     # 1
+    q = torch.zeros((1, 2 * g, d), dtype=dtype, device=DEV)
+    q[:, :, 5] = 1.0
+    q[:, :g, 5] = -float("inf")
+    q[:, :g, [c for c in range(d) if c != 5]] = 1.0
+    codes[:lens[0]][codes[:lens[0]] == 0x7f] = 0
+    out, lse = adakv.decode_attn_q8(layer, q, cu, 4, cache8, seg_len, want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0, :g]).all() and torch.isneginf(lse[0, :g]).all()
+    assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
