@@ -8,6 +8,7 @@
 // meet fp16 keys, all others bf16.  fp32 queries are three bf16 parts, the products of which are added in 32 bits.
 // 64 segments of 8192 rows on average, 64 query heads, d = 128, bf16: 27 us (4.8 TB/s) and 4.4 for the merge kernel (half as many rows in
 // 16 bits: 30 and 4.2).
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -340,7 +341,7 @@ __global__ __launch_bounds__((WHOLE ? 64 * WHOLE_WAVES<D, G> : 256)) void decode
       for (int j = 0; j < 8; ++j)
         if (16 * (j / 4) + 4 * lg + j % 4 > last) { sc[j] = -INFINITY; vv[j] = vword{0}; }
     }
-    const float cs = c_log2 * ks_now;
+    const float cs = fmaxf(c_log2 * ks_now, FLT_MIN);          // (0 times the -inf of a row past the end would be a NaN)
     float top = sc[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[j]);

@@ -71,3 +71,22 @@ def test_an_8_bit_step_whose_logits_are_all_minus_infinity(dtype, g, d, lens):
     torch.cuda.synchronize()
     assert torch.isnan(out[0, :g]).all() and torch.isneginf(lse[0, :g]).all()
     assert torch.isfinite(out[0, g:]).all() and torch.isfinite(lse[0, g:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FH, FS])
+@pytest.mark.parametrize("n", [7, 40])
+def test_an_8_bit_step_with_a_scale_next_to_zero(dtype, n):
+    """scale * 2^k of a block of zeros is below the fp32 range: all weights are alike, and rows past the end have none."""
+    layer = adakv.Layer(dtype, 2, 1, 64, 1, 7, 0.2, [n], [n], scale=1e-30)
+    cache8 = adakv.q8_cache(layer, 3, DEV)
+    cu, seg_len = torch.tensor([0, n], dtype=torch.int32, device=DEV), torch.tensor([n], dtype=torch.int32, device=DEV)
+    for s in cache8[2:]:
+        s.fill_(2.0 ** -60)
+    cache8.v_scale.fill_(1.0)
+    cache8.V.view(torch.uint8)[:n] = 0x38         # ones
+    q = torch.ones((1, 2, 64), dtype=dtype, device=DEV)
+    out, lse = adakv.decode_attn_q8(layer, q, cu, 3, cache8, seg_len, want_lse=True)
+    torch.cuda.synchronize()
+    assert (out == 1.0).all()
+    # (ln n by log2 and a multiplication: two roundings of log2, one of the constant and one of the product)
+    assert np.abs(f64(lse) - math.log(n)).max() <= 5 * 2.0 ** -24 * math.log(n)
