@@ -317,7 +317,8 @@ int adakv_decode_step(const adakv_layer *L, const void *q_new, const void *k_new
  * over the visible j: j <= r and (j > r - window or j < sinks).  row_lse[b][i][k] is the natural log of the
  * same sum of exp for row r = n_b + k, as adakv_score takes it.  Logits and sums are accumulated in
  * fp32; 16-bit layers round the softmax weights to their type for the second product.  Keys and
- * values that a row does not see have no part in its result, infinities and NaN included.
+ * values that a row does not see have no part in its result, infinities and NaN included.  Logits that are no finite
+ * numbers, or beyond 2^26: as for adakv_decode_attn.
  * Of L the call uses dtype, h_q, h_kv, d, w, batch, n, tok_off, scale and the strides.
  *
  *   q        (device) rows as K's; element (row, i, e) at row*q_stride_tok + i*q_stride_head + e, both

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
     }
   };
   auto store_lse = [&]() {
-    if (lse && r >= st.n[b] && half == 0) lse[r] = l == 0.0f ? -INFINITY : (m - BIAS<T> + log2f(l)) * LN2;
+    if (lse && r >= st.n[b] && half == 0) lse[r] = (m - BIAS<T> + log2f(l)) * LN2;
   };
 
   // Where something came out infinite or as NaN, a value that none should have seen may be the reason (a weight of 0 does not
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
       }
       l += other_half(l);
       if (wv % KS == 0 && w0 + l32 < n) {
-        store(o, cb, l == 0.0f ? 0.0f : 1.0f / l);
+        store(o, cb, 1.0f / l);
         if (cb == 0) store_lse();
       }
     }
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
   }
 
   if (w0 + l32 >= n) return;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const float inv = 1.0f / l;                                  // (a row sees itself: l is 0 where all its logits are -inf, 0 / 0)
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) store(acc[cb], cb, inv);
   store_lse();

@@ -90,3 +90,38 @@ def test_an_8_bit_step_with_a_scale_next_to_zero(dtype, n):
     assert (out == 1.0).all()
     # (ln n by log2 and a multiplication: two roundings of log2, one of the constant and one of the product)
     assert np.abs(f64(lse) - math.log(n)).max() <= 5 * 2.0 ** -24 * math.log(n)
+
+
+# ---- prompts -----------------------------------------------------------------------------------------------
+def prompt(dtype, h_q, h, d, lens, seed=0):
+    w = 2
+    layer = adakv.Layer(dtype, h_q, h, d, w, 7, 0.2, [n - w for n in lens], [w * h for _ in lens])
+    g = torch.Generator().manual_seed(seed)
+    return layer, *((torch.randn((sum(lens), k, d), generator=g) * f).to(dtype).to(DEV) for k, f in ((h_q, 2.0), (h, 1.0), (h, 1.0)))
+
+
+# query heads that make rows shared by four wavefronts, by two and by none
+SHARES = [(2, 260), (3, 260), (70, 260), (70, 500), (70, 1100)]
+
+
+@pytest.mark.parametrize("dtype, d", [(BF, 64), (BF, 128), (FH, 64), (FH, 128), (FS, 64), (FS, 128)])
+@pytest.mark.parametrize("h_q, n", SHARES[:4])
+def test_a_prompt_row_that_sees_infinite_keys_alone(dtype, d, h_q, n):
+    """Logits of -inf: weight 0 beside others, NaN and ln 0 where there are no others."""
+    layer, q, K, V = prompt(dtype, h_q, 1, d, [n])
+    q, at = q.abs() + 1.0, n - 1
+    window = 3
+    K[at - 1:] = -float("inf")                    # the last row sees n - 3 and these two, the one before n - 4, n - 3 and one
+    out, lse = adakv.window_attn(layer, q, K, V, window, want_lse=True)
+    torch.cuda.synchronize()
+    for hq in (0, h_q - 1):
+        for k, i in enumerate((n - 2, n - 1)):
+            see = np.arange(i - 2, n - 2)
+            ref, z, mag, big = S.attend(f64(q[i, hq]), f64(K[see, 0]), f64(V[see, 0]), 1 / math.sqrt(d))
+            keys = np.array(len(see))
+            assert_within(f64(out[i, hq]), ref, attention_bound(dtype, d, ref, mag, np.array(big), np.array(z), keys, rounded=True), f"row {i}")
+            assert_within(f64(lse[0, hq, k]), z, lse_bound(d, np.array(big), np.array(z), keys), f"lse {i}")
+    out, lse = adakv.window_attn(layer, q, K, V, 2, want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[n - 1].float()).all() and torch.isneginf(lse[0, :, 1]).all()
+    assert torch.isfinite(out[:n - 1].float()).all() and torch.isfinite(lse[0, :, 0]).all()
