@@ -141,12 +141,12 @@ template <typename T, int D, int KS> struct Step {
     return sc;
   }
 
-  // Weights against the reference m, and their sum.
-  static __device__ __forceinline__ Weights weights(const floatx16 &sc, float c_log2, float m, float &sum) {
+  // Weights against the reference m, and their sum; all of them times `by`.
+  static __device__ __forceinline__ Weights weights(const floatx16 &sc, float c_log2, float m, float &sum, float by = 1.0f) {
     float p[16], part[4];                      // (four sums: one after the other would be a chain of 16 additions)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_log2, BIAS<T> - m));
+      p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_log2, BIAS<T> - m)) * by;
       part[i % 4] = i < 4 ? p[i] : part[i % 4] + p[i];
     }
     sum = (part[0] + part[1]) + (part[2] + part[3]);
@@ -397,23 +397,41 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
     if (lse && r >= st.n[b] && half == 0) lse[r] = (m - BIAS<T> + log2f(l)) * LN2;
   };
 
+  l += other_half(l);
+
   // Where something came out infinite or as NaN, a value that none should have seen may be the reason (a weight of 0 does not
-  // cancel it): once more, 32 columns at a time, with a look at every value of the tiles that hold hidden keys.  (In the
-  // others every row sees every key.)
+  // cancel it), or values so large that their sum against the kept reference is beyond the type: once more, 32 columns at a
+  // time, with a look at every value of the tiles that hold hidden keys.  (In the others every row sees every key.)  The maximum
+  // and the sum of a row's weights are known by now and hold, so the weights are taken by their sum's power of two less: what is
+  // summed stays below the largest value.  (Not in fp16, whose values cannot sum up to the end of fp32 and whose weights would lose bits.)
   float worst = l * 0.0f;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) worst = fmaf(acc[cb][i], 0.0f, worst);
+    for (int i = 0; i < 16; ++i) worst = fmaf(acc[cb][i] * KS, 0.0f, worst);     // (KS such sums are added up below)
   const bool bad = __any(!(worst == 0.0f));
   if (lane == 0) sh_bad[wv] = bad;
   __syncthreads();
   if (sh_bad[0] | sh_bad[1] | sh_bad[2] | sh_bad[3]) {
+    if constexpr (KS > 1) {
+      float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(&shV[0][0]);
+      ml[wv][lane] = make_float2(m, l);
+      __syncthreads();
+      const float own = m;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) m = fmaxf(m, ml[wv / KS * KS + k][lane].x);
+      l *= __builtin_amdgcn_exp2f(own - m);
+#pragma unroll
+      for (int k = 1; k < KS; ++k) {
+        const float2 other = ml[wv / KS * KS + (wv + k) % KS][lane];
+        l += other.y * __builtin_amdgcn_exp2f(other.x - m);
+      }
+    }
+    const float by = is_f16<T> ? 1.0f : ldexpf(1.0f, -__builtin_amdgcn_frexp_expf(l)), inv = 1.0f / (l * by);
+    if (wv % KS == 0 && w0 + l32 < n) store_lse();
 #pragma nounroll
     for (int cb = 0; cb < CB; ++cb) {
       floatx16 o = floatx16{0};
-      m = M_INIT;
-      l = 0.0f;
       __syncthreads();
       load(0);
 #pragma nounroll
@@ -429,7 +447,8 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
           const u32x4 *values = shV[t % TL::TURNS] + kb * 32 * CH;
           floatx16 sc = S::logits(shK[t % TL::TURNS] + kb * 32 * CH, qf, here & 31, here >> 5);
           hide(sc, first, here >> 5);
-          const typename S::Weights w = weigh(sc, [&](float corr) { o *= corr; });
+          float sum;
+          const typename S::Weights w = S::weights(sc, sh.c_log2, m, sum, by);
           if (edge(j0)) {
             S::template add_block<true>(o, values, w, here, 0, cb);
             S::template add_block<true>(o, values, w, here, 1, cb);
@@ -443,15 +462,10 @@ __global__ __launch_bounds__(256, D == 128 ? (KS == 4 || (KS == 2 && T::SIZE == 
           }
         }
       }
-      l += other_half(l);
-      if (wv % KS == 0 && w0 + l32 < n) {
-        store(o, cb, 1.0f / l);
-        if (cb == 0) store_lse();
-      }
+      if (wv % KS == 0 && w0 + l32 < n) store(o, cb, inv);
     }
     return;
   }
-  l += other_half(l);
 
   if constexpr (KS > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place

@@ -1,4 +1,5 @@
-"""Attention where the numbers end: logits that are no numbers or infinite, rows that no weight is left for."""
+"""Attention where the numbers end: logits that are no numbers or infinite, rows that no weight is left for, values near the
+end of their type."""
 import math
 
 import numpy as np
@@ -125,3 +126,29 @@ def test_a_prompt_row_that_sees_infinite_keys_alone(dtype, d, h_q, n):
     torch.cuda.synchronize()
     assert torch.isnan(out[n - 1].float()).all() and torch.isneginf(lse[0, :, 1]).all()
     assert torch.isfinite(out[:n - 1].float()).all() and torch.isfinite(lse[0, :, 0]).all()
+
+
+@pytest.mark.parametrize("dtype, d", [(BF, 64), (BF, 128), (FS, 64), (FS, 128)])
+@pytest.mark.parametrize("h_q, n", SHARES)
+@pytest.mark.parametrize("hidden", [False, True])
+def test_prompt_values_near_the_end_of_their_type(dtype, d, h_q, n, hidden):
+    """Values from half the type's largest to all of it, of one sign or of both: a weighted mean of them is a number of the type.
+    `hidden`: beside a value that is none and that few rows see."""
+    layer, q, K, V = prompt(dtype, h_q, 1, d, [n])
+    top = torch.finfo(dtype).max
+    V = ((0.5 + 0.45 * torch.rand(V.shape, generator=torch.Generator().manual_seed(2))).to(DEV) * top).to(dtype)
+    V[:, :, 1::2] *= torch.where(torch.arange(n, device=DEV) % 3 == 0, -1.0, 1.0).to(dtype)[:, None, None]
+    window, sinks, at = (90, 3, 64) if hidden else (n, 0, n)
+    clean = V.clone()
+    if hidden:
+        V[at] = float("nan")
+    out, lse = adakv.window_attn(layer, q, K, V, window, sinks, want_lse=True)
+    torch.cuda.synchronize()
+    rows = np.array([i for i in range(n) if not at <= i < at + window])
+    assert torch.isnan(out[at:at + window].float()).all()
+    keys = np.array([S.visible(i, n, window, sinks).sum() for i in range(n)])
+    for hq in sorted({0, h_q - 1}):
+        ref, z, mag, big = S.prompt(f64(q[:, hq]), f64(K[:, 0]), f64(clean[:, 0]), window, sinks, 1 / math.sqrt(d))
+        bound = attention_bound(dtype, d, ref, mag, big, z, keys, rounded=True)
+        assert_within(f64(out[:, hq])[rows], ref[rows], bound[rows], f"head {hq}")
+        assert_within(f64(lse[0, hq]), z[n - 2:], lse_bound(d, big, z, keys)[n - 2:], f"lse {hq}")

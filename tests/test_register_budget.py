@@ -121,3 +121,15 @@ def test_no_scoring_kernel_spills(score_kernels, cut_kernels):
     """No scratch memory in any matrix-core scoring kernel."""
     for key, md in list(score_kernels.items()) + list(cut_kernels.items()):
         assert md["scratch"] == 0, (key, md)
+
+
+def test_no_prompt_attention_kernel_spills(metadata):
+    """The rare second sweep shares its registers with the tile loop: what it needs beyond them would be taken from that."""
+    ks = {}
+    for name, md in metadata.items():
+        m = re.search(r"window_attn_kernelI.*?(BF16|FP16|FP32)ELi(\d+)ELi(\d+)EE", name or "")
+        if m:
+            ks[m.group(1), int(m.group(2)), int(m.group(3))] = md
+    assert set(ks) == {(t, d, share) for t in ("BF16", "FP16", "FP32") for d in (64, 128) for share in (1, 2, 4)}
+    for key, md in ks.items():
+        assert md["scratch"] == 0, (key, md)
