@@ -320,17 +320,29 @@ def _stream(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
-def _zeros(shape, dtype, device, stream):
-    """Zeros that a call on `stream` writes over: cleared on that stream, not on the current one beside it."""
+def _made(make, shape, dtype, device, stream):
+    """A tensor that a call on `stream` writes: memory of that stream, which the current one, where the caller may read it,
+    is asked about before it is used again."""
     if stream is None:
-        return torch.zeros(shape, dtype=dtype, device=device)
+        return make(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.zeros(shape, dtype=dtype, device=device)
+        t = make(shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
 
 
-def _workspace(layer, ws):
+def _empty(shape, dtype, device, stream):
+    return _made(torch.empty, shape, dtype, device, stream)
+
+
+def _zeros(shape, dtype, device, stream):
+    return _made(torch.zeros, shape, dtype, device, stream)
+
+
+def _workspace(layer, ws, stream):
     if ws is None:
-        ws = torch.empty(max(workspace_bytes(layer), 16), dtype=torch.uint8, device="cuda")
+        ws = _empty(max(workspace_bytes(layer), 16), torch.uint8, "cuda", stream)
     _check_ws(ws)
     return ws, ws.data_ptr(), ws.numel()
 
@@ -342,9 +354,9 @@ def score(layer: Layer, q_window, K, row_lse=None, out=None, ws=None, stream=Non
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
     _need(row_lse, layer.batch * layer.h_q * layer.w, "row_lse")
     if out is None:
-        out = torch.empty(layer._scores, dtype=torch.float32, device=K.device)
+        out = _empty(layer._scores, torch.float32, K.device, stream)
     _need(out, layer._scores, "scores")
-    ws, wp, wn = _workspace(layer, ws)
+    ws, wp, wn = _workspace(layer, ws, stream)
     st = lib.adakv_score(ctypes.byref(layer.c), _ptr(q_window, "q_window", layer.torch_dtype),
                          _ptr(K, "K", layer.torch_dtype), _ptr(row_lse, "row_lse", torch.float32),
                          _ptr(out, "scores", torch.float32), wp, wn, _stream(stream))
@@ -357,13 +369,13 @@ def allocate(layer: Layer, scores, budgets=None, cu_seqlens=None, ws=None, strea
     """adakv_allocate: budgets [batch*h_kv] and cu_seqlens [batch*h_kv+1], int32."""
     lib = load_library()
     if budgets is None:
-        budgets = torch.empty(layer._segments, dtype=torch.int32, device=scores.device)
+        budgets = _empty(layer._segments, torch.int32, scores.device, stream)
     if cu_seqlens is None:
-        cu_seqlens = torch.empty(layer._segments + 1, dtype=torch.int32, device=scores.device)
+        cu_seqlens = _empty(layer._segments + 1, torch.int32, scores.device, stream)
     _need(scores, layer._scores, "scores")
     _need(budgets, layer._segments, "budgets")
     _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
-    ws, wp, wn = _workspace(layer, ws)
+    ws, wp, wn = _workspace(layer, ws, stream)
     st = lib.adakv_allocate(ctypes.byref(layer.c), _ptr(scores, "scores", torch.float32),
                             _ptr(budgets, "budgets", torch.int32),
                             _ptr(cu_seqlens, "cu_seqlens", torch.int32), wp, wn, _stream(stream))
@@ -376,12 +388,12 @@ def select(layer: Layer, scores, budgets, cu_seqlens, indices=None, ws=None, str
     """adakv_select: retained positions [sum_b B_b] int32, flattened by (sequence, head)."""
     lib = load_library()
     if indices is None:
-        indices = torch.empty(layer._rows_out, dtype=torch.int32, device=scores.device)
+        indices = _empty(layer._rows_out, torch.int32, scores.device, stream)
     _need(scores, layer._scores, "scores")
     _need(budgets, layer._segments, "budgets")
     _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
     _need(indices, layer._rows_out, "indices")
-    ws, wp, wn = _workspace(layer, ws)
+    ws, wp, wn = _workspace(layer, ws, stream)
     st = lib.adakv_select(ctypes.byref(layer.c), _ptr(scores, "scores", torch.float32),
                           _ptr(budgets, "budgets", torch.int32),
                           _ptr(cu_seqlens, "cu_seqlens", torch.int32),
@@ -395,9 +407,9 @@ def compact(layer: Layer, K, V, indices, cu_seqlens, K_out=None, V_out=None, str
     """adakv_compact: K_out, V_out [sum_b B_b, d] in the layer's dtype."""
     lib = load_library()
     if K_out is None:
-        K_out = torch.empty((layer._rows_out, layer.d), dtype=layer.torch_dtype, device=K.device)
+        K_out = _empty((layer._rows_out, layer.d), layer.torch_dtype, K.device, stream)
     if V_out is None:
-        V_out = torch.empty((layer._rows_out, layer.d), dtype=layer.torch_dtype, device=K.device)
+        V_out = _empty((layer._rows_out, layer.d), layer.torch_dtype, K.device, stream)
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
     _check_kv(layer, V, "V", layer.v_strides, layer.strides_given[1])
     _need(indices, layer._rows_out, "indices")
@@ -422,7 +434,7 @@ def compress(layer: Layer, q_window, K, V, row_lse=None, ws=None, stream=None, b
     b = bufs or {}
     dev = K.device
     if ws is None:
-        ws = torch.empty(max(workspace_bytes(layer), 16), dtype=torch.uint8, device=dev)
+        ws = _empty(max(workspace_bytes(layer), 16), torch.uint8, dev, stream)
     if not pipeline:
         sc = score(layer, q_window, K, row_lse=row_lse, out=b.get("scores"), ws=ws, stream=stream)
         bud, cu = allocate(layer, sc, b.get("budgets"), b.get("cu_seqlens"), ws=ws, stream=stream)
@@ -437,7 +449,7 @@ def compress(layer: Layer, q_window, K, V, row_lse=None, ws=None, stream=None, b
 
     def buf(name, shape, dtype):
         t = b.get(name)
-        return t if t is not None else torch.empty(shape, dtype=dtype, device=dev)
+        return t if t is not None else _empty(shape, dtype, dev, stream)
 
     sc = buf("scores", layer._scores, torch.float32)
     bud = buf("budgets", layer._segments, torch.int32)
@@ -483,7 +495,7 @@ def compress_static(layer: Layer, q_window, K, V, row_lse=None, stream=None, buf
     out = {}
     for name, numel, shape, dtype in want:
         t = b.get(name)
-        out[name] = t if t is not None else torch.empty(shape, dtype=dtype, device=dev)
+        out[name] = t if t is not None else _empty(shape, dtype, dev, stream)
         _need(out[name], numel, name)
     st = lib.adakv_compress_static(
         ctypes.byref(layer.c), _ptr(q_window, "q_window", layer.torch_dtype),
@@ -524,7 +536,7 @@ def probe_read(src, sink=None, stream=None):
     if not src.is_contiguous():
         raise ValueError("src must be contiguous")
     if sink is None:
-        sink = torch.empty(PROBE_SINK_BYTES, dtype=torch.uint8, device=src.device)
+        sink = _empty(PROBE_SINK_BYTES, torch.uint8, src.device, stream)
     if sink.numel() * sink.element_size() < PROBE_SINK_BYTES or not sink.is_contiguous():
         raise ValueError("sink too small")
     st = load_library().adakv_probe_read(_ptr(src, "src"), src.numel() * src.element_size(),
@@ -567,11 +579,11 @@ def cache_build(layer: Layer, K, V, indices, cu_seqlens, headroom, K_cache=None,
     lib = load_library()
     rows = cache_rows(layer, headroom)
     if K_cache is None:
-        K_cache = torch.empty((rows, layer.d), dtype=layer.torch_dtype, device=K.device)
+        K_cache = _empty((rows, layer.d), layer.torch_dtype, K.device, stream)
     if V_cache is None:
-        V_cache = torch.empty((rows, layer.d), dtype=layer.torch_dtype, device=K.device)
+        V_cache = _empty((rows, layer.d), layer.torch_dtype, K.device, stream)
     if seg_len is None:
-        seg_len = torch.empty(layer._segments, dtype=torch.int32, device=K.device)
+        seg_len = _empty(layer._segments, torch.int32, K.device, stream)
     if K_cache.shape[0] < rows or V_cache.shape[0] < rows or seg_len.numel() < layer._segments:
         raise ValueError("cache or seg_len too small for this layer and head-room")
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
@@ -632,12 +644,11 @@ def decode_attn(layer: Layer, q_new, cu_seqlens, headroom, K_cache, V_cache, seg
     if K_cache.size(0) < rows or V_cache.size(0) < rows:
         raise ValueError("cache too small for this layer and head-room")
     if out is None:
-        out = torch.empty(want, dtype=torch.float32, device=q_new.device)
+        out = _empty(want, torch.float32, q_new.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(want[:2], dtype=torch.float32, device=q_new.device)
+        lse = _empty(want[:2], torch.float32, q_new.device, stream)
     if ws is None:
-        ws = torch.empty(max(decode_workspace_bytes(layer, headroom), 16), dtype=torch.uint8,
-                         device=q_new.device)
+        ws = _empty(max(decode_workspace_bytes(layer, headroom), 16), torch.uint8, q_new.device, stream)
     _check_decode_bufs(layer, headroom, K_cache, V_cache, cu_seqlens, seg_len, out, lse, ws)
     if window is not None:
         _one_device(stream, q_new=q_new, cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len, out=out, lse=lse, ws=ws)
@@ -686,12 +697,11 @@ def decode_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, K_cache
     if K_cache.size(0) < rows or V_cache.size(0) < rows:
         raise ValueError("cache too small for this layer and head-room")
     if out is None:
-        out = torch.empty(want, dtype=torch.float32, device=q_new.device)
+        out = _empty(want, torch.float32, q_new.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(want[:2], dtype=torch.float32, device=q_new.device)
+        lse = _empty(want[:2], torch.float32, q_new.device, stream)
     if ws is None:
-        ws = torch.empty(max(decode_workspace_bytes(layer, headroom), 16), dtype=torch.uint8,
-                         device=q_new.device)
+        ws = _empty(max(decode_workspace_bytes(layer, headroom), 16), torch.uint8, q_new.device, stream)
     _check_decode_bufs(layer, headroom, K_cache, V_cache, cu_seqlens, seg_len, out, lse, ws)
     _need(overflow, 1, "overflow")
     if window is not None:
@@ -766,7 +776,7 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     if out is None:
         out = _zeros((q.shape[0], layer.h_q, layer.d), layer.torch_dtype, q.device, stream)
     if row_lse is None and want_lse:
-        row_lse = torch.empty((layer.batch, layer.h_q, layer.w), dtype=torch.float32, device=q.device)
+        row_lse = _empty((layer.batch, layer.h_q, layer.w), torch.float32, q.device, stream)
     _need(out, rows * layer.h_q * layer.d, "out")
     _need(row_lse, layer.batch * layer.h_q * layer.w, "row_lse")
     dt = layer.torch_dtype
@@ -832,7 +842,7 @@ def cache_build_q8(layer: Layer, K, V, indices, cu_seqlens, headroom, cache=None
     if cache is None:
         cache = q8_cache(layer, headroom, K.device, stream)
     if seg_len is None:
-        seg_len = torch.empty(layer._segments, dtype=torch.int32, device=K.device)
+        seg_len = _empty(layer._segments, torch.int32, K.device, stream)
     _check_kv(layer, K, "K", layer.k_strides, layer.strides_given[0])
     _check_kv(layer, V, "V", layer.v_strides, layer.strides_given[1])
     _need(indices, layer._rows_out, "indices")
@@ -876,11 +886,11 @@ def _decode_q8(name, layer, q_new, new, cu_seqlens, headroom, cache, seg_len, ov
         _check_new(layer, *new)
         _need(over[0], 1, "overflow")
     if out is None:
-        out = torch.empty(want, dtype=torch.float32, device=q_new.device)
+        out = _empty(want, torch.float32, q_new.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(want[:2], dtype=torch.float32, device=q_new.device)
+        lse = _empty(want[:2], torch.float32, q_new.device, stream)
     if ws is None:
-        ws = torch.empty(max(decode_workspace_bytes(layer, headroom), 16), dtype=torch.uint8, device=q_new.device)
+        ws = _empty(max(decode_workspace_bytes(layer, headroom), 16), torch.uint8, q_new.device, stream)
     at, named = _q8_ptrs(layer, headroom, cache)
     _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
     _need(seg_len, layer._segments, "seg_len")
@@ -922,9 +932,9 @@ def _move(name, layer, picks, cu_seqlens, headroom, src, seg_len, headroom_out, 
     _need(overflow, 1, "overflow")
     dev = cu_seqlens.device
     if cu_out is None:
-        cu_out = torch.empty(to._segments + 1, dtype=torch.int32, device=dev)
+        cu_out = _empty(to._segments + 1, torch.int32, dev, stream)
     if len_out is None:
-        len_out = torch.empty(to._segments, dtype=torch.int32, device=dev)
+        len_out = _empty(to._segments, torch.int32, dev, stream)
     _need(cu_out, to._segments + 1, "cu_out")
     _need(len_out, to._segments, "len_out")
     (at, named), (at_out, named_out) = src(layer, headroom), dst(to, headroom_out)
