@@ -169,13 +169,14 @@ template <typename F> PyObject *checked(const char *name, Py_ssize_t n, Py_ssize
   }
 }
 
-// A call of the library without the interpreter's lock.
+// A call of the library without the interpreter's lock, which is back however the call ends.  `f` asks no tensor for anything:
+// what a tensor says may be an exception.
 template <typename F> int unlocked(F &&f) {
-  int st;
-  Py_BEGIN_ALLOW_THREADS
-  st = f();
-  Py_END_ALLOW_THREADS
-  return st;
+  struct Unlock {
+    PyThreadState *state = PyEval_SaveThread();
+    ~Unlock() { PyEval_RestoreThread(state); }
+  } unlock;
+  return f();
 }
 
 // (device, function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, window, sinks, out, lse, ws, stream)
@@ -192,8 +193,9 @@ PyObject *decode_window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int32_t window = x.i32(1), sinks = x.i32();
     float *out = x.data<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->d), *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q);
     const at::Tensor &ws = x.buffer(at::kByte, 0);
+    const size_t ws_bytes = (size_t)ws.numel();
     void *p = ws.data_ptr(), *stream = x.pointer();
-    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, len, over, window, sinks, out, lse, p, (size_t)ws.numel(), stream); });
+    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, len, over, window, sinks, out, lse, p, ws_bytes, stream); });
   });
 }
 
@@ -212,8 +214,9 @@ PyObject *decode_step_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int32_t *len = x.data<int32_t>(at::kInt, l.nseg), *over = x.data_or_none<int32_t>(at::kInt, 1);
     float *out = x.data<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->d), *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q);
     const at::Tensor &ws = x.buffer(at::kByte, 0);
+    const size_t ws_bytes = (size_t)ws.numel();
     void *p = ws.data_ptr(), *stream = x.pointer();
-    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, ks, vs, len, over, out, lse, p, (size_t)ws.numel(), stream); });
+    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, ks, vs, len, over, out, lse, p, ws_bytes, stream); });
   });
 }
 
@@ -252,7 +255,9 @@ PyObject *window_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *out = x.data<void>(l.type, tokens * L->h_q * L->d);
     float *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->w);
     void *stream = x.pointer();
-    return unlocked([&] { return fn(L, q.data_ptr(), q.stride(0), q.stride(1), K, V, window, sinks, out, lse, stream); });
+    const int64_t q_tok = q.stride(0), q_head = q.stride(1);
+    void *qp = q.data_ptr();
+    return unlocked([&] { return fn(L, qp, q_tok, q_head, K, V, window, sinks, out, lse, stream); });
   });
 }
 
