@@ -327,8 +327,8 @@ int adakv_decode_step(const adakv_layer *L, const void *q_new, const void *k_new
  *   out      (device) [rows][h_q][d] contiguous, L->dtype, 16-byte aligned, no part of q, K or V; rows of no
  *                     sequence stay as they are
  *   row_lse  (device) [batch][h_q][w] fp32, written; may be NULL
- * Supported (else ADAKV_EUNSUPPORTED): up to 2^28 rows a sequence; rows of K and of V less than 16 MiB apart; at most 2^32 rows times query heads in
- * all, each sequence's rows counted in 64s.
+ * Supported (else ADAKV_EUNSUPPORTED): up to 2^28 rows a sequence; rows of K and of V less than 16 MiB apart;
+ * fewer than 2^31 rows times query heads in all, each sequence's rows rounded up to a multiple of 128.
  */
 int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
                       int64_t q_stride_head, const void *K, const void *V, int32_t window,

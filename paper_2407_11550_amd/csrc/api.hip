@@ -402,19 +402,20 @@ int adakv_window_attn(const adakv_layer *L, const void *q, int64_t q_stride_tok,
   int rc = build_tables(L, st, dm);
   if (rc != ADAKV_OK) return rc;
   if (window < 1 || sinks < 0 || q_stride_tok < L->d || q_stride_head < L->d) return ADAKV_EINVAL;
+  // a launch holds fewer than 2^32 threads: workgroups of 256, one for 128 rows of a head (sharing is for few)
+  long long blocks = 0;
+  for (int b = 0; b < st.batch; ++b) {
+    const long long rows = (long long)st.n[b] + dm.w;
+    if (rows > (1 << 28)) return ADAKV_EUNSUPPORTED;
+    blocks += (rows + 127) / 128;
+  }
+  if (blocks * dm.h_q >= (1 << 24)) return ADAKV_EUNSUPPORTED;
   if (!q || !K || !V || !out) return ADAKV_EINVAL;
   const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
   if (q_stride_tok * esz % 16 != 0 || q_stride_head * esz % 16 != 0) return ADAKV_EUNSUPPORTED;
   if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return ADAKV_EUNSUPPORTED;
   // (a tile has up to 128 rows, whose offsets are below 2^31)
   if (L->k_stride_tok >= (1 << 24) / esz || L->v_stride_tok >= (1 << 24) / esz) return ADAKV_EUNSUPPORTED;
-  long long blocks = 0;
-  for (int b = 0; b < st.batch; ++b) {
-    const long long rows = (long long)st.n[b] + dm.w;
-    if (rows > (1 << 28)) return ADAKV_EUNSUPPORTED;
-    blocks += (rows + 63) / 64;
-  }
-  if (blocks * dm.h_q > (1 << 20) * 64ll) return ADAKV_EUNSUPPORTED;
   hipError_t e = launch_window_attn(st, dm, L->dtype, q, q_stride_tok, q_stride_head, K, V, window, sinks, out, row_lse,
                                     (hipStream_t)hip_stream);
   return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
