@@ -369,7 +369,8 @@ int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void
 /* Floats in k_scale and in v_scale (0 on invalid input). */
 size_t adakv_q8_scales(const adakv_layer *L, int32_t headroom);
 
-/* adakv_cache_build into an 8-bit cache.  Arguments as there; K_q8, V_q8 16-byte aligned. */
+/* adakv_cache_build into an 8-bit cache.  Arguments as there; K_q8, V_q8 16-byte aligned.  At most
+ * 10^9 retained rows (else ADAKV_EUNSUPPORTED). */
 int adakv_cache_build_q8(const adakv_layer *L, const void *K, const void *V,
                          const int32_t *indices, const int32_t *cu_seqlens, int32_t headroom,
                          void *K_q8, void *V_q8, float *k_scale, float *v_scale, int32_t *seg_len,

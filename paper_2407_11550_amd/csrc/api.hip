@@ -475,6 +475,8 @@ int adakv_cache_build_q8(const adakv_layer *L, const void *K, const void *V,
   int rc = build_tables(L, st, dm);
   if (rc != ADAKV_OK) return rc;
   if ((rc = check_headroom(st, dm, headroom)) != ADAKV_OK) return rc;
+  // a launch holds fewer than 2^32 threads: workgroups of 256 for two blocks
+  if (st.out_off[st.batch] > 1000000000) return ADAKV_EUNSUPPORTED;
   if (!K || !V || !indices || !cu_seqlens || !K_q8 || !V_q8 || !k_scale || !v_scale || !seg_len) return ADAKV_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(K_q8) || !aligned16(V_q8)) return ADAKV_EUNSUPPORTED;
   hipError_t e = launch_cache_build_q8(st, dm, L->dtype, K, V, indices, cu_seqlens, headroom,

@@ -25,3 +25,9 @@ def test_prompts_fit_into_one_launch(lib, h_q, rows, status):
     layer = adakv.Layer(torch.bfloat16, h_q, 1, 64, w, 7, 0.2, [n - w for n in rows], [w for _ in rows])
     got = lib.adakv_window_attn(ctypes.byref(layer.c), None, 64 * h_q, 64, ONE, ONE, 16, 0, ONE, None, None)
     assert got == status
+
+
+@pytest.mark.parametrize("rows, status", [(10 ** 9, -1), (10 ** 9 + 1, -2)])
+def test_an_8_bit_cache_is_built_by_one_launch(lib, rows, status):
+    layer = adakv.Layer(torch.bfloat16, 8, 8, 64, 1, 7, 0.2, [130_000_000], [rows])
+    assert lib.adakv_cache_build_q8(ctypes.byref(layer.c), None, ONE, ONE, ONE, 0, ONE, ONE, ONE, ONE, ONE, None) == status
