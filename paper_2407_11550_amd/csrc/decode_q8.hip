@@ -68,9 +68,9 @@ __global__ __launch_bounds__(256) void cache_build_q8_kernel(
     if (cu[mid] / Q8_BLOCK + mid <= i) lo = mid; else hi = mid;
   }
   const int s = lo, from = min(max(cu[s], 0), rows_total), len = min(cu[s + 1], rows_total) - from;
-  const int blk = i - (cu[s] / Q8_BLOCK + s), t0 = blk * Q8_BLOCK;
+  const int blk = i - (from / Q8_BLOCK + s), t0 = blk * Q8_BLOCK;
   if (blk == 0 && !values && lane == 0 && seg_len) seg_len[s] = max(len, 0);
-  if (t0 >= len) return;
+  if (t0 < 0 || t0 >= len) return;             // (below 0: offsets that do not begin with 0)
   const int b = s / h, c = s % h, col = lane % LPR, slot = lane / LPR;
   const char *src = (values ? V + c * v_head : K + c * k_head) + col * 16;
   const long long stride = values ? v_tok : k_tok;

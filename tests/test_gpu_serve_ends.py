@@ -93,6 +93,26 @@ def test_an_8_bit_step_with_a_scale_next_to_zero(dtype, n):
     assert np.abs(f64(lse) - math.log(n)).max() <= 5 * 2.0 ** -24 * math.log(n)
 
 
+@pytest.mark.parametrize("cu", [[1 << 20, 40, 70], [40, 10, 70], [0, 1 << 20, 70], [-(1 << 31), 40, 70], [33, 40, 1 << 20], [0, -70, 70], [70, 70, 0]], ids=str)
+def test_an_8_bit_build_stays_inside_with_corrupt_offsets(cu):
+    """Offsets that are no running sum: nothing around the cache, its scales and the lengths is written."""
+    print(cu, flush=True)
+    h, hr, w, d, rows = 2, 5, 2, 64, 70
+    layer = adakv.Layer(BF, h, h, d, w, 7, 0.2, [98], [rows])
+    K = torch.randn((100, h, d), device=DEV).to(BF)
+    idx = torch.arange(rows, dtype=torch.int32, device=DEV)
+    held, scales, pad = adakv.cache_rows(layer, hr), adakv.q8_scales(layer, hr), 4096
+    big = [torch.full((held + 2 * pad, d), 0x55, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    big += [torch.full((scales + 2 * pad,), 7.0, device=DEV) for _ in range(2)]
+    lens = torch.full((h + 2 * pad,), 7, dtype=torch.int32, device=DEV)
+    inside = [t[pad:len(t) - pad] for t in big]
+    cache8 = adakv.Q8Cache(*(t.view(torch.float8_e4m3fn) for t in inside[:2]), *inside[2:])
+    adakv.cache_build_q8(layer, K, K, idx, torch.tensor(cu, dtype=torch.int32, device=DEV), hr, cache8, lens[pad:pad + h])
+    torch.cuda.synchronize()
+    for t, fill in zip((*big, lens), (0x55, 0x55, 7, 7, 7)):
+        assert (t[:pad] == fill).all() and (t[-pad:] == fill).all()
+
+
 # ---- prompts -----------------------------------------------------------------------------------------------
 def prompt(dtype, h_q, h, d, lens, seed=0):
     w = 2
