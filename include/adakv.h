@@ -411,7 +411,8 @@ int adakv_decode_step_q8(const adakv_layer *L, const void *q_new, const void *k_
  *
  *     cu_out[i*h_kv + c + 1] - cu_out[i*h_kv + c] = cu_seqlens[s + 1] - cu_seqlens[s],  s = from[i]*h_kv + c
  *     len_out[i*h_kv + c] = min(seg_len[s], capacity there); if that is less than seg_len[s], the rows behind
- *                           are left out and *overflow is set to 1 (it is never cleared)
+ *                           are left out and *overflow is set to 1 (it is never cleared).  A length below 0 counts as
+ *                           0; one beyond the capacity in the source moves as many rows as that, and sets *overflow
  *
  * Rows that no segment holds are not written.  Source and destination must not overlap (ADAKV_EINVAL).
  *

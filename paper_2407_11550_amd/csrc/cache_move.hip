@@ -40,8 +40,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(
   // a segment a lane; offsets are clamped into the sequence, so that corrupt ones cannot leave the buffers
   const int c_l = min(lane, h - 1);
   const int at_l = min(max(cu[b * h + c_l] - src_row, 0), rows), end_l = min(max(cu[b * h + c_l + 1] - src_row, at_l), rows);
-  const int held_l = min(max(seg_len[b * h + c_l], 0), end_l - at_l + headroom);
-  const int fit_l = min(held_l, end_l - at_l + headroom_out);
+  const int held_l = max(seg_len[b * h + c_l], 0);         // (a corrupt length: no more rows than the source has)
+  const int fit_l = min(held_l, end_l - at_l + min(headroom, headroom_out));
   if (k == 0 && !values && tid < h) {
     for (int d = d0; d < d1; ++d) {
       cu_out[mt.to[d] * h + tid] = mt.dst_row[d] + at_l;
