@@ -547,9 +547,10 @@ hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const
     share = reach <= 64 ? (wgs <= 256 ? 2 : 1) : wgs <= (even ? 64 : 128) ? 4 : wgs <= (even ? 192 : 384) * by_d ? 2 : 1;
   if (share > 1) ct = chunks(128 / share);
   const dim3 grid((unsigned)((long long)ct.off[st.batch] * dm.h_q));
+  // (a trace's name tells how many wavefronts share rows)
 #define ADAKV_WINDOW_KS(T, D, KS)                                                                                           \
-  ADAKV_LAUNCH("window_attn", (window_attn_kernel<T, D, KS>), grid, dim3(256), s, st, ct, sh, (const char *)q, (const char *)K, \
-               (const char *)V, (char *)out, row_lse)
+  ADAKV_LAUNCH(KS == 1 ? "window_attn" : KS == 2 ? "window_attn_2" : "window_attn_4", (window_attn_kernel<T, D, KS>), grid,   \
+               dim3(256), s, st, ct, sh, (const char *)q, (const char *)K, (const char *)V, (char *)out, row_lse)
 #define ADAKV_WINDOW(T, D)                                                                                                  \
   do {                                                                                                                      \
     if (share == 4) ADAKV_WINDOW_KS(T, D, 4);                                                                               \
