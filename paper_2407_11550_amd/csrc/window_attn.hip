@@ -9,9 +9,10 @@
 //
 // 4 d flops per visible pair: bound by the matrix instructions, whose operands a wavefront of 32 rows reads from LDS at nearly the
 // rate that LDS has (1 KB a matrix instruction: 124 of 128 bytes a clock when those follow one another), with much vector work
-// beside them.  16384 tokens, all visible, 32 heads over 8, d = 128, bf16: 2.0 to 2.1 ms, 1050 to 1100 TFLOP/s
-// (a library product of 8192^3 1130 to 1400); without reading operands it would be 1.64 ms, without loading tiles either 1.26.
-// 64 rows a wavefront would read half as much, but leave one wavefront per SIMD: 2.6 ms.  d = 64: vector work, 650 TFLOP/s.
+// beside them and, in every tile, a wait for the next one's loads (load_to_lds).  16384 tokens, all visible, 32 heads over 8,
+// d = 128, bf16: 2.09 to 2.14 ms in a row, 1030 to 1050 TFLOP/s, 2.25 on average with pauses (a library product of 8192^3 1130 to 1400);
+// without reading operands it would be 1.64 ms, without loading tiles 1.77, without either 1.26.  64 rows a wavefront read half as
+// much, but leave one wavefront per SIMD: 2.6 ms.  d = 64: vector work and the same wait, 620 TFLOP/s.
 #include <math.h>
 
 #include <type_traits>
@@ -74,6 +75,9 @@ __device__ __forceinline__ float other_half(float x) {
 // 64 x 16 bytes from base + at + the lane's off, straight into 1 KB of LDS, behind the compiler's back: the tiles take
 // turns in LDS, and it would wait for every load before it reads any.  (In front of the load stand the wait states that
 // follow a write of m0, one, and a scalar register's write by the vector unit, five.)
+// The next tile's loads do not run beside the whole of this tile's work, though: the compiler keeps the waits for the queries,
+// which are loaded in front of the loop and first used in it, between the first products of every tile, and by then they are
+// waits for the loads just asked for.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"        // m0 among the clobbers
 __device__ __forceinline__ void load_to_lds(const char *base, unsigned off, unsigned at, const u32x4 *dst) {
