@@ -388,7 +388,8 @@ int adakv_append_q8(const adakv_layer *L, const void *k_new, const void *v_new,
 
 /*
  * adakv_decode_attn and adakv_decode_step over an 8-bit cache: the attention of q_new over the values
- * that the cache stands for, accumulated in fp32 (the appended row is attended as it was stored).
+ * that the cache stands for, accumulated in fp32 (the appended row is attended as it was stored).  Logits that are
+ * no finite numbers: as for adakv_decode_attn.
  *   ws (device) adakv_decode_workspace_bytes(L, headroom) bytes
  */
 int adakv_decode_attn_q8(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
