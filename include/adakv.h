@@ -351,6 +351,83 @@ int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void
                              size_t ws_bytes, void *hip_stream);
 
 /*
+ * ---- Rotary positions, and norms of the heads ---------------------------------------------------
+ *
+ * What stands between the projections and the calls above: the queries and keys of a prompt, or of the
+ * new tokens of a batch, turned by their positions.  (A compressed segment's length is no position, so a
+ * token's position is an argument.)
+ */
+
+typedef enum { ADAKV_ROTARY_HALF = 0, ADAKV_ROTARY_INTERLEAVED = 1 } adakv_rotary_layout;
+typedef enum { ADAKV_ROTARY_PLAIN = 0, ADAKV_ROTARY_LINEAR = 1, ADAKV_ROTARY_BASE = 2, ADAKV_ROTARY_PARTS = 3 } adakv_rotary_scaling;
+
+/* Pair i < dims/2 of a head are its elements i and i + dims/2 (HALF) or 2i and 2i + 1 (INTERLEAVED); its elements from dims on
+ * belong to no pair. */
+typedef struct {
+  int32_t layout;           /* adakv_rotary_layout                                             */
+  int32_t dims;             /* even, 0 <= dims <= d; 0: nothing is turned                      */
+  float magnitude;          /* factor of the elements that are turned; 0 means 1               */
+  const double *freq;       /* (device) [dims/2] radians a position; may be NULL if dims is 0  */
+} adakv_rotation;
+
+/* Rows of heads: element (row, i, e) at row*stride_tok + i*stride_head + e of x.  Both strides >= d; rows 16-byte aligned. */
+typedef struct {
+  void *x;                  /* (device) L->dtype                                               */
+  int64_t stride_tok, stride_head;
+} adakv_heads;
+
+/*
+ * Frequencies, on the host and in 64 bits: freq[i] = base^(-2i/dims), and for contexts `factor` times as long
+ *     LINEAR   freq[i] / factor
+ *     BASE     those of the base  base * factor^(dims/(dims-2))  (dims = 2: the one frequency is 1)
+ *     PARTS    freq[i] * (u + (1 - u)/factor),  u = (original_len * freq[i] / (2 pi) - low) / (high - low) held to 0..1: what
+ *              turns `high` times within the original length and more keeps its frequency, what turns `low` times or less is as with
+ *              LINEAR (with such a schedule a magnitude of 1 + 0.1 ln(factor) is usual)
+ *   freq (host) [dims/2], written
+ * Returns ADAKV_EINVAL for a NULL freq, dims odd or below 2, a base not above 0, an unknown scaling, and where the scaling uses them, factor < 1,
+ * original_len < 1, low < 0 or high <= low; also for
+ * numbers that are not finite, the stretched base among them.  ADAKV_EUNSUPPORTED for dims > 128.
+ */
+int adakv_rotary_frequencies(int32_t dims, double base, int32_t scaling, double factor,
+                             int32_t original_len, double low, double high, double *freq);
+
+/*
+ * Every row of q and k turned by its position p: with t = p * freq[i] and m the magnitude, the elements a, b of pair i become
+ *
+ *     m (a cos t - b sin t),  m (b cos t + a sin t);
+ *
+ * the others stay.  In fp32 but for the angles, which are made in 64 bits; the result is rounded once.  Turning with the frequencies'
+ * negatives takes it back.
+ * Of L the call uses dtype, h_q, h_kv, d, and without positions also w, batch, n and tok_off.
+ *
+ *   positions    (device) [rows] int32: row r of q and k is at positions[r]; a row with one below 0 is left out (its
+ *                         rows of the outputs stay as they are).  NULL: the rows of L's sequences, each counted from its sequence's
+ *                         first; `rows` is not looked at, rows of no sequence stay as they are
+ *   q, q_out     (host)   [rows][h_q][d]; both NULL: only k is turned
+ *   k, k_out     (host)   [rows][h_kv][d]; both NULL: only q is turned.  (k_out with L's strides of K is what adakv_score and
+ *                         adakv_window_attn read)
+ * An output may be its own input, at the same address and with the same strides (else ADAKV_EINVAL); no other element of
+ * an output may be one of an input, or of another place of an output: either a token's heads lie within stride_tok, or a head's tokens
+ * within stride_head (else ADAKV_EINVAL).
+ * Supported (else ADAKV_EUNSUPPORTED): up to 2^30 rows in all.
+ */
+int adakv_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows,
+                 const int32_t *positions, const adakv_heads *q, const adakv_heads *k,
+                 const adakv_heads *q_out, const adakv_heads *k_out, void *hip_stream);
+
+/*
+ * The same behind a norm of every head: x / sqrt(mean of the squares of its d elements + eps), times a weight for each element,
+ * is what is turned.  Squares are summed in fp32: elements of 2^60 and more may give zeros or NaN, as a head of zeros does with eps = 0.
+ *
+ *   q_weight, k_weight (device) [d] L->dtype, 16-byte aligned; each may be NULL if its q or k is
+ *   eps                >= 0 and finite (else ADAKV_EINVAL)
+ */
+int adakv_norm_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows,
+                      const int32_t *positions, const adakv_heads *q, const adakv_heads *k,
+                      const void *q_weight, const void *k_weight, float eps,
+                      const adakv_heads *q_out, const adakv_heads *k_out, void *hip_stream);
+
+/*
  * ---- The decode-side cache in 8 bits ----------------------------------------------------------
  *
  * K_q8 and V_q8 have the layout of K_cache and V_cache with one byte an element: an e4m3 number (the

@@ -48,6 +48,14 @@ class _CLayer(ctypes.Structure):
     ]
 
 
+class _CRotation(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("dims", ctypes.c_int32), ("magnitude", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+
+class _CHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("stride_tok", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -99,6 +107,12 @@ def load_library():
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args
+    RP, HP = ctypes.POINTER(_CRotation), ctypes.POINTER(_CHeads)
+    lib.adakv_rotary.restype = lib.adakv_norm_rotary.restype = lib.adakv_rotary_frequencies.restype = ctypes.c_int
+    lib.adakv_rotary.argtypes = [P, RP, L64, V, HP, HP, HP, HP, V]
+    lib.adakv_norm_rotary.argtypes = [P, RP, L64, V, HP, HP, V, V, ctypes.c_float, HP, HP, V]
+    lib.adakv_rotary_frequencies.argtypes = [I, ctypes.c_double, I, ctypes.c_double, I, ctypes.c_double, ctypes.c_double,
+                                             ctypes.POINTER(ctypes.c_double)]
     lib.adakv_q8_scales.restype = Z
     lib.adakv_q8_scales.argtypes = [P, I]
     lib.adakv_decode_workspace_bytes.restype = Z
@@ -120,7 +134,8 @@ def load_library():
     if _marshal is None:                # built since this module was imported
         _marshal = _load_marshal()
     _decode_step_address = ctypes.cast(lib.adakv_decode_step, V).value
-    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8"):
+    for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8", "rotary",
+                 "norm_rotary"):
         _addresses[name] = ctypes.cast(getattr(lib, "adakv_" + name), V).value
     _lib = lib
     return lib
@@ -786,6 +801,119 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     if st != 0:
         raise AdaKVError(st, "adakv_window_attn")
     return (out, row_lse) if (want_lse or row_lse is not None) else out
+
+
+# ---- rotary positions, and norms of the heads ---------------------------------------------------------
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}                          # adakv_rotary_layout
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}       # adakv_rotary_scaling
+
+
+def rotary_frequencies(dims, base=10000.0, scaling="none", factor=1.0, original_len=0, low=1.0, high=4.0):
+    """adakv_rotary_frequencies: radians a position of the dims/2 pairs, as a list."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {', '.join(ROTARY_SCALINGS)}, got {scaling!r}")
+    out = (ctypes.c_double * max(int(dims) // 2, 1))()
+    st = load_library().adakv_rotary_frequencies(int(dims), float(base), ROTARY_SCALINGS[scaling], float(factor), int(original_len),
+                                                 float(low), float(high), out)
+    if st != 0:
+        raise AdaKVError(st, "adakv_rotary_frequencies")
+    return list(out)
+
+
+class Rotary:
+    """How heads are turned (adakv_rotation): `dims` elements of each, pairs in the given `layout`, frequencies as
+    adakv_rotary_frequencies makes them, or those of the tensor `freq` (float64, [dims/2], on the device)."""
+
+    def __init__(self, dims, base=10000.0, layout="half", scaling="none", factor=1.0, original_len=0, low=1.0, high=4.0, magnitude=1.0,
+                 freq=None, device="cuda"):
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError(f"layout must be one of {', '.join(ROTARY_LAYOUTS)}, got {layout!r}")
+        if not magnitude > 0:
+            raise ValueError(f"magnitude must be above 0, got {magnitude}")
+        self.dims, self.layout, self.magnitude = int(dims), layout, float(magnitude)
+        if freq is None:
+            made = rotary_frequencies(dims, base, scaling, factor, original_len, low, high) if self.dims else []
+            freq = torch.tensor(made, dtype=torch.float64, device=device)
+        _need(freq, self.dims // 2, "freq")
+        self.freq = freq
+        self.c = _CRotation(ROTARY_LAYOUTS[layout], self.dims, self.magnitude, _ptr(freq, "freq", torch.float64) if self.dims else None)
+        self._address = ctypes.addressof(self.c)
+
+    def inverse(self) -> "Rotary":
+        """The one that takes this one back."""
+        return Rotary(self.dims, layout=self.layout, magnitude=1.0 / self.magnitude, freq=-self.freq)
+
+
+def _heads(t, name, rows, heads, d, dtype):
+    """Rows of heads, any strides of rows and heads: the tensor as the library takes it.  (A dimension of one has no stride.)"""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.stride(2) != 1:
+        raise ValueError(f"{name} must be [tokens, {heads}, {d}] with contiguous rows")
+    if t.shape[0] < rows:
+        raise ValueError(f"{name} has {t.shape[0]} tokens, the call reaches {rows}")
+    tok, head = t.stride(0) if t.shape[0] > 1 else heads * d, t.stride(1) if heads > 1 else d
+    return _CHeads(_ptr(t, name, dtype), tok, head)
+
+
+def _rotary(name, layer, rotation, q, k, weights, eps, positions, q_out, k_out, stream):
+    """Both calls: `weights` are (q_weight, k_weight), or empty."""
+    lib = load_library()
+    if q_out is not None and k_out is not None and _native(name[6:], layer, stream, rotation._address, rotation.dims, rotation.freq,
+                                                           layer.last_token_row, positions, q, k, *(weights or (None, None)), eps,
+                                                           q_out, k_out, check="rotary"):
+        return q_out, k_out
+    if q is None and k is None:
+        raise ValueError("q or k must be given")
+    given = q if q is not None else k
+    if positions is not None:
+        rows = given.shape[0]
+        if positions.numel() != rows or not positions.is_contiguous() or (k is not None and k.shape[0] != rows):
+            raise ValueError(f"positions must be contiguous, one for each token of q and k, of which there are {rows}" +
+                             (f" and {k.shape[0]}" if k is not None else ""))
+    else:
+        rows = layer.last_token_row
+    for w, x, nm in zip(weights, (q, k), ("q_weight", "k_weight")):
+        if x is not None:
+            if w is None:
+                raise ValueError(f"{nm} must be given")
+            _need(w, layer.d, nm)
+    dt, ins, outs = layer.torch_dtype, [], []
+    made = {}
+    for x, o, nm, heads in ((q, q_out, "q", layer.h_q), (k, k_out, "k", layer.h_kv)):
+        if x is None:
+            if o is not None:
+                raise ValueError(f"{nm}_out is given without {nm}")
+            ins.append(None)
+            outs.append(None)
+            continue
+        ins.append(_heads(x, nm, rows, heads, layer.d, dt))
+        if o is None:
+            o = _zeros((x.shape[0], heads, layer.d), dt, x.device, stream)
+        outs.append(_heads(o, nm + "_out", rows, heads, layer.d, dt))
+        made[nm] = o
+    wp = [_ptr(w, nm, dt) for w, nm in zip(weights, ("q_weight", "k_weight"))]
+    pp = _ptr(positions, "positions", torch.int32)
+    _one_device(stream, q=q, k=k, q_out=made.get("q"), k_out=made.get("k"), positions=positions, freq=rotation.freq if rotation.dims else None,
+                **dict(zip(("q_weight", "k_weight"), weights)))
+    if rows == 0:                       # (an empty tensor has no address, which would mean the layer's own rows)
+        return made.get("q"), made.get("k")
+    by = [None if h is None else ctypes.byref(h) for h in ins + outs]
+    st = getattr(lib, name)(ctypes.byref(layer.c), ctypes.byref(rotation.c), rows, pp, *by[:2], *wp, *((eps,) if weights else ()), *by[2:],
+                            _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, name)
+    return made.get("q"), made.get("k")
+
+
+def rotary(layer: Layer, rotation: Rotary, q, k, positions=None, q_out=None, k_out=None, stream=None):
+    """adakv_rotary: q [tokens, h_q, d] and k [tokens, h_kv, d] (any strides of tokens and heads) turned by their positions,
+    int32 [tokens] (below 0: the token is left out), or without them by each token's place in the layer's sequences.  q or
+    k may be None.  Returns (q_out, k_out); tokens left out: as they were, zero in outputs made here."""
+    return _rotary("adakv_rotary", layer, rotation, q, k, (), 0.0, positions, q_out, k_out, stream)
+
+
+def norm_rotary(layer: Layer, rotation: Rotary, q, k, q_weight, k_weight, eps=1e-6, positions=None, q_out=None, k_out=None, stream=None):
+    """adakv_norm_rotary: `rotary` behind a norm of every head, with weights [d]."""
+    return _rotary("adakv_norm_rotary", layer, rotation, q, k, (q_weight, k_weight), float(eps), positions, q_out, k_out, stream)
 
 
 # ---- the decode-side cache in 8 bits --------------------------------------------------------------------

@@ -460,6 +460,90 @@ int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void
                        ws, ws_bytes, hip_stream);
 }
 
+// ---- rotary positions and head norms ----------------------------------------------------------------
+int adakv_rotary_frequencies(int32_t dims, double base, int32_t scaling, double factor, int32_t original_len, double low, double high,
+                             double *freq) {
+  if (!freq || dims < 2 || dims % 2 != 0 || !(base > 0.0) || isinf(base)) return ADAKV_EINVAL;
+  if (scaling < ADAKV_ROTARY_PLAIN || scaling > ADAKV_ROTARY_PARTS) return ADAKV_EINVAL;
+  if (scaling != ADAKV_ROTARY_PLAIN && (!(factor >= 1.0) || isinf(factor))) return ADAKV_EINVAL;
+  if (scaling == ADAKV_ROTARY_PARTS && (original_len < 1 || !(low >= 0.0) || !(high > low) || isinf(high))) return ADAKV_EINVAL;
+  if (dims > 128) return ADAKV_EUNSUPPORTED;
+  if (scaling == ADAKV_ROTARY_BASE && dims > 2) base *= pow(factor, dims / (dims - 2.0));
+  if (isinf(base)) return ADAKV_EINVAL;
+  for (int i = 0; i < dims / 2; ++i) {
+    const double f = pow(base, -2.0 * i / dims);
+    double by = 1.0;
+    if (scaling == ADAKV_ROTARY_LINEAR) by = 1.0 / factor;
+    if (scaling == ADAKV_ROTARY_PARTS) {
+      const double u = (original_len * f / 6.283185307179586477 - low) / (high - low), share = u < 0.0 ? 0.0 : u > 1.0 ? 1.0 : u;
+      by = share + (1.0 - share) / factor;
+    }
+    freq[i] = f * by;
+  }
+  return ADAKV_OK;
+}
+
+// An input and its output, of `rows` rows of `count` heads.
+static int check_heads(const adakv_heads *x, const adakv_heads *o, long long rows, int count, int d, int esz) {
+  if (!x->x || !o->x) return ADAKV_EINVAL;
+  const int64_t strides[4] = {x->stride_tok, x->stride_head, o->stride_tok, o->stride_head};
+  for (int64_t sd : strides)
+    if (sd < d || sd > (1ll << 40)) return ADAKV_EINVAL;
+  const __int128 tok = o->stride_tok, head = o->stride_head;
+  if (tok < (count - 1) * head + d && head < (rows - 1) * tok + d) return ADAKV_EINVAL;
+  if (x->x == o->x && (x->stride_tok != o->stride_tok || x->stride_head != o->stride_head)) return ADAKV_EINVAL;
+  if (!aligned16(x->x) || !aligned16(o->x)) return ADAKV_EUNSUPPORTED;
+  for (int64_t sd : strides)
+    if (sd * esz % 16 != 0) return ADAKV_EUNSUPPORTED;
+  return ADAKV_OK;
+}
+
+// (both forms)
+static int rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, const int32_t *positions, const adakv_heads *q,
+                  const adakv_heads *k, const adakv_heads *q_out, const adakv_heads *k_out, bool norm, const void *q_weight,
+                  const void *k_weight, float eps, void *hip_stream) {
+  SeqTab st; Dims dm;
+  int rc = build_tables(L, st, dm);
+  if (rc != ADAKV_OK) return rc;
+  if (!R || (R->layout != ADAKV_ROTARY_HALF && R->layout != ADAKV_ROTARY_INTERLEAVED)) return ADAKV_EINVAL;
+  if (R->dims < 0 || R->dims % 2 != 0 || R->dims > L->d || (R->dims > 0 && !R->freq)) return ADAKV_EINVAL;
+  if (!(R->magnitude >= 0.0f) || isinf(R->magnitude)) return ADAKV_EINVAL;
+  if ((!q && !k) || !q != !q_out || !k != !k_out) return ADAKV_EINVAL;
+  if (norm && ((q && !q_weight) || (k && !k_weight) || !(eps >= 0.0f) || isinf(eps))) return ADAKV_EINVAL;
+  long long all = 0, reach = rows;             // rows; one past the last one
+  if (positions) {
+    if (rows < 0) return ADAKV_EINVAL;
+    all = rows;
+  } else {
+    reach = 0;
+    for (int b = 0; b < st.batch; ++b) {
+      const long long mine = (long long)st.n[b] + dm.w, end = st.tok_off[b] + mine;
+      all += mine;
+      reach = end > reach ? end : reach;
+    }
+  }
+  if (all > (1 << 30) || reach > (1ll << 40)) return ADAKV_EUNSUPPORTED;
+  const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
+  if (q && (rc = check_heads(q, q_out, reach, dm.h_q, dm.d, esz)) != ADAKV_OK) return rc;
+  if (k && (rc = check_heads(k, k_out, reach, dm.h_kv, dm.d, esz)) != ADAKV_OK) return rc;
+  if (norm && (!aligned16(q_weight) || !aligned16(k_weight))) return ADAKV_EUNSUPPORTED;
+  if (((uintptr_t)R->freq & 7u) != 0 || ((uintptr_t)positions & 3u) != 0) return ADAKV_EUNSUPPORTED;
+  hipError_t e = launch_rotary(st, dm, L->dtype, *R, (int)all, positions, q, k, q_out, k_out, norm, q_weight, k_weight, eps,
+                               (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, const int32_t *positions, const adakv_heads *q,
+                 const adakv_heads *k, const adakv_heads *q_out, const adakv_heads *k_out, void *hip_stream) {
+  return rotary(L, R, rows, positions, q, k, q_out, k_out, false, nullptr, nullptr, 0.0f, hip_stream);
+}
+
+int adakv_norm_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, const int32_t *positions, const adakv_heads *q,
+                      const adakv_heads *k, const void *q_weight, const void *k_weight, float eps, const adakv_heads *q_out,
+                      const adakv_heads *k_out, void *hip_stream) {
+  return rotary(L, R, rows, positions, q, k, q_out, k_out, true, q_weight, k_weight, eps, hip_stream);
+}
+
 // ---- the cache in 8 bits --------------------------------------------------------------------------
 size_t adakv_q8_scales(const adakv_layer *L, int32_t headroom) {
   SeqTab st; Dims dm;

@@ -215,6 +215,12 @@ hipError_t launch_cache_move(const SeqTab &st, const Dims &dm, int row_bytes, in
 hipError_t launch_window_attn(const SeqTab &st, const Dims &dm, int dtype, const void *q, long long q_tok, long long q_head,
                               const void *K, const void *V, int window, int sinks, void *out, float *row_lse, hipStream_t s);
 
+// ---- rotary positions and head norms (rotary.hip) --------------------------------------------
+// positions == nullptr: the rows of st's sequences.  q and q_out, or k and k_out, may be null together.
+hipError_t launch_rotary(const SeqTab &st, const Dims &dm, int dtype, const adakv_rotation &R, int rows, const int *positions,
+                         const adakv_heads *q, const adakv_heads *k, const adakv_heads *q_out, const adakv_heads *k_out, bool norm,
+                         const void *q_weight, const void *k_weight, float eps, hipStream_t s);
+
 // Profiling aid (adakv_trace_arm): while armed on this host thread, every kernel launch carries
 // a pair of the caller's events that receive the kernel's own start and end timestamps.
 bool trace_pair(const char *name, hipEvent_t *start, hipEvent_t *stop);

@@ -310,6 +310,47 @@ PyObject *cache_move(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// Rows of heads, any strides of rows and heads (a dimension of one has none).
+adakv_heads heads_of(const at::Tensor &t, int64_t rows, int64_t h, int64_t d) {
+  if (t.dim() != 3 || t.size(0) < rows || t.size(1) != h || t.size(2) != d || t.stride(2) != 1) throw Refused();
+  return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : h * d, h > 1 ? t.stride(1) : d};
+}
+
+// (device, function, layer, rotation, dims, freq, tokens of the layer, positions, q, k, q_weight, k_weight, eps, q_out, k_out, stream); the
+// weights are None for the function without a norm
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("rotary", n, 16, a, [](Args &x) {
+    void *fn = x.pointer();
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    const auto *R = static_cast<const adakv_rotation *>(x.pointer());
+    const int64_t dims = x.whole(0, L->d);
+    if (!R || R->dims != dims || R->freq != x.data<double>(at::kDouble, dims / 2)) throw Refused();
+    const int64_t tokens = x.whole(1, std::numeric_limits<int64_t>::max());
+    const bool given = x.a[x.at] != Py_None;
+    const at::Tensor *pos = given ? &x.buffer(at::kInt, 0) : nullptr;
+    if (!given) ++x.at;
+    const at::Tensor &q = x.tensor(l.type), &k = x.tensor(l.type);
+    if (q.dim() != 3 || k.dim() != 3 || q.size(0) == 0 || (given && (pos->numel() != q.size(0) || k.size(0) != q.size(0)))) throw Refused();
+    const int64_t rows = given ? q.size(0) : tokens;
+    const bool norm = x.a[x.at] != Py_None;
+    const void *qw = x.data_or_none<void>(l.type, L->d), *kw = x.data_or_none<void>(l.type, L->d);
+    if (norm != (kw != nullptr)) throw Refused();
+    const double eps = PyFloat_Check(x.a[x.at]) ? PyFloat_AS_DOUBLE(x.a[x.at]) : throw Refused();
+    ++x.at;
+    const at::Tensor &qo = x.tensor(l.type), &ko = x.tensor(l.type);
+    void *stream = x.pointer();
+    const int32_t *pp = given ? static_cast<const int32_t *>(pos->data_ptr()) : nullptr;
+    const adakv_heads h[4] = {heads_of(q, rows, L->h_q, L->d), heads_of(k, rows, L->h_kv, L->d), heads_of(qo, rows, L->h_q, L->d),
+                              heads_of(ko, rows, L->h_kv, L->d)};
+    return unlocked([&] {
+      if (norm)
+        return reinterpret_cast<decltype(&adakv_norm_rotary)>(fn)(L, R, rows, pp, h, h + 1, qw, kw, (float)eps, h + 2, h + 3, stream);
+      return reinterpret_cast<decltype(&adakv_rotary)>(fn)(L, R, rows, pp, h, h + 1, h + 2, h + 3, stream);
+    });
+  });
+}
+
 PyMethodDef methods[] = {
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL,
      "decode_step(function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, out, lse, ws, stream)"},
@@ -319,6 +360,7 @@ PyMethodDef methods[] = {
     ADAKV_METHOD(cache_build_q8),
     ADAKV_METHOD(window_attn),
     ADAKV_METHOD(cache_move),
+    ADAKV_METHOD(rotary),
 #undef ADAKV_METHOD
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
