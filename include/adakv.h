@@ -351,6 +351,50 @@ int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void
                              size_t ws_bytes, void *hip_stream);
 
 /*
+ * ---- A decoding step over shared caches ---------------------------------------------------------
+ *
+ * Sequences whose prompts begin alike (continuations of one prompt, questions about one document) share the
+ * cache of that beginning: it is kept once, and a step reads its rows once for all of them.  Its keys and values
+ * come in front of a sequence's own, which are in the layer's own cache as above (with B = w*h_kv and lengths of 0 to
+ * begin with, where a sequence has nothing else yet).
+ */
+typedef struct {
+  const adakv_layer *L;      /* of the shared caches, its sequences; dtype, h_q, h_kv and d as the other layer's.  Of L these calls
+                                use w, batch, n and B besides (B only to size the caches)                                  */
+  const int32_t *of;         /* (host) [batch of the layer that decodes]: the shared cache of each of its sequences, -1 for none */
+  const int32_t *cu_seqlens; /* (device) and the rest: a cache as adakv_cache_build makes it, only read                    */
+  int32_t headroom;
+  const void *K_cache, *V_cache;
+  const int32_t *seg_len;
+} adakv_prefix;
+
+/* Scratch bytes of the two calls (0 on invalid input). */
+size_t adakv_prefix_workspace_bytes(const adakv_layer *L, int32_t headroom, const adakv_prefix *P);
+
+/*
+ * adakv_decode_attn and adakv_decode_step over the rows of both: for sequence b, query head i and c = i/g, with the rows of the
+ * shared segment of[b]*h_kv + c, if there is one, in front of those of segment b*h_kv + c,
+ *
+ *     out[b][i][:] = sum_t softmax_t(scale * q_new[b][i] . k_t) v_t,   lse[b][i] = ln sum_t exp(scale * q_new[b][i] . k_t)
+ *
+ * with L's scale.  No rows at all give a zero row and lse = -inf.  fp16 layers hold a softmax weight over a shared segment in 22 bits
+ * down to 2^-24 of the part's largest, and to 2^-46 of it beyond.  Logits and values that are no finite numbers, the
+ * appended row, seg_len and overflow, and the other arguments: as for adakv_decode_attn and adakv_decode_step.  In a step the shared
+ * caches are no part of the layer's own (ADAKV_EINVAL).
+ *   ws (device) adakv_prefix_workspace_bytes(L, headroom, P) bytes
+ * ADAKV_EINVAL for an entry of `of` that names no shared cache, or a shared layer of another dtype or other h_q, h_kv or d.
+ */
+int adakv_decode_prefix_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens,
+                             int32_t headroom, const void *K_cache, const void *V_cache,
+                             const int32_t *seg_len, const adakv_prefix *P, float *out, float *lse,
+                             void *ws, size_t ws_bytes, void *hip_stream);
+int adakv_decode_prefix_step(const adakv_layer *L, const void *q_new, const void *k_new,
+                             const void *v_new, const int32_t *cu_seqlens, int32_t headroom,
+                             void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow,
+                             const adakv_prefix *P, float *out, float *lse, void *ws,
+                             size_t ws_bytes, void *hip_stream);
+
+/*
  * ---- Rotary positions, and norms of the heads ---------------------------------------------------
  *
  * What stands between the projections and the calls above: the queries and keys of a prompt, or of the

@@ -56,6 +56,11 @@ class _CHeads(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("stride_tok", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
 
 
+class _CPrefix(ctypes.Structure):
+    _fields_ = [("L", ctypes.POINTER(_CLayer)), ("of", ctypes.POINTER(ctypes.c_int32)), ("cu_seqlens", ctypes.c_void_p),
+                ("headroom", ctypes.c_int32), ("K_cache", ctypes.c_void_p), ("V_cache", ctypes.c_void_p), ("seg_len", ctypes.c_void_p)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -107,6 +112,12 @@ def load_library():
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args
+    XP = ctypes.POINTER(_CPrefix)
+    lib.adakv_decode_prefix_attn.restype = lib.adakv_decode_prefix_step.restype = ctypes.c_int
+    lib.adakv_decode_prefix_attn.argtypes = [P, V, V, I, V, V, V, XP, V, V, V, Z, V]
+    lib.adakv_decode_prefix_step.argtypes = [P, V, V, V, V, I, V, V, V, V, XP, V, V, V, Z, V]
+    lib.adakv_prefix_workspace_bytes.restype = Z
+    lib.adakv_prefix_workspace_bytes.argtypes = [P, I, XP]
     RP, HP = ctypes.POINTER(_CRotation), ctypes.POINTER(_CHeads)
     lib.adakv_rotary.restype = lib.adakv_norm_rotary.restype = lib.adakv_rotary_frequencies.restype = ctypes.c_int
     lib.adakv_rotary.argtypes = [P, RP, L64, V, HP, HP, HP, HP, V]
@@ -135,7 +146,7 @@ def load_library():
         _marshal = _load_marshal()
     _decode_step_address = ctypes.cast(lib.adakv_decode_step, V).value
     for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8", "rotary",
-                 "norm_rotary"):
+                 "norm_rotary", "decode_prefix_step"):
         _addresses[name] = ctypes.cast(getattr(lib, "adakv_" + name), V).value
     _lib = lib
     return lib
@@ -801,6 +812,87 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     if st != 0:
         raise AdaKVError(st, "adakv_window_attn")
     return (out, row_lse) if (want_lse or row_lse is not None) else out
+
+
+# ---- a decoding step over shared caches -------------------------------------------------------------------
+class Prefix:
+    """Caches that sequences share (adakv_prefix): `layer` describes the shared caches, which are its sequences, the tensors are
+    a cache as cache_build makes it, and of[b] is the shared cache of sequence b of the layer that decodes, or -1.  The tensors
+    are read, never written, and may change between calls."""
+
+    def __init__(self, layer: Layer, cu_seqlens, headroom, K_cache, V_cache, seg_len, of):
+        self.layer, self.headroom, self.of = layer, int(headroom), [int(p) for p in of]
+        if any(not -1 <= p < layer.batch for p in self.of):
+            raise ValueError(f"of must name the shared caches, 0 to {layer.batch - 1}, or -1")
+        _check_cache(layer, headroom, K_cache, V_cache)
+        _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
+        _need(seg_len, layer._segments, "seg_len")
+        self.tensors = dict(cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len)
+        at = (_ptr(cu_seqlens, "cu_seqlens", torch.int32), _ptr(K_cache, "K_cache", layer.torch_dtype),
+              _ptr(V_cache, "V_cache", layer.torch_dtype), _ptr(seg_len, "seg_len", torch.int32))
+        self.device = K_cache.get_device()
+        if any(t.get_device() != self.device for t in self.tensors.values()):
+            raise ValueError("the tensors of shared caches must be on one device")
+        self._of = (ctypes.c_int32 * max(len(self.of), 1))(*self.of)
+        self.c = _CPrefix(ctypes.pointer(layer.c), self._of, at[0], self.headroom, *at[1:])
+        self._address = ctypes.addressof(self.c)
+
+
+def prefix_workspace_bytes(layer: Layer, headroom: int, prefix: Prefix) -> int:
+    """adakv_prefix_workspace_bytes."""
+    if len(prefix.of) != layer.batch:
+        raise ValueError(f"the shared caches are given for {len(prefix.of)} sequences, the layer has {layer.batch}")
+    return int(load_library().adakv_prefix_workspace_bytes(ctypes.byref(layer.c), int(headroom), ctypes.byref(prefix.c)))
+
+
+def _decode_prefix(name, layer, q_new, new, cu_seqlens, headroom, K_cache, V_cache, seg_len, over, prefix, out, lse, ws, stream, want_lse):
+    """Both calls: `new` and `over` are (k_new, v_new) and (overflow,), or empty."""
+    lib = load_library()
+    want = (layer.batch, layer.h_q, layer.d)
+    if q_new.shape != want or not q_new.is_contiguous():
+        raise ValueError(f"q_new must be contiguous {want}")
+    if new:
+        _check_new(layer, *new)
+        _need(over[0], 1, "overflow")
+    if len(prefix.of) != layer.batch:
+        raise ValueError(f"the shared caches are given for {len(prefix.of)} sequences, the layer has {layer.batch}")
+    rows = cache_rows(layer, headroom)
+    if K_cache.size(0) < rows or V_cache.size(0) < rows:
+        raise ValueError("cache too small for this layer and head-room")
+    if out is None:
+        out = _empty(want, torch.float32, q_new.device, stream)
+    if lse is None and want_lse:
+        lse = _empty(want[:2], torch.float32, q_new.device, stream)
+    if ws is None:
+        ws = _empty(max(prefix_workspace_bytes(layer, headroom, prefix), 16), torch.uint8, q_new.device, stream)
+    _check_decode_bufs(layer, headroom, K_cache, V_cache, cu_seqlens, seg_len, out, lse, ws)
+    dt = layer.torch_dtype
+    args = (_ptr(q_new, "q_new", dt), *(_ptr(t, nm, dt) for t, nm in zip(new, ("k_new", "v_new"))), _ptr(cu_seqlens, "cu_seqlens", torch.int32),
+            int(headroom), _ptr(K_cache, "K_cache", dt), _ptr(V_cache, "V_cache", dt), _ptr(seg_len, "seg_len", torch.int32),
+            *(_ptr(t, "overflow", torch.int32) for t in over), ctypes.byref(prefix.c), _ptr(out, "out", torch.float32), _ptr(lse, "lse", torch.float32))
+    _one_device(stream, q_new=q_new, cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len, out=out, lse=lse, ws=ws,
+                **dict(zip(("k_new", "v_new"), new)), **dict(zip(("overflow",), over)), **{"prefix." + k: t for k, t in prefix.tensors.items()})
+    st = getattr(lib, name)(ctypes.byref(layer.c), *args, ws.data_ptr(), ws.numel(), _stream(stream))
+    if st != 0:
+        raise AdaKVError(st, name)
+    return (out, lse) if (want_lse or lse is not None) else out
+
+
+def decode_prefix_attn(layer: Layer, q_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, prefix: Prefix, out=None, lse=None, ws=None,
+                       stream=None, want_lse=False):
+    """adakv_decode_prefix_attn: decode_attn over the sequences' shared caches and their own."""
+    return _decode_prefix("adakv_decode_prefix_attn", layer, q_new, (), cu_seqlens, headroom, K_cache, V_cache, seg_len, (), prefix, out, lse,
+                          ws, stream, want_lse)
+
+
+def decode_prefix_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, prefix: Prefix, overflow=None,
+                       out=None, lse=None, ws=None, stream=None, want_lse=False):
+    """adakv_decode_prefix_step: append k_new/v_new to every sequence's own segments and attend over the shared caches and these."""
+    if (lse is not None or not want_lse) and _native("decode_prefix_step", layer, stream, q_new, k_new, v_new, cu_seqlens, headroom, K_cache,
+                                                     V_cache, seg_len, overflow, prefix._address, prefix.device, len(prefix.of), out, lse, ws):
+        return out if lse is None else (out, lse)
+    return _decode_prefix("adakv_decode_prefix_step", layer, q_new, (k_new, v_new), cu_seqlens, headroom, K_cache, V_cache, seg_len,
+                          (overflow,), prefix, out, lse, ws, stream, want_lse)
 
 
 # ---- rotary positions, and norms of the heads ---------------------------------------------------------

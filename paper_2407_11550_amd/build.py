@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 # compile, so their instantiations are built as four translation units side by side
 UNITS = [("score_mfma.hip", ["-DADAKV_MFMA_PART=%d" % part], "score_mfma_%d.o" % part) for part in (1, 2, 3, 4)]
 UNITS += [(src, [], src.replace(".hip", ".o")) for src in
-          ("api.hip", "score_generic.hip", "select.hip", "compact.hip", "probe.hip", "decode_q8.hip", "cache_move.hip", "window_attn.hip", "rotary.hip")]
+          ("decode_prefix.hip", "api.hip", "score_generic.hip", "select.hip", "compact.hip", "probe.hip", "decode_q8.hip", "cache_move.hip",
+           "window_attn.hip", "rotary.hip")]
 # the decoding kernels with a window beside those without
 UNITS += [("decode.hip", ["-DADAKV_DECODE_PART=%d" % part], "decode_%d.o" % part) for part in (1, 2)]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

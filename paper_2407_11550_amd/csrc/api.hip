@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "decode_prefix.h"
 
 namespace adakv {
 
@@ -308,6 +309,12 @@ int adakv_compress_static(const adakv_layer *L, const void *q_window, const void
                         V_out, ws, ADAKV_STATIC_SCRATCH_BYTES, hip_stream);
 }
 
+struct Range { const void *at; size_t bytes; };
+static bool overlap(const Range &a, const Range &b) {
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
+}
+
 // ---- decode side ------------------------------------------------------------------------------
 static int check_headroom(const SeqTab &st, const Dims &dm, int32_t headroom) {
   if (headroom < 0) return ADAKV_EINVAL;
@@ -458,6 +465,79 @@ int adakv_decode_window_step(const adakv_layer *L, const void *q_new, const void
   if (!k_new || !v_new) return ADAKV_EINVAL;
   return decode_window(L, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, window, sinks, out, lse,
                        ws, ws_bytes, hip_stream);
+}
+
+// ---- a decoding step over shared caches ---------------------------------------------------------------
+// The layer's and the shared caches' tables, and what follows from both.
+struct PrefixTables {
+  SeqTab st, shared;
+  Dims dm, shared_dm;
+  Sharing sh;
+  PrefixPlan plan;
+};
+static int prefix_tables(const adakv_layer *L, int32_t headroom, const adakv_prefix *P, PrefixTables &t) {
+  int rc = build_tables(L, t.st, t.dm);
+  if (rc != ADAKV_OK) return rc;
+  if ((rc = check_headroom(t.st, t.dm, headroom)) != ADAKV_OK) return rc;
+  if (!P || !P->L || !P->of) return ADAKV_EINVAL;
+  if ((rc = build_tables(P->L, t.shared, t.shared_dm)) != ADAKV_OK) return rc;
+  if ((rc = check_headroom(t.shared, t.shared_dm, P->headroom)) != ADAKV_OK) return rc;
+  if (P->L->dtype != L->dtype || P->L->h_q != L->h_q || P->L->h_kv != L->h_kv || P->L->d != L->d) return ADAKV_EINVAL;
+  for (int b = 0; b < t.st.batch; ++b)
+    if (P->of[b] < -1 || P->of[b] >= t.shared.batch) return ADAKV_EINVAL;
+  if (!decode_supported(t.dm)) return ADAKV_EUNSUPPORTED;
+  t.sh = share(t.st, t.dm, t.shared.batch, P->of);
+  t.plan = plan_prefix(t.st, t.dm, L->dtype, headroom, t.sh, t.shared, P->headroom);
+  return ADAKV_OK;
+}
+
+size_t adakv_prefix_workspace_bytes(const adakv_layer *L, int32_t headroom, const adakv_prefix *P) {
+  PrefixTables t;
+  return prefix_tables(L, headroom, P, t) == ADAKV_OK ? t.plan.total + 256 : 0;
+}
+
+// (both forms; k_new == NULL: attention only)
+static int decode_prefix(const adakv_layer *L, const void *q_new, const void *k_new, const void *v_new, const int32_t *cu_seqlens,
+                         int32_t headroom, void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow, const adakv_prefix *P,
+                         float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  PrefixTables t;
+  const int rc = prefix_tables(L, headroom, P, t);
+  if (rc == ADAKV_EINVAL) return rc;
+  if (!q_new || !cu_seqlens || !K_cache || !V_cache || !seg_len || !out) return ADAKV_EINVAL;
+  if (!P->cu_seqlens || !P->K_cache || !P->V_cache || !P->seg_len) return ADAKV_EINVAL;
+  if (rc != ADAKV_OK) return rc;
+  if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(K_cache) || !aligned16(V_cache) ||
+      !aligned16(P->K_cache) || !aligned16(P->V_cache))
+    return ADAKV_EUNSUPPORTED;
+  if (k_new) {
+    const size_t row = (size_t)t.dm.d * (L->dtype == ADAKV_FP32 ? 4 : 2), heads = (size_t)t.dm.h_kv;
+    const size_t own = (t.st.out_off[t.st.batch] + t.st.batch * heads * headroom) * row;
+    const size_t theirs = (t.shared.out_off[t.shared.batch] + t.shared.batch * heads * P->headroom) * row;
+    for (const void *x : {(const void *)K_cache, (const void *)V_cache})
+      for (const void *y : {P->K_cache, P->V_cache})
+        if (overlap({x, own}, {y, theirs})) return ADAKV_EINVAL;
+  }
+  if (!ws || ws_bytes < t.plan.total + 256) return ADAKV_EWORKSPACE;
+  char *wsp = (char *)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  const SharedCache sc = {P->K_cache, P->V_cache, P->cu_seqlens, P->seg_len, P->headroom};
+  hipError_t e = launch_decode_prefix(t.st, t.dm, L->dtype, headroom, t.plan, t.sh, sc, q_new, k_new, v_new, cu_seqlens, K_cache,
+                                      V_cache, seg_len, overflow, out, lse, wsp, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
+}
+
+int adakv_decode_prefix_attn(const adakv_layer *L, const void *q_new, const int32_t *cu_seqlens, int32_t headroom, const void *K_cache,
+                             const void *V_cache, const int32_t *seg_len, const adakv_prefix *P, float *out, float *lse, void *ws,
+                             size_t ws_bytes, void *hip_stream) {
+  return decode_prefix(L, q_new, nullptr, nullptr, cu_seqlens, headroom, (void *)K_cache, (void *)V_cache, (int32_t *)seg_len, nullptr, P,
+                       out, lse, ws, ws_bytes, hip_stream);
+}
+
+int adakv_decode_prefix_step(const adakv_layer *L, const void *q_new, const void *k_new, const void *v_new, const int32_t *cu_seqlens,
+                             int32_t headroom, void *K_cache, void *V_cache, int32_t *seg_len, int32_t *overflow, const adakv_prefix *P,
+                             float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  if (!k_new || !v_new) return ADAKV_EINVAL;
+  return decode_prefix(L, q_new, k_new, v_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, P, out, lse, ws, ws_bytes,
+                       hip_stream);
 }
 
 // ---- rotary positions and head norms ----------------------------------------------------------------
@@ -620,12 +700,6 @@ int adakv_decode_step_q8(const adakv_layer *L, const void *q_new, const void *k_
 }
 
 // ---- sequences of a cache, moved --------------------------------------------------------------------
-struct Range { const void *at; size_t bytes; };
-static bool overlap(const Range &a, const Range &b) {
-  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
-  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
-}
-
 // (both forms; a cache in 8 bits has scales)
 static int cache_move(const adakv_layer *L, int32_t count, const int32_t *from, const int32_t *cu_seqlens, int32_t headroom,
                       const Q8Cache &c, const int32_t *seg_len, int32_t headroom_out, int32_t *cu_out, const Q8Cache &o,

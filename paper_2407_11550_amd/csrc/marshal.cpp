@@ -199,6 +199,28 @@ PyObject *decode_window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (device, function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, shared caches, their device, sequences that
+// they are given for, out, lse, ws, stream)
+PyObject *decode_prefix_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("decode_prefix_step", n, 19, a, [](Args &x) {
+    const auto fn = reinterpret_cast<decltype(&adakv_decode_prefix_step)>(x.pointer());
+    const Layer l(x);
+    const adakv_layer *L = l.L;
+    void *q = x.rows(l.type, L->batch, L->h_q, L->d), *k = x.rows(l.type, L->batch, L->h_kv, L->d), *v = x.rows(l.type, L->batch, L->h_kv, L->d);
+    const int32_t *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
+    const int32_t headroom = x.i32();
+    void *K = x.cache(l.type, l.rows(headroom), L->d), *V = x.cache(l.type, l.rows(headroom), L->d);
+    int32_t *len = x.data<int32_t>(at::kInt, l.nseg), *over = x.data_or_none<int32_t>(at::kInt, 1);
+    const auto *P = static_cast<const adakv_prefix *>(x.pointer());
+    if (x.whole(0, 1 << 16) != x.device || x.whole(0, ADAKV_MAX_BATCH) != L->batch) throw Refused();
+    float *out = x.data<float>(at::kFloat, (int64_t)L->batch * L->h_q * L->d), *lse = x.data_or_none<float>(at::kFloat, (int64_t)L->batch * L->h_q);
+    const at::Tensor &ws = x.buffer(at::kByte, 0);
+    const size_t ws_bytes = (size_t)ws.numel();
+    void *p = ws.data_ptr(), *stream = x.pointer();
+    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, len, over, P, out, lse, p, ws_bytes, stream); });
+  });
+}
+
 // (device, function, layer, q, k, v, cu_seqlens, headroom, K, V, k_scale, v_scale, seg_len, overflow, out, lse, ws, stream)
 PyObject *decode_step_q8(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return checked("decode_step_q8", n, 18, a, [](Args &x) {
@@ -361,6 +383,7 @@ PyMethodDef methods[] = {
     ADAKV_METHOD(window_attn),
     ADAKV_METHOD(cache_move),
     ADAKV_METHOD(rotary),
+    ADAKV_METHOD(decode_prefix_step),
 #undef ADAKV_METHOD
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
