@@ -519,9 +519,10 @@ static int decode_prefix(const adakv_layer *L, const void *q_new, const void *k_
   }
   if (!ws || ws_bytes < t.plan.total + 256) return ADAKV_EWORKSPACE;
   char *wsp = (char *)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
-  const SharedCache sc = {P->K_cache, P->V_cache, P->cu_seqlens, P->seg_len, P->headroom};
-  hipError_t e = launch_decode_prefix(t.st, t.dm, L->dtype, headroom, t.plan, t.sh, sc, q_new, k_new, v_new, cu_seqlens, K_cache,
-                                      V_cache, seg_len, overflow, out, lse, wsp, (hipStream_t)hip_stream);
+  const Segments shared = {(const char *)P->K_cache, (const char *)P->V_cache, P->cu_seqlens, P->seg_len, P->headroom};
+  const Segments own = {(const char *)K_cache, (const char *)V_cache, cu_seqlens, seg_len, headroom};
+  hipError_t e = launch_decode_prefix(t.dm, L->dtype, t.plan, t.sh, shared, own, q_new, k_new, v_new, seg_len, overflow, out, lse, wsp,
+                                      (hipStream_t)hip_stream);
   return e == hipSuccess ? ADAKV_OK : ADAKV_EHIP;
 }
 

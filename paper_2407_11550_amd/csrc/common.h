@@ -182,10 +182,6 @@ hipError_t launch_decode_attn(const SeqTab &st, const Dims &dm, int dtype, int h
 hipError_t launch_decode_window(const SeqTab &st, const Dims &dm, int dtype, int headroom, int limit, int sinks,
                                 const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc,
                                 int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s);
-// The partial results of a plan without `whole`, not merged; lengths stay as they are, and the merge is told of appended rows (seg_tab).
-hipError_t launch_decode_parts(const SeqTab &st, const Dims &dm, int dtype, int headroom, const DecodePlan &pl, const void *q,
-                               const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc, int *seg_len, char *ws,
-                               hipStream_t s);
 // Merges the partial results of a plan's workgroups; new_len: the lengths of a call that appends, else null.
 void launch_decode_combine(int nseg, int d, int g, const DecodePlan &pl, char *ws, int *new_len, int *overflow,
                            float *out, float *lse, hipStream_t s);

@@ -627,7 +627,7 @@ template <typename T, int D, int G>
 void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan &pl,
                 const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc,
                 void *Vc, int *seg_len, int *overflow, float *out, float *lse, char *ws,
-                Window win, bool merge, hipStream_t s) {
+                Window win, hipStream_t s) {
   const int nseg = st.batch * dm.h_kv;
   const int per = (nseg + 255) / 256;
   float *part_acc = (float *)(ws + pl.part_acc);
@@ -668,8 +668,7 @@ void run_decode(const SeqTab &st, const Dims &dm, int headroom, const DecodePlan
                  nseg, dm.h_kv, per, pl.split, headroom, dm.scale * LOG2E, (const T *)q, (const char *)k_new,
                  (const char *)v_new, cu, (const int *)seg_len, (char *)Kc, (char *)Vc, res, win);
   // only a call that appends hands the lengths to the merge kernel for updating
-  if (merge)
-    launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
+  launch_decode_combine(nseg, D, G, pl, ws, k_new ? seg_len : nullptr, overflow, out, lse, s);
 }
 
 struct DecodeArgs {
@@ -680,7 +679,6 @@ struct DecodeArgs {
   float *out, *lse;
   char *ws;
   Window win;
-  bool merge = true;                           // false: partial results are all that is asked for
 };
 
 template <typename T, int D>
@@ -688,7 +686,7 @@ bool run_decode_g(const SeqTab &st, const Dims &dm, int headroom, const DecodePl
                   const DecodeArgs &a, hipStream_t s) {
 #define ADAKV_DECODE_G(G)                                                                       \
   run_decode<T, D, G>(st, dm, headroom, pl, a.q, a.k_new, a.v_new, a.cu, a.Kc, a.Vc, a.seg_len,   \
-                      a.overflow, a.out, a.lse, a.ws, a.win, a.merge, s)
+                      a.overflow, a.out, a.lse, a.ws, a.win, s)
   switch (dm.g) {
     case 1: ADAKV_DECODE_G(1); return true;
     case 2: ADAKV_DECODE_G(2); return true;
@@ -826,13 +824,6 @@ hipError_t launch_decode_attn(const SeqTab &st, const Dims &dm, int dtype, int h
                               float *lse, char *ws, hipStream_t s) {
   const DecodePlan pl = plan_decode(st, dm, dtype, headroom);
   const DecodeArgs a = {q, k_new, v_new, cu, Kc, Vc, seg_len, overflow, out, lse, ws, {}};
-  return run_decode_t(st, dm, dtype, headroom, pl, a, s) ? hipGetLastError() : hipErrorInvalidValue;
-}
-
-hipError_t launch_decode_parts(const SeqTab &st, const Dims &dm, int dtype, int headroom, const DecodePlan &pl, const void *q,
-                               const void *k_new, const void *v_new, const int *cu, void *Kc, void *Vc, int *seg_len, char *ws,
-                               hipStream_t s) {
-  const DecodeArgs a = {q, k_new, v_new, cu, Kc, Vc, seg_len, nullptr, nullptr, nullptr, ws, {}, false};
   return run_decode_t(st, dm, dtype, headroom, pl, a, s) ? hipGetLastError() : hipErrorInvalidValue;
 }
 

@@ -42,7 +42,7 @@ template <bool WIN> __device__ __forceinline__ int place_of(int r, int hidden, W
 }
 
 // Finds it from a prefix sum, over the segments, of the parts that their lengths make (blocks of `split` rows).  The
-// same in all lanes.  False: the workgroup has nothing to do (the launch is an upper bound).  The merge kernel finds a
+// same in all lanes.  `before_us`: workgroups of the launch in front of these.  False: the workgroup has nothing to do (the launch is an upper bound).  The merge kernel finds a
 // segment's partial results through seg_tab; the launch has at least one workgroup per segment, and workgroup s
 // files the entry of segment s.
 //
@@ -52,8 +52,8 @@ template <bool WIN> __device__ __forceinline__ int place_of(int r, int hidden, W
 // the workgroup takes segments t*per .. t*per+per-1 and the result goes through sh[0..21].
 template <int NWV = 4, bool WIN = false>
 __device__ __forceinline__ bool find_work(int nseg, int per, int split, int headroom, int grow, const int *cu,
-                                          const int *seg_len, int *sh, int4 *seg_tab, Work &wk, Window win = {}) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, blk = (int)blockIdx.x;
+                                          const int *seg_len, int *sh, int4 *seg_tab, Work &wk, Window win = {}, int before_us = 0) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, blk = (int)blockIdx.x - before_us;
   if (nseg <= 64) {
     const int s = min(lane, nseg - 1);
     const int from = cu[s], cap = cu[s + 1] - from + headroom;

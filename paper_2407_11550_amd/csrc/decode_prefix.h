@@ -14,20 +14,34 @@ struct Sharing {
   unsigned char group[ADAKV_MAX_BATCH];        // a sequence's shared cache, or NONE
   unsigned char place[ADAKV_MAX_BATCH];        // and which of that cache's sequences it is
 };
-struct SharedCache {
-  const void *K, *V;
+// A flattened cache with head-room.
+struct Segments {
+  const char *K, *V;
   const int *cu, *seg_len;
   int headroom;
 };
+// How segments are split: query rows of a workgroup and rows of a shared segment per part; rows of an own one; workgroups of the
+// shared ones, which come first, own segments, and how many of these a thread counts.
+struct PrefixSplit {
+  int rb, shared_split, own_split;
+  int shared_blocks, own_segments, own_per;
+};
+// Partial results: sums, maxima and sums of weights, and which are whose.
+struct PrefixSums {
+  float *shared_acc, *own_acc;
+  float2 *shared_ml, *own_ml;
+  int4 *shared_tab, *own_tab;
+};
 struct PrefixPlan {
-  DecodePlan own;                              // of the sequences' own segments
-  int rb, split, nblk;                         // query rows of a workgroup; rows of a shared segment per part; workgroups at most
-  size_t part_acc, part_ml, tab, total;        // byte offsets: the shared segments' partial results; their first workgroups
+  PrefixSplit split;
+  int own_blocks;                              // workgroups of the own segments, an upper bound as shared_blocks is
+  size_t shared_acc, own_acc, shared_ml, own_ml, shared_tab, own_tab, total;   // byte offsets
 };
 Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of);
 PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh, const SeqTab &shared, int shared_headroom);
-hipError_t launch_decode_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const PrefixPlan &pl, const Sharing &sh,
-                                const SharedCache &sc, const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc,
-                                void *Vc, int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s);
+// k_new == nullptr: attention only
+hipError_t launch_decode_prefix(const Dims &dm, int dtype, const PrefixPlan &pl, const Sharing &sh, const Segments &shared, const Segments &own,
+                                const void *q, const void *k_new, const void *v_new, int *seg_len, int *overflow, float *out, float *lse,
+                                char *ws, hipStream_t s);
 
 }  // namespace adakv

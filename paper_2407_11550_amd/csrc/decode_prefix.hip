@@ -2,24 +2,24 @@
 // segment of a shared cache and over its own, which is one softmax over the rows of both.
 //
 // With M = g query heads of all the sequences that share a segment, its rows are read once for M rows of queries: 4 d M flops for
-// 4 d bytes (16 bits).  Both products run on the matrix cores as the prompt's do (attn_tiles.h), S^T = K Q^T and O^T += V^T P^T, a
-// query per lane, tiles of the segment in LDS.  Weights stay in 32 bits, as in the other decoding steps: what is added up is an fp32
-// result.  bf16: a weight is cut into three bf16 parts whose sum it is to 2^-24, which share one operand of V and
-// one sum.  fp16: two fp16 parts, the lower one times 2^11 with a sum of its own, 22 bits for weights down to 2^-24 of the largest and
-// 2^-45 of it beyond.  fp32: the fp32 matrix instruction.
+// 4 d bytes (16 bits).  Own segments are the same with the g heads of one sequence.  Both products run on the matrix cores as the prompt's do
+// (attn_tiles.h), S^T = K Q^T and O^T += V^T P^T, a query per lane, tiles of the segment in LDS.  Weights stay in 32 bits, as in the other
+// decoding steps: what is added up is an fp32 result.  bf16: a weight is cut into three bf16 parts whose sum it is to 2^-24, which share one
+// operand of V and one sum.  fp16: two fp16 parts, the lower one times 2^11 with a sum of its own, 22 bits for weights down to 2^-24
+// of the largest and 2^-45 of it beyond.  fp32: the fp32 matrix instruction.
 //
 // A segment is split into parts as in decode.hip; a workgroup takes a part for 128, 64 or 32 rows of queries (1, 2 or 4 wavefronts
-// share 32 of them) and files the sums, and a last kernel merges, for each query head, the parts of its own segment and of the shared one.
+// share 32 of them) and files the sums.  A second kernel merges, for each query head, the parts of its own segment and of the shared one, and
+// the row that the call appends, which it also puts into the cache.
 #include <math.h>
 
 #include "attn_tiles.h"
+#include "decode_parts.h"
 #include "decode_prefix.h"
+#include "row_parts.h"
 
 namespace adakv {
 namespace {
-
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float M_INIT = -1.0e30f;             // finite "no row seen yet"
 
 // Weights are taken against a kept reference, 2^BIAS times, and the reference is moved, to the maximum of all so far, only where the
 // sum of a lane's 16 weights of a tile is beyond MOST.  Moved, the largest weight is 2^BIAS, so 16 of them are below MOST.  32 bits and bf16: none
@@ -51,12 +51,6 @@ template <typename TL> __device__ __forceinline__ u32x4 tile_values(const u32x4 
   return u32x4{a0.x, a0.y, a1.x, a1.y};
 }
 
-__device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-// x0 and x1 cut to bf16, x0 in the lower half of the word.
-__device__ __forceinline__ unsigned pack(float x0, float x1) {
-  return __builtin_amdgcn_perm(__float_as_uint(x1), __float_as_uint(x0), 0x07060302u);
-}
-
 // The weights of 32 keys and their products with values.
 template <typename T, int D, typename TL> struct Weights {
   static constexpr int CB = D / 32;
@@ -80,11 +74,11 @@ template <typename T, int D, typename TL> struct Weights {
           w[1][i] = round2<T>(x0, x1);
         } else {
           w[0][i] = pack(x0, x1);
-          x0 -= cut(x0);
-          x1 -= cut(x1);
+          x0 -= cut(x0, true);
+          x1 -= cut(x1, true);
           w[1][i] = pack(x0, x1);
-          x0 -= cut(x0);
-          x1 -= cut(x1);
+          x0 -= cut(x0, true);
+          x1 -= cut(x1, true);
           w[2][i] = pack(x0, x1);
         }
       }
@@ -129,71 +123,111 @@ template <typename T, int D, typename TL> struct Weights {
   }
 };
 
-// What a workgroup works on: part `j` of segment s of the shared caches, rows r0 .. r1 - 1, and query rows from `row` on.
-struct Part {
-  int s, j, row, rows, parts, first_row;
-};
+// Elements 4 e .. 4 e + 3 of a row, in 32 bits.
+template <typename T> __device__ __forceinline__ void load4(const char *row, int e, float (&f)[4]) {
+  if constexpr (is_f32<T>) {
+    const float4 x = reinterpret_cast<const float4 *>(row)[e];
+    f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+  } else {
+    const uint2 x = reinterpret_cast<const uint2 *>(row)[e];
+    f[0] = half_of<T>(x.x & 0xffffu); f[1] = half_of<T>(x.x >> 16);
+    f[2] = half_of<T>(x.y & 0xffffu); f[3] = half_of<T>(x.y >> 16);
+  }
+}
 
-// Finds it, as find_work does in decode_parts.h: from a prefix sum, over the segments, of the workgroups that their lengths make.  A segment's
-// workgroups for the same part lie a multiple of 8 apart, so that one of the chip's 8 caches has the rows for all of them.
-template <int RB>
-__device__ __forceinline__ bool find_part(const Sharing &sh, int split, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
+// What a workgroup works on: keys r0 .. r0 + n - 1 of a segment whose rows begin at `first_row` of its cache, for query rows from `row` on of the M
+// that look at it, `ks` wavefronts to 32 of them.
+struct Part {
+  long long first_row;
+  int s, row, M, ks, n;
+  int first, out;                              // of its sequences in Sharing::order (of an own segment: the sequence); where its sums go
+  bool own;
+};
+// Rows of each part: equal parts in whole tiles, none of them empty.
+__device__ __forceinline__ int rows_a_part(int rows, int parts, int split, int tile) {
+  return min(split, ((rows + parts - 1) / parts + tile - 1) / tile * tile);
+}
+
+// Finds a part of a shared segment, as find_work does in decode_parts.h: from a prefix sum, over the segments, of the workgroups that their lengths make.
+// With several blocks of query rows a segment's workgroups for the same part lie a multiple of 8 apart, so that one of the chip's 8 caches has
+// the rows for all of them; a segment's first part then stands where the last one's would have gone on, so that the places left over
+// fall on all 8 alike.  Partial results go in the parts' order.
+__device__ __forceinline__ bool find_shared(const Sharing &sh, int rb, int split, int tile, int headroom, const int *cu, const int *seg_len, int4 *tab,
+                                            Part &pt) {
   const int nseg = sh.groups * sh.h, lane = threadIdx.x & 63, blk = (int)blockIdx.x;
-  int base = 0;
+  int base = 0, done = 0;                      // workgroups and parts of the segments so far
   bool found = false;
+  const int my_first = sh.first[lane], my_many = sh.first[lane + 1] - my_first;       // of shared cache `lane`
   for (int s0 = 0; s0 < nseg; s0 += 64) {
     const int s = min(s0 + lane, nseg - 1), p = s / sh.h;
     const int from = cu[s], cap = cu[s + 1] - from + headroom;
     const int len = min(max(seg_len[s], 0), cap);              // (a corrupt length can never leave the segment)
-    const int many = sh.first[p + 1] - sh.first[p], blocks = (many * sh.g + RB - 1) / RB;
+    const int blocks = (__shfl(my_many, p) * sh.g + rb - 1) / rb;
     const int parts = (len + split - 1) / split, step = blocks > 1 ? (parts + 7) / 8 * 8 : parts;
     const int n = s0 + lane < nseg ? blocks * step : 0;
     const int upto = wave_scan_incl(n) + base, first = upto - n;
     if (s0 + lane == blk && blk < nseg && threadIdx.x < 64) tab[s] = make_int4(first, parts, step, len);
+    const int turned = wave_scan_incl(n ? parts : 0) + done;
     const unsigned long long here = __ballot(blk >= first && blk < upto);
     if (here != 0 && !found) {
-      const int L = __ffsll(here) - 1, at = blk - __builtin_amdgcn_readlane(first, L), st = __builtin_amdgcn_readlane(step, L);
+      const int L = __ffsll(here) - 1, first_L = __builtin_amdgcn_readlane(first, L), st = __builtin_amdgcn_readlane(step, L);
+      const int count = __builtin_amdgcn_readlane(parts, L), at = blk - first_L, block = at / st;
+      const int turn = st == count ? 0 : (__builtin_amdgcn_readlane(turned, L) - count) % 8;
+      const int j = (at - block * st + st - turn) % st;
+      found = j < count;
+      const int all = __builtin_amdgcn_readlane(len, L), rows = rows_a_part(all, count, split, tile);
       pt.s = s0 + L;
-      pt.j = at % st;
-      pt.row = at / st * RB;
-      pt.rows = __builtin_amdgcn_readlane(len, L);
-      pt.parts = __builtin_amdgcn_readlane(parts, L);
-      pt.first_row = __builtin_amdgcn_readlane(from, L);
-      found = pt.j < pt.parts;
+      pt.first_row = (long long)__builtin_amdgcn_readlane(from, L) + (long long)pt.s * headroom + (long long)j * rows;
+      pt.n = min(all - j * rows, rows);
+      pt.row = block * rb;
+      pt.out = first_L + block * st + j;
     }
     base = __builtin_amdgcn_readlane(upto, 63);
+    done = __builtin_amdgcn_readlane(turned, 63);
     if (found && blk < s0 + 64) break;                         // (a later round may have the entry that this workgroup files)
   }
-  return found;
+  if (!found) return false;
+  const int p = pt.s / sh.h;
+  pt.first = __builtin_amdgcn_readlane(my_first, p);
+  pt.M = __builtin_amdgcn_readlane(my_many, p) * sh.g;
+  pt.ks = 128 / rb;
+  pt.own = false;
+  return true;
 }
 
-template <typename T, int D, int KS>
-__global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 4) ? 1 : 2) void prefix_attn_kernel(
-    Sharing sh, int split, int headroom, float c_log2, const char *__restrict__ q, const int *__restrict__ cu,
-    const int *__restrict__ seg_len, const char *__restrict__ Kc, const char *__restrict__ Vc, float *__restrict__ part_acc,
-    float2 *__restrict__ part_ml, int4 *__restrict__ tab) {
-  typedef Tile<T, D, KS> TL;
+template <typename T, int D> using Rows = Tile<T, D, D == 64 && T::SIZE == 2 ? 4 : 2>;         // tiles of 64 or (256 bytes a row less) 128 rows
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_attn_kernel(Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q,
+                                                                                         Segments shared, Segments own, PrefixSums sums) {
+  typedef Rows<T, D> TL;
   typedef Weights<T, D, TL> W;
-  constexpr int RB = 128 / KS;                                 // query rows of the workgroup
-  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, KB = KT / 32 / KS, CB = D / 32;
-  __shared__ __align__(16) u32x4 shK[TL::TURNS][TL::WORDS], shV[TL::TURNS][TL::WORDS];
-  __shared__ int sh_bad[4];
+  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, CB = D / 32;
+  static_assert(TL::TURNS == 2, "the next tile has a place of its own");
+  __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
+  __shared__ int sh_bad[4], sh_scan[24];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int order = sh.order[lane];
   Part pt;
-  if (!find_part<RB>(sh, split, headroom, cu, seg_len, tab, pt)) return;
-  const int p = pt.s / sh.h, c = pt.s % sh.h;
-  const int M = (sh.first[p + 1] - sh.first[p]) * sh.g;
-  // (equal parts, in whole tiles; none is empty)
-  const int rows = min(split, ((pt.rows + pt.parts - 1) / pt.parts + KT - 1) / KT * KT);
-  const int r0 = pt.j * rows, n = min(pt.rows - r0, rows);     // keys of this part
-  const char *Kh = Kc + ((long long)pt.first_row + (long long)pt.s * headroom + r0) * ROWB;
-  const char *Vh = Vc + ((long long)pt.first_row + (long long)pt.s * headroom + r0) * ROWB;
+  if ((int)blockIdx.x < sp.shared_blocks) {
+    if (!find_shared(sh, sp.rb, sp.shared_split, KT, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
+  } else {
+    Work wk;
+    if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
+      return;
+    const int rows = rows_a_part(wk.rows, wk.parts, sp.own_split, KT);
+    pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, 0, sh.g, KT / 32, min(wk.rows - wk.j * rows, rows), wk.s / sh.h,
+          (int)blockIdx.x - sp.shared_blocks, true};
+  }
+  const Segments &seg = pt.own ? own : shared;
+  const char *Kh = seg.K + pt.first_row * ROWB, *Vh = seg.V + pt.first_row * ROWB;
+  const int c = pt.s % sh.h, n = pt.n, ks = pt.ks;
 
-  const int w0 = pt.row + 32 * (wv / KS), m_row = min(w0 + l32, M - 1);         // the wavefront's first query row, this lane's
-  const bool idle = w0 >= M;
-  const int b = sh.order[sh.first[p] + m_row / sh.g];
+  const int w0 = pt.row + 32 * (wv / ks), m_row = min(w0 + l32, pt.M - 1);      // the wavefront's first query row, this lane's
+  const bool idle = w0 >= pt.M;
+  const int b = pt.own ? pt.first : __shfl(order, pt.first + m_row / sh.g);
   const char *Qh = q + ((long long)(b * sh.h + c) * sh.g + m_row % sh.g) * ROWB;
   u32x4 qf[CH / 2];
 #pragma unroll
@@ -203,7 +237,7 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
   // the wavefront's share of a tile: rows on (wv * LOADS + i) * RPI + lane / CH; rows past the end repeat the last one
   auto load = [&](int t) __attribute__((always_inline)) {
     const char *kb = scalar_address(Kh + (long long)t * KT * ROWB), *vb = scalar_address(Vh + (long long)t * KT * ROWB);
-    const u32x4 *dk = shK[t % TL::TURNS] + wv * TL::LOADS * 64, *dv = shV[t % TL::TURNS] + wv * TL::LOADS * 64;
+    const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
     const int end = n - 1 - t * KT;
 #pragma unroll
     for (int i = 0; i < TL::LOADS; ++i) {
@@ -216,19 +250,16 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
       load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
     }
   };
-  // tile t is there, and the next one on its way where it has a place of its own
+  // tile t is there, and the next one on its way
   auto await = [&](int t) __attribute__((always_inline)) {
-    if constexpr (TL::TURNS == 2) {
-      meet();
-      if (t + 1 < tiles) load(t + 1);
-    } else {
-      if (t > 0) {
-        meet();
-        load(t);
-      }
-      meet();
-    }
+    meet();
+    if (t + 1 < tiles) load(t + 1);
   };
+
+  load(0);
+  // (the wait for the queries stands here, once, and not in front of the first products of every tile, where it would be one for the next tile's loads)
+#pragma unroll
+  for (int s = 0; s < CH / 2; ++s) asm volatile("" : "+v"(qf[s]));
 
   floatx16 acc[W::SUMS][CB];
 #pragma unroll
@@ -247,14 +278,12 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
     return (part[0] + part[1]) + (part[2] + part[3]);
   };
 
-  load(0);
   for (int t = 0; t < tiles; ++t) {
     await(t);
     if (idle) continue;
-    const u32x4 *tk = shK[t % TL::TURNS], *tv = shV[t % TL::TURNS];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int kk = wv % KS * KB + kb, left = n - t * KT - 32 * kk;           // this wavefront's 32 keys of the tile; how many are
+    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
+    for (int kk = wv % ks; kk < KT / 32; kk += ks) {           // this wavefront's 32 keys of the tile
+      const int left = n - t * KT - 32 * kk;                   // how many are
       if (left <= 0) break;
       floatx16 sc = tile_logits<T, TL>(tk + kk * 32 * CH, qf, l32, half);
       if (left < 32) {
@@ -309,11 +338,10 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
         await(t);
         if (idle) continue;
 #pragma nounroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const int kk = wv % KS * KB + kb;
+        for (int kk = wv % ks; kk < KT / 32; kk += ks) {
           if (n - t * KT - 32 * kk <= 0) break;
           // (the rows past the end repeat the last one, so their weights may stay)
-          const floatx16 sc = tile_logits<T, TL>(shK[t % TL::TURNS] + kk * 32 * CH, qf, l32, half);
+          const floatx16 sc = tile_logits<T, TL>(tiles_lds[0][t % 2] + kk * 32 * CH, qf, l32, half);
           float pr[16];
           weigh(sc, pr);
           if constexpr (is_f16<T>) {                           // (none is too small for the type)
@@ -322,7 +350,7 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
           }
           W w;
           w.set(pr);
-          w.add_first(o, shV[t % TL::TURNS] + kk * 32 * CH, lane, cb);
+          w.add_first(o, tiles_lds[1][t % 2] + kk * 32 * CH, lane, cb);
         }
       }
 #pragma unroll
@@ -331,25 +359,25 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
   }
   m -= BIAS<T>;
 
-  if constexpr (KS > 1) {
+  if (ks > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place
     typedef float Shared[CB * 16][64];
-    static_assert((4 - 4 / KS) * sizeof(Shared) <= sizeof(shK), "the sums have room");
-    Shared *sums = reinterpret_cast<Shared *>(&shK[0][0]);
-    float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(&shV[0][0]);
-    const int place = wv / KS * (KS - 1) - 1;                  // + 1 .. KS - 1
+    static_assert((4 - 128 / KT) * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
+    Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
+    float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 4 - 128 / KT);
+    const int place = wv / ks * (ks - 1) - 1;                  // + 1 .. ks - 1
     meet();
-    if (wv % KS) {
+    if (wv % ks) {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sums[place + wv % KS][cb * 16 + i][lane] = acc[0][cb][i];
-      ml[place + wv % KS][lane] = make_float2(m, l);
+        for (int i = 0; i < 16; ++i) others[place + wv % ks][cb * 16 + i][lane] = acc[0][cb][i];
+      ml[place + wv % ks][lane] = make_float2(m, l);
     }
     __syncthreads();
-    if (wv % KS) return;
-#pragma unroll
-    for (int k = 1; k < KS; ++k) {
+    if (wv % ks) return;
+#pragma nounroll
+    for (int k = 1; k < ks; ++k) {
       const float2 other = ml[place + k][lane];
       const float mn = fmaxf(m, other.x), f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(other.x - mn);
       m = mn;
@@ -357,43 +385,54 @@ __global__ __launch_bounds__(256, KS == 4 || (D == 128 && KS == 2 && T::SIZE == 
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0][cb][i] = acc[0][cb][i] * f0 + sums[place + k][cb * 16 + i][lane] * f1;
+        for (int i = 0; i < 16; ++i) acc[0][cb][i] = acc[0][cb][i] * f0 + others[place + k][cb * 16 + i][lane] * f1;
     }
   }
 
-  if (w0 + l32 >= M) return;
-  const long long place = (long long)blockIdx.x * RB + w0 - pt.row + l32;
-  float *dst = part_acc + place * D + 4 * half;
+  if (w0 + l32 >= pt.M) return;
+  const long long place = (long long)pt.out * (pt.own ? sh.g : sp.rb) + w0 - pt.row + l32;
+  float *dst = (pt.own ? sums.own_acc : sums.shared_acc) + place * D + 4 * half;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       *reinterpret_cast<float4 *>(dst + 32 * cb + 8 * k) = make_float4(acc[0][cb][4 * k], acc[0][cb][4 * k + 1], acc[0][cb][4 * k + 2], acc[0][cb][4 * k + 3]);
-  if (half == 0) part_ml[place] = make_float2(m, l);
+  if (half == 0) (pt.own ? sums.own_ml : sums.shared_ml)[place] = make_float2(m, l);
 }
 
-// One workgroup per (own segment, query head of its group) merges the parts of the head's own segment and of the shared one, which are two lists of partial
-// results, and normalises.  Parts are merged NSLOT side by side, each by D/4 lanes, then across slots.
-template <int D>
-__global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb, const int4 *__restrict__ seg_tab, int *__restrict__ seg_len,
-                                                             int *__restrict__ overflow, const float *__restrict__ own_acc,
-                                                             const float2 *__restrict__ own_ml, const int4 *__restrict__ tab,
-                                                             const float *__restrict__ part_acc, const float2 *__restrict__ part_ml,
-                                                             float *__restrict__ out, float *__restrict__ lse) {
-  constexpr int LPE = D / 4, NSLOT = 256 / LPE, UC = 4;
+// One workgroup per (own segment, query head of its group) merges the parts of the head's own segment, of the shared one and the row that the call
+// appends, which are one list of partial results, and normalises.  They are merged NSLOT side by side, each by D/4 lanes, then across slots.  The
+// first head's workgroup puts the row into the cache.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb, float c_log2, const char *__restrict__ q, const char *__restrict__ k_new,
+                                                             const char *__restrict__ v_new, Segments own, int *new_len,
+                                                             int *__restrict__ overflow, PrefixSums sums, float *__restrict__ out,
+                                                             float *__restrict__ lse) {
+  constexpr int LPE = D / 4, NSLOT = 256 / LPE, UC = 4, ROWB = D * T::SIZE;
   __shared__ float sh_a[NSLOT][D];
   __shared__ float sh_m[NSLOT], sh_l[NSLOT];
   const int tid = threadIdx.x, s = blockIdx.x, gi = blockIdx.y, b = s / sh.h, c = s % sh.h;
-  const int4 own = seg_tab[s];                 // first partial, partials, rows now, 1 if a row was appended
-  if (seg_len && gi == 0 && tid == 0) {        // the call appended: the new lengths become visible
-    if (own.w) seg_len[s] = own.z;
-    else if (overflow) *overflow = 1;          // the segment was full, its new row was dropped
-  }
-  int cnt = own.y;
-  long long first = 0, step = 0;
   const int p = sh.group[b];
+  const int4 mine = sums.own_tab[s];           // first partial, partials, rows
+  const int from = own.cu[s];
+  // (the length is what the other kernel saw: this one writes the new one)
+  const bool room = k_new && mine.z < own.cu[s + 1] - from + own.headroom;
+  if (k_new && gi == 0) {
+    const long long at = ((long long)from + (long long)s * own.headroom + mine.z) * ROWB;
+    if (room && tid < 2 * (ROWB / 16)) {
+      const int col = tid % (ROWB / 16) * 16;
+      const bool v = tid >= ROWB / 16;
+      *reinterpret_cast<u32x4 *>(const_cast<char *>(v ? own.V : own.K) + at + col) = *reinterpret_cast<const u32x4 *>((v ? v_new : k_new) + (long long)s * ROWB + col);
+    }
+    if (tid == 0) {
+      if (room) new_len[s] = mine.z + 1;
+      else if (overflow) *overflow = 1;        // the segment was full, its new row was dropped
+    }
+  }
+  int cnt = mine.y;
+  long long first = 0, step = 0;
   if (p != Sharing::NONE) {
-    const int4 e = tab[p * sh.h + c];          // first workgroup, parts, workgroups from one block of rows to the next
+    const int4 e = sums.shared_tab[p * sh.h + c];              // first workgroup, parts, workgroups from one block of rows to the next
     const int row = sh.place[b] * sh.g + gi;
     cnt += e.y;
     first = ((long long)e.x + row / rb * e.z) * rb + row % rb;
@@ -402,29 +441,40 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
   const int e4 = tid % LPE, slot = tid / LPE;
   float m = M_INIT, l = 0.0f;
   float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  auto add = [&](float om, float ol, const float4 &oa) {
+    const float mn = fmaxf(m, om), fo = fast_exp2(m - mn), fn = fast_exp2(om - mn);
+    l = l * fo + ol * fn;
+    a.x = a.x * fo + oa.x * fn; a.y = a.y * fo + oa.y * fn;
+    a.z = a.z * fo + oa.z * fn; a.w = a.w * fo + oa.w * fn;
+    m = mn;
+  };
   for (int i0 = slot; i0 < cnt; i0 += NSLOT * UC) {
     float2 ml[UC];
     float4 pa[UC];
 #pragma unroll
     for (int u = 0; u < UC; ++u) {
       const int i = i0 + u * NSLOT, ii = i < cnt ? i : i0;
-      const bool mine = ii < own.y;
-      const long long at = mine ? (long long)(own.x + ii) * sh.g + gi : first + (ii - own.y) * step;
-      ml[u] = (mine ? own_ml : part_ml)[at];
-      pa[u] = *reinterpret_cast<const float4 *>((mine ? own_acc : part_acc) + at * D + e4 * 4);
+      const bool of_own = ii < mine.y;
+      const long long at = of_own ? (long long)(mine.x + ii) * sh.g + gi : first + (ii - mine.y) * step;
+      ml[u] = (of_own ? sums.own_ml : sums.shared_ml)[at];
+      pa[u] = *reinterpret_cast<const float4 *>((of_own ? sums.own_acc : sums.shared_acc) + at * D + e4 * 4);
       if (i >= cnt) { ml[u] = make_float2(M_INIT, 0.0f); pa[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
     }
 #pragma unroll
-    for (int u = 0; u < UC; ++u) {
-      const float mn = fmaxf(m, ml[u].x);
-      const float fo = __builtin_amdgcn_exp2f(m - mn), fn = __builtin_amdgcn_exp2f(ml[u].x - mn);
-      l = l * fo + ml[u].y * fn;
-      a.x = a.x * fo + pa[u].x * fn; a.y = a.y * fo + pa[u].y * fn;
-      a.z = a.z * fo + pa[u].z * fn; a.w = a.w * fo + pa[u].w * fn;
-      m = mn;
-    }
+    for (int u = 0; u < UC; ++u) add(ml[u].x, ml[u].y, pa[u]);
   }
-  const int live = cnt < NSLOT ? cnt : NSLOT;  // slots that had partials
+  const long long row = (long long)s * sh.g + gi;
+  if (room && slot == cnt % NSLOT) {           // the appended row: one of weight 1 at its logit
+    float x[4], k[4], v[4];
+    load4<T>(q + row * ROWB, e4, x);
+    load4<T>(k_new + (long long)s * ROWB, e4, k);
+    load4<T>(v_new + (long long)s * ROWB, e4, v);
+    float dot = fmaf(x[0], k[0], x[1] * k[1]) + fmaf(x[2], k[2], x[3] * k[3]);
+#pragma unroll
+    for (int o = 1; o < LPE; o <<= 1) dot += __shfl_xor(dot, o);
+    add(dot * c_log2, 1.0f, make_float4(v[0], v[1], v[2], v[3]));
+  }
+  const int all = cnt + room, live = all < NSLOT ? all : NSLOT;                // slots that had any
   if (slot < live) {
     *reinterpret_cast<float4 *>(&sh_a[slot][e4 * 4]) = a;
     if (e4 == 0) { sh_m[slot] = m; sh_l[slot] = l; }
@@ -434,25 +484,24 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
     float M = M_INIT, acc = 0.0f, ll = 0.0f;
     for (int k = 0; k < live; ++k) M = fmaxf(M, sh_m[k]);
     for (int k = 0; k < live; ++k) {
-      const float f = __builtin_amdgcn_exp2f(sh_m[k] - M);
+      const float f = fast_exp2(sh_m[k] - M);
       acc = fmaf(sh_a[k][tid], f, acc);
       ll = fmaf(sh_l[k], f, ll);
     }
-    const long long row = (long long)s * sh.g + gi;
-    out[row * D + tid] = cnt > 0 ? acc / ll : 0.0f;
+    out[row * D + tid] = all > 0 ? acc / ll : 0.0f;
     if (lse && tid == 0) lse[row] = (M + log2f(ll)) * LN2;
   }
 }
 
-template <typename T, int D> void run_parts(const Sharing &sh, const PrefixPlan &pl, const SharedCache &sc, float c_log2, const void *q, char *ws, hipStream_t s) {
-#define ADAKV_PREFIX(KS)                                                                                                          \
-  ADAKV_LAUNCH(KS == 1 ? "prefix_attn" : KS == 2 ? "prefix_attn_2" : "prefix_attn_4", (prefix_attn_kernel<T, D, KS>),              \
-               dim3(pl.nblk), dim3(256), s, sh, pl.split, sc.headroom, c_log2, (const char *)q, sc.cu, sc.seg_len, (const char *)sc.K, \
-               (const char *)sc.V, (float *)(ws + pl.part_acc), (float2 *)(ws + pl.part_ml), (int4 *)(ws + pl.tab))
-  if (pl.rb == 128) ADAKV_PREFIX(1);
-  else if (pl.rb == 64) ADAKV_PREFIX(2);
-  else ADAKV_PREFIX(4);
-#undef ADAKV_PREFIX
+template <typename T, int D>
+void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const void *q, const void *k_new, const void *v_new, const Segments &shared,
+                const Segments &own, int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s) {
+  const PrefixSums sums = {(float *)(ws + pl.shared_acc), (float *)(ws + pl.own_acc), (float2 *)(ws + pl.shared_ml), (float2 *)(ws + pl.own_ml),
+                           (int4 *)(ws + pl.shared_tab), (int4 *)(ws + pl.own_tab)};
+  ADAKV_LAUNCH("prefix_attn", (prefix_attn_kernel<T, D>), dim3(pl.split.shared_blocks + pl.own_blocks), dim3(256), s, sh, pl.split, c_log2,
+               (const char *)q, shared, own, sums);
+  ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, sh.g), dim3(256), s, sh, pl.split.rb, c_log2,
+               (const char *)q, (const char *)k_new, (const char *)v_new, own, seg_len, overflow, sums, out, lse);
 }
 
 }  // namespace
@@ -479,57 +528,61 @@ Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of) {
 
 PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh, const SeqTab &shared, int shared_headroom) {
   PrefixPlan pl = {};
-  pl.own = plan_decode(st, dm, dtype, headroom);
-  pl.own.whole = false;                        // (partial results, for the merge)
-  pl.part_acc = align_up(pl.own.total, 256);
   const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) * sh.g; };
   int most = 0;
   for (int p = 0; p < sh.groups; ++p) most = rows_of(p) > most ? rows_of(p) : most;
-  pl.rb = most <= 32 ? 32 : most <= 64 ? 64 : 128;
-  const auto blocks_of = [&](int p) { return (rows_of(p) + pl.rb - 1) / pl.rb; };
+  const int rb = pl.split.rb = most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;
+  const auto blocks_of = [&](int p) { return (rows_of(p) + rb - 1) / rb; };
   const auto cap_of = [&](int p) { return (long long)shared.out_off[p + 1] - shared.out_off[p] + (long long)dm.h_kv * shared_headroom; };
   long long all = 0, least = 0;                // rows times workgroups that read them; workgroups at least
   for (int p = 0; p < sh.groups; ++p) {
     all += cap_of(p) * blocks_of(p);
     least += (long long)blocks_of(p) * dm.h_kv;
   }
-  const long long round_wgs = pl.rb == 32 ? 256 : 512, room = round_wgs - least;
-  long long want = room > 64 ? (all + room - 1) / room : all / 512;
-  if (want < 128) want = 128;
-  pl.split = (int)((want + 127) / 128 * 128);
+  const auto split_of = [](long long rows, long long wgs) {
+    const long long want = wgs > 64 ? (rows + wgs - 1) / wgs : rows / 512;
+    return (int)((want < 128 ? 128 : want) + 127) / 128 * 128;
+  };
+  pl.split.shared_split = split_of(all, 512 - least);
   long long nblk = 0;
   for (int p = 0; p < sh.groups; ++p) {
     const long long blocks = blocks_of(p);
-    // parts of a segment: at most capacity / split + 1; with several blocks of rows up to 7 more places each
-    nblk += blocks * (cap_of(p) / pl.split + dm.h_kv * (blocks > 1 ? 8 : 1));
+    // parts of a segment: at most capacity / split + 1; with several blocks of rows up to 7 places more for each
+    nblk += blocks * (cap_of(p) / pl.split.shared_split + dm.h_kv * (blocks > 1 ? 8 : 1));
   }
-  const long long nseg = (long long)sh.groups * dm.h_kv;
-  pl.nblk = (int)(nblk > nseg ? nblk : nseg);  // (workgroup s files the entry of segment s)
-  pl.part_ml = pl.part_acc + align_up((size_t)pl.nblk * pl.rb * dm.d * sizeof(float), 256);
-  pl.tab = pl.part_ml + align_up((size_t)pl.nblk * pl.rb * sizeof(float2), 256);
-  pl.total = pl.tab + align_up((size_t)nseg * sizeof(int4), 256);
+  const long long nseg = (long long)sh.groups * dm.h_kv, own = (long long)st.batch * dm.h_kv;
+  pl.split.shared_blocks = (int)(nblk > nseg ? nblk : nseg);   // (workgroup s files the entry of segment s)
+  const long long own_cap = (long long)st.out_off[st.batch] + own * headroom;
+  pl.split.own_segments = (int)own;
+  pl.split.own_per = (int)((own + 255) / 256);
+  pl.split.own_split = split_of(own_cap, 512);
+  pl.own_blocks = (int)(own_cap / pl.split.own_split + own);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align_up(bytes, 256);
+    return here;
+  };
+  pl.shared_acc = take((size_t)pl.split.shared_blocks * rb * dm.d * sizeof(float));
+  pl.own_acc = take((size_t)pl.own_blocks * dm.g * dm.d * sizeof(float));
+  pl.shared_ml = take((size_t)pl.split.shared_blocks * rb * sizeof(float2));
+  pl.own_ml = take((size_t)pl.own_blocks * dm.g * sizeof(float2));
+  pl.shared_tab = take((size_t)nseg * sizeof(int4));
+  pl.own_tab = take((size_t)own * sizeof(int4));
+  pl.total = at;
   return pl;
 }
 
-hipError_t launch_decode_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const PrefixPlan &pl, const Sharing &sh,
-                                const SharedCache &sc, const void *q, const void *k_new, const void *v_new, const int *cu, void *Kc,
-                                void *Vc, int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s) {
-  hipError_t e = launch_decode_parts(st, dm, dtype, headroom, pl.own, q, k_new, v_new, cu, Kc, Vc, seg_len, ws, s);
-  if (e != hipSuccess) return e;
-  const float c_log2 = dm.scale * LOG2E;
-  if (sh.first[sh.groups] > 0) {
-    if (dtype == ADAKV_BF16) dm.d == 64 ? run_parts<BF16, 64>(sh, pl, sc, c_log2, q, ws, s) : run_parts<BF16, 128>(sh, pl, sc, c_log2, q, ws, s);
-    else if (dtype == ADAKV_FP16) dm.d == 64 ? run_parts<FP16, 64>(sh, pl, sc, c_log2, q, ws, s) : run_parts<FP16, 128>(sh, pl, sc, c_log2, q, ws, s);
-    else dm.d == 64 ? run_parts<FP32, 64>(sh, pl, sc, c_log2, q, ws, s) : run_parts<FP32, 128>(sh, pl, sc, c_log2, q, ws, s);
-  }
-  const dim3 grid(st.batch * dm.h_kv, dm.g);
-#define ADAKV_PREFIX_COMBINE(D)                                                                                                      \
-  ADAKV_LAUNCH("prefix_combine", prefix_combine_kernel<D>, grid, dim3(256), s, sh, pl.rb, (const int4 *)(ws + pl.own.seg_tab),        \
-               k_new ? seg_len : nullptr, overflow, (const float *)(ws + pl.own.part_acc), (const float2 *)(ws + pl.own.part_ml),     \
-               (const int4 *)(ws + pl.tab), (const float *)(ws + pl.part_acc), (const float2 *)(ws + pl.part_ml), out, lse)
-  if (dm.d == 64) ADAKV_PREFIX_COMBINE(64);
-  else ADAKV_PREFIX_COMBINE(128);
-#undef ADAKV_PREFIX_COMBINE
+hipError_t launch_decode_prefix(const Dims &dm, int dtype, const PrefixPlan &pl, const Sharing &sh, const Segments &shared, const Segments &own,
+                                const void *q, const void *k_new, const void *v_new, int *seg_len, int *overflow, float *out, float *lse,
+                                char *ws, hipStream_t s) {
+#define ADAKV_PREFIX(T)                                                                                                                     \
+  (dm.d == 64 ? run_prefix<T, 64>(sh, pl, dm.scale * LOG2E, q, k_new, v_new, shared, own, seg_len, overflow, out, lse, ws, s)               \
+              : run_prefix<T, 128>(sh, pl, dm.scale * LOG2E, q, k_new, v_new, shared, own, seg_len, overflow, out, lse, ws, s))
+  if (dtype == ADAKV_BF16) ADAKV_PREFIX(BF16);
+  else if (dtype == ADAKV_FP16) ADAKV_PREFIX(FP16);
+  else ADAKV_PREFIX(FP32);
+#undef ADAKV_PREFIX
   return hipGetLastError();
 }
 
