@@ -487,7 +487,7 @@ static int prefix_tables(const adakv_layer *L, int32_t headroom, const adakv_pre
     if (P->of[b] < -1 || P->of[b] >= t.shared.batch) return ADAKV_EINVAL;
   if (!decode_supported(t.dm)) return ADAKV_EUNSUPPORTED;
   t.sh = share(t.st, t.dm, t.shared.batch, P->of);
-  t.plan = plan_prefix(t.st, t.dm, L->dtype, headroom, t.sh, t.shared, P->headroom);
+  t.plan = plan_prefix(t.st, t.dm, L->dtype, headroom, t.sh);
   return ADAKV_OK;
 }
 

@@ -20,11 +20,11 @@ struct Segments {
   const int *cu, *seg_len;
   int headroom;
 };
-// How segments are split: query rows of a workgroup and rows of a shared segment per part; rows of an own one; workgroups of the
-// shared ones, which come first, own segments, and how many of these a thread counts.
+// How segments are split.  Shared ones, which come first: query rows of a workgroup; parts beyond one for each segment and block of rows;
+// workgroups, an upper bound.  Own ones: rows of a part; segments, and how many of them a thread counts.
 struct PrefixSplit {
-  int rb, shared_split, own_split;
-  int shared_blocks, own_segments, own_per;
+  int rb, spare, shared_blocks;
+  int own_split, own_segments, own_per;
 };
 // Partial results: sums, maxima and sums of weights, and which are whose.
 struct PrefixSums {
@@ -38,7 +38,7 @@ struct PrefixPlan {
   size_t shared_acc, own_acc, shared_ml, own_ml, shared_tab, own_tab, total;   // byte offsets
 };
 Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of);
-PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh, const SeqTab &shared, int shared_headroom);
+PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh);
 // k_new == nullptr: attention only
 hipError_t launch_decode_prefix(const Dims &dm, int dtype, const PrefixPlan &pl, const Sharing &sh, const Segments &shared, const Segments &own,
                                 const void *q, const void *k_new, const void *v_new, int *seg_len, int *overflow, float *out, float *lse,

@@ -5,13 +5,15 @@
 // 4 d bytes (16 bits).  Own segments are the same with the g heads of one sequence.  Both products run on the matrix cores as the prompt's do
 // (attn_tiles.h), S^T = K Q^T and O^T += V^T P^T, a query per lane, tiles of the segment in LDS.  Weights stay in 32 bits, as in the other
 // decoding steps: what is added up is an fp32 result.  bf16: a weight is cut into three bf16 parts whose sum it is to 2^-24, which share one
-// operand of V and one sum.  fp16: two fp16 parts, the lower one times 2^11 with a sum of its own, 22 bits for weights down to 2^-24
+// operand of V and one sum.  fp16: two fp16 parts, the lower one times 2^11 with a sum of its own, 22 bits for weights down to 2^-23
 // of the largest and 2^-45 of it beyond.  fp32: the fp32 matrix instruction.
 //
 // A segment is split into parts as in decode.hip; a workgroup takes a part for 128, 64 or 32 rows of queries (1, 2 or 4 wavefronts
 // share 32 of them) and files the sums.  A second kernel merges, for each query head, the parts of its own segment and of the shared one, and
 // the row that the call appends, which it also puts into the cache.
 #include <math.h>
+
+#include <type_traits>
 
 #include "attn_tiles.h"
 #include "decode_parts.h"
@@ -22,9 +24,9 @@ namespace adakv {
 namespace {
 
 // Weights are taken against a kept reference, 2^BIAS times, and the reference is moved, to the maximum of all so far, only where the
-// sum of a lane's 16 weights of a tile is beyond MOST.  Moved, the largest weight is 2^BIAS, so 16 of them are below MOST.  32 bits and bf16: none
+// sum of a lane's 16 or 32 weights is beyond MOST.  Moved, the largest weight is 2^BIAS, so 32 of them are no more than MOST.  32 bits and bf16: none
 // is above 1, so that no sum is larger than the values times the rows.  fp16: none beyond the type.
-template <typename T> constexpr float BIAS = is_f16<T> ? 10.0f : -15.0f;
+template <typename T> constexpr float BIAS = is_f16<T> ? 9.0f : -15.0f;
 template <typename T> constexpr float MOST = is_f16<T> ? 0x1p15f : 1.0f;
 constexpr float LOW_UP = 0x1p11f, LOW_DOWN = 0x1p-11f;         // of an fp16 weight's lower part
 
@@ -143,55 +145,77 @@ struct Part {
   int first, out;                              // of its sequences in Sharing::order (of an own segment: the sequence); where its sums go
   bool own;
 };
-// Rows of each part: equal parts in whole tiles, none of them empty.
-__device__ __forceinline__ int rows_a_part(int rows, int parts, int split, int tile) {
-  return min(split, ((rows + parts - 1) / parts + tile - 1) / tile * tile);
-}
-
-// Finds a part of a shared segment, as find_work does in decode_parts.h: from a prefix sum, over the segments, of the workgroups that their lengths make.
-// With several blocks of query rows a segment's workgroups for the same part lie a multiple of 8 apart, so that one of the chip's 8 caches has
-// the rows for all of them; a segment's first part then stands where the last one's would have gone on, so that the places left over
-// fall on all 8 alike.  Partial results go in the parts' order.
-__device__ __forceinline__ bool find_shared(const Sharing &sh, int rb, int split, int tile, int headroom, const int *cu, const int *seg_len, int4 *tab,
-                                            Part &pt) {
-  const int nseg = sh.groups * sh.h, lane = threadIdx.x & 63, blk = (int)blockIdx.x;
-  int base = 0, done = 0;                      // workgroups and parts of the segments so far
-  bool found = false;
-  const int my_first = sh.first[lane], my_many = sh.first[lane + 1] - my_first;       // of shared cache `lane`
-  for (int s0 = 0; s0 < nseg; s0 += 64) {
-    const int s = min(s0 + lane, nseg - 1), p = s / sh.h;
-    const int from = cu[s], cap = cu[s + 1] - from + headroom;
-    const int len = min(max(seg_len[s], 0), cap);              // (a corrupt length can never leave the segment)
-    const int blocks = (__shfl(my_many, p) * sh.g + rb - 1) / rb;
-    const int parts = (len + split - 1) / split, step = blocks > 1 ? (parts + 7) / 8 * 8 : parts;
-    const int n = s0 + lane < nseg ? blocks * step : 0;
-    const int upto = wave_scan_incl(n) + base, first = upto - n;
-    if (s0 + lane == blk && blk < nseg && threadIdx.x < 64) tab[s] = make_int4(first, parts, step, len);
-    const int turned = wave_scan_incl(n ? parts : 0) + done;
-    const unsigned long long here = __ballot(blk >= first && blk < upto);
-    if (here != 0 && !found) {
-      const int L = __ffsll(here) - 1, first_L = __builtin_amdgcn_readlane(first, L), st = __builtin_amdgcn_readlane(step, L);
-      const int count = __builtin_amdgcn_readlane(parts, L), at = blk - first_L, block = at / st;
-      const int turn = st == count ? 0 : (__builtin_amdgcn_readlane(turned, L) - count) % 8;
-      const int j = (at - block * st + st - turn) % st;
-      found = j < count;
-      const int all = __builtin_amdgcn_readlane(len, L), rows = rows_a_part(all, count, split, tile);
-      pt.s = s0 + L;
-      pt.first_row = (long long)__builtin_amdgcn_readlane(from, L) + (long long)pt.s * headroom + (long long)j * rows;
-      pt.n = min(all - j * rows, rows);
-      pt.row = block * rb;
-      pt.out = first_L + block * st + j;
-    }
-    base = __builtin_amdgcn_readlane(upto, 63);
-    done = __builtin_amdgcn_readlane(turned, 63);
-    if (found && blk < s0 + 64) break;                         // (a later round may have the entry that this workgroup files)
+// Finds a part of a shared segment, as find_work does in decode_parts.h from a prefix sum, over the segments, of the parts that their lengths make; but
+// a part is as long as it has to be for all of them to be `spare` and one for each segment at most, whatever the capacities are: the
+// call lasts as long as its longest part.
+// With several blocks of query rows a shared cache's workgroups come in groups of 8 parts, 8 for each block of rows, so that those for one part lie
+// a multiple of 8 apart and one of the chip's 8 caches has the rows for all of them.  There are none without work in between: a workgroup that ends at
+// once makes the next ones come two to a compute unit where another has room (512 parts with 50 of those among them: 98 us, behind them 71).
+// The first part's workgroup files the segment's entry.
+template <int TILE>
+__device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int rb, int spare, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
+  const int h = sh.h, groups = sh.groups, nseg = groups * h, lane = threadIdx.x & 63;
+  const int my_first = sh.first[lane], my_many = lane < groups ? sh.first[lane + 1] - my_first : 0;    // of shared cache `lane`
+  const int my_blocks = (my_many * sh.g + rb - 1) / rb;
+  int from, len;
+  auto look = [&](int s) {                     // at a segment
+    from = cu[s];
+    len = min(max(seg_len[s], 0), cu[s + 1] - from + headroom);                // (a corrupt length can never leave the segment)
+    return (len + TILE - 1) / TILE;
+  };
+  // tiles of each shared cache, one a lane, and all of them as often as they are read (less than 2^31 / TILE rows, times 16 blocks)
+  const bool few = nseg <= 64;                 // a segment a lane
+  int tiles = 0, split, my_parts = 0, upto = 0;
+  if (few) {
+    tiles = look(min(lane, nseg - 1));
+    const int blocks = __shfl(my_blocks, min(lane, nseg - 1) / h);             // (of all lanes: one that is off has nothing to give)
+    const int all = wave_sum(lane < nseg ? tiles * blocks : 0);
+    split = max(1, (all + spare - 1) / spare);                 // tiles a part
+    const int parts = lane < nseg && blocks > 0 ? (tiles + split - 1) / split : 0;
+    upto = wave_scan_incl(parts);
+    const int last = __shfl(upto, min(lane * h + h - 1, 63)), before = __shfl(upto, max(min(lane * h, 64) - 1, 0));
+    my_parts = lane < groups ? last - (lane ? before : 0) : 0;
+  } else {
+    int mine = 0;
+#pragma unroll 4
+    for (int c = 0; c < h; ++c) mine += look(min(lane, groups - 1) * h + c);
+    const int all = wave_sum(mine * my_blocks);
+    split = max(1, (all + spare - 1) / spare);
+#pragma unroll 4
+    for (int c = 0; c < h; ++c) my_parts += (look(min(lane, groups - 1) * h + c) + split - 1) / split;
+    my_parts = my_blocks > 0 ? my_parts : 0;
   }
-  if (!found) return false;
-  const int p = pt.s / sh.h;
+  const int size = my_blocks > 1 ? my_blocks * ((my_parts + 7) / 8 * 8) : my_parts, end = wave_scan_incl(size);
+  const unsigned long long here = __ballot(blk >= end - size && blk < end);
+  if (here == 0) return false;
+  const int p = __ffsll(here) - 1, base = __builtin_amdgcn_readlane(end - size, p), blocks = __builtin_amdgcn_readlane(my_blocks, p);
+  const int count = __builtin_amdgcn_readlane(my_parts, p), at = blk - base;
+  const int i = blocks > 1 ? at / (8 * blocks) * 8 + at % 8 : at, block = blocks > 1 ? at / 8 % blocks : 0;    // which part of the cache's
+  if (i >= count) return false;
+  int before;                                  // parts in front of the segment's, in its cache
+  if (few) {
+    const int shift = p ? __builtin_amdgcn_readlane(upto, p * h - 1) : 0;
+    const int L = __ffsll(__ballot(upto - shift > i)) - 1;
+    pt.s = L;
+    before = (L ? __builtin_amdgcn_readlane(upto, L - 1) : 0) - shift;
+  } else {
+    tiles = look(p * h + min(lane, h - 1));
+    upto = wave_scan_incl(lane < h ? (tiles + split - 1) / split : 0);
+    const int L = __ffsll(__ballot(upto > i)) - 1;
+    pt.s = p * h + L;
+    before = L ? __builtin_amdgcn_readlane(upto, L - 1) : 0;
+  }
+  const int L = few ? pt.s : pt.s - p * h, j = i - before, all = __builtin_amdgcn_readlane(tiles, L), parts = (all + split - 1) / split;
+  const int rows = (all + parts - 1) / parts * TILE, held = __builtin_amdgcn_readlane(len, L);       // equal parts, none of them empty
+  pt.first_row = (long long)__builtin_amdgcn_readlane(from, L) + (long long)pt.s * headroom + (long long)j * rows;
+  pt.n = min(held - j * rows, rows);
+  pt.row = block * rb;
+  pt.out = base + block * count + i;
   pt.first = __builtin_amdgcn_readlane(my_first, p);
   pt.M = __builtin_amdgcn_readlane(my_many, p) * sh.g;
   pt.ks = 128 / rb;
   pt.own = false;
+  if (j == 0 && block == 0 && threadIdx.x == 0) tab[pt.s] = make_int4(base + before, parts, count, held);
   return true;
 }
 
@@ -203,6 +227,7 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   typedef Rows<T, D> TL;
   typedef Weights<T, D, TL> W;
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, CB = D / 32;
+  constexpr bool PAIRS = !(is_f16<T> && D == 128);             // (its two sets of sums leave no registers for the logits of two)
   static_assert(TL::TURNS == 2, "the next tile has a place of its own");
   __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
   __shared__ int sh_bad[4], sh_scan[24];
@@ -212,12 +237,12 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   const int order = sh.order[lane];
   Part pt;
   if ((int)blockIdx.x < sp.shared_blocks) {
-    if (!find_shared(sh, sp.rb, sp.shared_split, KT, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
+    if (!find_shared<KT>(sh, (int)blockIdx.x, sp.rb, sp.spare, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
   } else {
     Work wk;
     if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
       return;
-    const int rows = rows_a_part(wk.rows, wk.parts, sp.own_split, KT);
+    const int rows = min(sp.own_split, ((wk.rows + wk.parts - 1) / wk.parts + KT - 1) / KT * KT);    // (as above)
     pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, 0, sh.g, KT / 32, min(wk.rows - wk.j * rows, rows), wk.s / sh.h,
           (int)blockIdx.x - sp.shared_blocks, true};
   }
@@ -239,15 +264,17 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     const char *kb = scalar_address(Kh + (long long)t * KT * ROWB), *vb = scalar_address(Vh + (long long)t * KT * ROWB);
     const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
     const int end = n - 1 - t * KT;
+    int here = lane;
+    asm volatile("" : "+v"(here));             // (addresses are made here, not kept in registers)
 #pragma unroll
     for (int i = 0; i < TL::LOADS; ++i) {
-      const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
-      load_to_lds(kb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_k(row)) * 16, 0u, dk + i * 64);
+      const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH;
+      load_to_lds(kb, (unsigned)min(row, end) * ROWB + ((here % CH) ^ TL::swz_k(row)) * 16, 0u, dk + i * 64);
     }
 #pragma unroll
     for (int i = 0; i < TL::LOADS; ++i) {
-      const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
-      load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
+      const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH;
+      load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((here % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
     }
   };
   // tile t is there, and the next one on its way
@@ -277,38 +304,65 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     }
     return (part[0] + part[1]) + (part[2] + part[3]);
   };
+  // N times 32 keys of the tile t, `apart` from each other: all the logits, all the weights, then the sums, with nothing but the rare move of
+  // the reference in between, so that the matrix instructions of one run beside the vector instructions of another.
+  auto add_keys = [&](auto many, int t, int kk, int apart) __attribute__((always_inline)) {
+    constexpr int N = decltype(many)::value;
+    int here = lane;
+    asm volatile("" : "+v"(here));             // (addresses are made here, not kept in registers)
+    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
+    floatx16 sc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) sc[k] = tile_logits<T, TL>(tk + (kk + k * apart) * 32 * CH, qf, here & 31, here >> 5);
+    const int left = n - t * KT - 32 * kk;     // keys from the first on
+    if (left < 32 * ((N - 1) * apart + 1)) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[k][i] = 8 * (i / 4) + 4 * half + i % 4 < left - 32 * k * apart ? sc[k][i] : -INFINITY;
+    }
+    float pr[N][16], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float one = weigh(sc[k], pr[k]);
+      sum = k ? sum + one : one;
+    }
+    if (__builtin_expect(__any(!(sum <= MOST<T>)), 0)) {       // too far above the reference (or no number): a new one
+      float top = sc[0][0];
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[k][i]);
+      const float mn = fmaxf(m, fmaxf(top, other_half(top)) * c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int i = 0; i < W::SUMS; ++i)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[i][cb] *= corr;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float one = weigh(sc[k], pr[k]);
+        sum = k ? sum + one : one;
+      }
+    }
+    l += sum;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      W w;
+      w.set(pr[k]);
+      w.add_values(acc, tv + (kk + k * apart) * 32 * CH, here);
+    }
+  };
 
   for (int t = 0; t < tiles; ++t) {
     await(t);
     if (idle) continue;
-    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
-    for (int kk = wv % ks; kk < KT / 32; kk += ks) {           // this wavefront's 32 keys of the tile
-      const int left = n - t * KT - 32 * kk;                   // how many are
-      if (left <= 0) break;
-      floatx16 sc = tile_logits<T, TL>(tk + kk * 32 * CH, qf, l32, half);
-      if (left < 32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + 4 * half + i % 4 < left ? sc[i] : -INFINITY;
-      }
-      float pr[16];
-      float sum = weigh(sc, pr);
-      if (__builtin_expect(__any(!(sum <= MOST<T>)), 0)) {     // too far above the reference (or no number): a new one
-        float top = sc[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
-        const float mn = fmaxf(m, fmaxf(top, other_half(top)) * c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= corr;
-#pragma unroll
-        for (int i = 0; i < W::SUMS; ++i)
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb) acc[i][cb] *= corr;
-        sum = weigh(sc, pr);
-      }
-      l += sum;
-      W w;
-      w.set(pr);
-      w.add_values(acc, tv + kk * 32 * CH, lane);
+    const int mine = wv % ks;                  // this wavefront's 32 keys of the tile, and every ks-th 32 from there
+    if (PAIRS && 2 * ks <= KT / 32) {
+      for (int kk = mine; kk < KT / 32 && n - t * KT - 32 * kk > 0; kk += 2 * ks) add_keys(std::integral_constant<int, 2>{}, t, kk, ks);
+    } else {
+      for (int kk = mine; kk < KT / 32 && n - t * KT - 32 * kk > 0; kk += ks) add_keys(std::integral_constant<int, 1>{}, t, kk, ks);
     }
   }
   l += other_half(l);
@@ -405,7 +459,7 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
 // first head's workgroup puts the row into the cache.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb, float c_log2, const char *__restrict__ q, const char *__restrict__ k_new,
-                                                             const char *__restrict__ v_new, Segments own, int *new_len,
+                                                             const char *__restrict__ v_new, Segments shared, Segments own, int *new_len,
                                                              int *__restrict__ overflow, PrefixSums sums, float *__restrict__ out,
                                                              float *__restrict__ lse) {
   constexpr int LPE = D / 4, NSLOT = 256 / LPE, UC = 4, ROWB = D * T::SIZE;
@@ -431,8 +485,9 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
   }
   int cnt = mine.y;
   long long first = 0, step = 0;
-  if (p != Sharing::NONE) {
-    const int4 e = sums.shared_tab[p * sh.h + c];              // first workgroup, parts, workgroups from one block of rows to the next
+  // (a shared segment without rows has no entry)
+  if (p != Sharing::NONE && shared.seg_len[p * sh.h + c] > 0 && shared.cu[p * sh.h + c + 1] - shared.cu[p * sh.h + c] + shared.headroom > 0) {
+    const int4 e = sums.shared_tab[p * sh.h + c];              // first partial of the first block of rows, parts, from one block to the next
     const int row = sh.place[b] * sh.g + gi;
     cnt += e.y;
     first = ((long long)e.x + row / rb * e.z) * rb + row % rb;
@@ -501,7 +556,7 @@ void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const voi
   ADAKV_LAUNCH("prefix_attn", (prefix_attn_kernel<T, D>), dim3(pl.split.shared_blocks + pl.own_blocks), dim3(256), s, sh, pl.split, c_log2,
                (const char *)q, shared, own, sums);
   ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, sh.g), dim3(256), s, sh, pl.split.rb, c_log2,
-               (const char *)q, (const char *)k_new, (const char *)v_new, own, seg_len, overflow, sums, out, lse);
+               (const char *)q, (const char *)k_new, (const char *)v_new, shared, own, seg_len, overflow, sums, out, lse);
 }
 
 }  // namespace
@@ -526,36 +581,27 @@ Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of) {
   return sh;
 }
 
-PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh, const SeqTab &shared, int shared_headroom) {
+PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh) {
   PrefixPlan pl = {};
   const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) * sh.g; };
   int most = 0;
   for (int p = 0; p < sh.groups; ++p) most = rows_of(p) > most ? rows_of(p) : most;
   const int rb = pl.split.rb = most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;
   const auto blocks_of = [&](int p) { return (rows_of(p) + rb - 1) / rb; };
-  const auto cap_of = [&](int p) { return (long long)shared.out_off[p + 1] - shared.out_off[p] + (long long)dm.h_kv * shared_headroom; };
-  long long all = 0, least = 0;                // rows times workgroups that read them; workgroups at least
+  long long n = 0, padding = 0;                // workgroups at least, one for each segment and block of rows; places that groups of 8 take
   for (int p = 0; p < sh.groups; ++p) {
-    all += cap_of(p) * blocks_of(p);
-    least += (long long)blocks_of(p) * dm.h_kv;
+    n += (long long)blocks_of(p) * dm.h_kv;
+    if (blocks_of(p) > 1) padding += 7ll * blocks_of(p);
   }
-  const auto split_of = [](long long rows, long long wgs) {
-    const long long want = wgs > 64 ? (rows + wgs - 1) / wgs : rows / 512;
-    return (int)((want < 128 ? 128 : want) + 127) / 128 * 128;
-  };
-  pl.split.shared_split = split_of(all, 512 - least);
-  long long nblk = 0;
-  for (int p = 0; p < sh.groups; ++p) {
-    const long long blocks = blocks_of(p);
-    // parts of a segment: at most capacity / split + 1; with several blocks of rows up to 7 places more for each
-    nblk += blocks * (cap_of(p) / pl.split.shared_split + dm.h_kv * (blocks > 1 ? 8 : 1));
-  }
+  const long long want = 256;
+  pl.split.spare = (int)(want - n > n / 2 + 1 ? want - n : n / 2 + 1);
+  pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
+  const int tile = dm.d == 64 && dtype != ADAKV_FP32 ? 128 : 64;
   const long long nseg = (long long)sh.groups * dm.h_kv, own = (long long)st.batch * dm.h_kv;
-  pl.split.shared_blocks = (int)(nblk > nseg ? nblk : nseg);   // (workgroup s files the entry of segment s)
-  const long long own_cap = (long long)st.out_off[st.batch] + own * headroom;
+  const long long own_cap = (long long)st.out_off[st.batch] + own * headroom, a_part = (own_cap + 511) / 512;
   pl.split.own_segments = (int)own;
   pl.split.own_per = (int)((own + 255) / 256);
-  pl.split.own_split = split_of(own_cap, 512);
+  pl.split.own_split = (int)((a_part < tile ? tile : a_part) + tile - 1) / tile * tile;
   pl.own_blocks = (int)(own_cap / pl.split.own_split + own);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
