@@ -13,8 +13,6 @@
 // the row that the call appends, which it also puts into the cache.
 #include <math.h>
 
-#include <type_traits>
-
 #include "attn_tiles.h"
 #include "decode_parts.h"
 #include "decode_prefix.h"
@@ -137,12 +135,11 @@ template <typename T> __device__ __forceinline__ void load4(const char *row, int
   }
 }
 
-// What a workgroup works on: keys r0 .. r0 + n - 1 of a segment whose rows begin at `first_row` of its cache, for query rows from `row` on of the M
-// that look at it, `ks` wavefronts to 32 of them.
+// What a workgroup works on: n keys from row `first_row` of the cache on, of segment s, for query rows from `row` on of the M that look at it.
 struct Part {
   long long first_row;
-  int s, row, M, ks, n;
-  int first, out;                              // of its sequences in Sharing::order (of an own segment: the sequence); where its sums go
+  int s, row, M, n;
+  int out, first;                              // where its sums go; the segment's first sequence in Sharing::order, or its only one
   bool own;
 };
 // Finds a part of a shared segment, as find_work does in decode_parts.h from a prefix sum, over the segments, of the parts that their lengths make; but
@@ -152,11 +149,11 @@ struct Part {
 // a multiple of 8 apart and one of the chip's 8 caches has the rows for all of them.  There are none without work in between: a workgroup that ends at
 // once makes the next ones come two to a compute unit where another has room (512 parts with 50 of those among them: 98 us, behind them 71).
 // The first part's workgroup files the segment's entry.
-template <int TILE>
-__device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int rb, int spare, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
+template <int TILE, int RB>
+__device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spare, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
   const int h = sh.h, groups = sh.groups, nseg = groups * h, lane = threadIdx.x & 63;
   const int my_first = sh.first[lane], my_many = lane < groups ? sh.first[lane + 1] - my_first : 0;    // of shared cache `lane`
-  const int my_blocks = (my_many * sh.g + rb - 1) / rb;
+  const int my_blocks = (my_many * sh.g + RB - 1) / RB;
   int from, len;
   auto look = [&](int s) {                     // at a segment
     from = cu[s];
@@ -209,11 +206,10 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int rb, 
   const int rows = (all + parts - 1) / parts * TILE, held = __builtin_amdgcn_readlane(len, L);       // equal parts, none of them empty
   pt.first_row = (long long)__builtin_amdgcn_readlane(from, L) + (long long)pt.s * headroom + (long long)j * rows;
   pt.n = min(held - j * rows, rows);
-  pt.row = block * rb;
+  pt.row = block * RB;
   pt.out = base + block * count + i;
   pt.first = __builtin_amdgcn_readlane(my_first, p);
   pt.M = __builtin_amdgcn_readlane(my_many, p) * sh.g;
-  pt.ks = 128 / rb;
   pt.own = false;
   if (j == 0 && block == 0 && threadIdx.x == 0) tab[pt.s] = make_int4(base + before, parts, count, held);
   return true;
@@ -221,36 +217,22 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int rb, 
 
 template <typename T, int D> using Rows = Tile<T, D, D == 64 && T::SIZE == 2 ? 4 : 2>;         // tiles of 64 or (256 bytes a row less) 128 rows
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_attn_kernel(Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q,
-                                                                                         Segments shared, Segments own, PrefixSums sums) {
+// Sums of a part, `KS` wavefronts to 32 query rows.
+template <typename T, int D, int KS>
+__device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
+                                         int stride, u32x4 (&tiles_lds)[2][2][Rows<T, D>::WORDS], int (&sh_bad)[4]) {
   typedef Rows<T, D> TL;
   typedef Weights<T, D, TL> W;
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, CB = D / 32;
-  constexpr bool PAIRS = !(is_f16<T> && D == 128);             // (its two sets of sums leave no registers for the logits of two)
-  static_assert(TL::TURNS == 2, "the next tile has a place of its own");
-  __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
-  __shared__ int sh_bad[4], sh_scan[24];
-
+  // 32 keys at a time, or two times 32 where a wavefront has so many of a tile (fp16, d = 128: its two sets of sums leave no registers for the logits of two)
+  constexpr int PAIR = 2 * KS <= KT / 32 && !(is_f16<T> && D == 128) ? 2 : 1;
+  constexpr bool TIGHT = D == 128 && KS == 1;                 // addresses are made where they are used, not kept in registers
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int order = sh.order[lane];
-  Part pt;
-  if ((int)blockIdx.x < sp.shared_blocks) {
-    if (!find_shared<KT>(sh, (int)blockIdx.x, sp.rb, sp.spare, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
-  } else {
-    Work wk;
-    if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
-      return;
-    const int rows = min(sp.own_split, ((wk.rows + wk.parts - 1) / wk.parts + KT - 1) / KT * KT);    // (as above)
-    pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, 0, sh.g, KT / 32, min(wk.rows - wk.j * rows, rows), wk.s / sh.h,
-          (int)blockIdx.x - sp.shared_blocks, true};
-  }
-  const Segments &seg = pt.own ? own : shared;
   const char *Kh = seg.K + pt.first_row * ROWB, *Vh = seg.V + pt.first_row * ROWB;
-  const int c = pt.s % sh.h, n = pt.n, ks = pt.ks;
+  const int c = pt.s % sh.h, n = pt.n;
 
-  const int w0 = pt.row + 32 * (wv / ks), m_row = min(w0 + l32, pt.M - 1);      // the wavefront's first query row, this lane's
+  const int w0 = pt.row + 32 * (wv / KS), m_row = min(w0 + l32, pt.M - 1);      // the wavefront's first query row, this lane's
   const bool idle = w0 >= pt.M;
   const int b = pt.own ? pt.first : __shfl(order, pt.first + m_row / sh.g);
   const char *Qh = q + ((long long)(b * sh.h + c) * sh.g + m_row % sh.g) * ROWB;
@@ -265,7 +247,7 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
     const int end = n - 1 - t * KT;
     int here = lane;
-    asm volatile("" : "+v"(here));             // (addresses are made here, not kept in registers)
+    if (TIGHT) asm volatile("" : "+v"(here));
 #pragma unroll
     for (int i = 0; i < TL::LOADS; ++i) {
       const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH;
@@ -304,12 +286,12 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     }
     return (part[0] + part[1]) + (part[2] + part[3]);
   };
-  // N times 32 keys of the tile t, `apart` from each other: all the logits, all the weights, then the sums, with nothing but the rare move of
+  // 32 keys of tile t, or two times 32: all the logits, all the weights, then the sums, with nothing but the rare move of
   // the reference in between, so that the matrix instructions of one run beside the vector instructions of another.
-  auto add_keys = [&](auto many, int t, int kk, int apart) __attribute__((always_inline)) {
-    constexpr int N = decltype(many)::value;
+  auto add_keys = [&](int t, int kk) __attribute__((always_inline)) {
+    constexpr int N = PAIR, apart = KS;
     int here = lane;
-    asm volatile("" : "+v"(here));             // (addresses are made here, not kept in registers)
+    if (TIGHT) asm volatile("" : "+v"(here));
     const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
     floatx16 sc[N];
 #pragma unroll
@@ -358,12 +340,10 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   for (int t = 0; t < tiles; ++t) {
     await(t);
     if (idle) continue;
-    const int mine = wv % ks;                  // this wavefront's 32 keys of the tile, and every ks-th 32 from there
-    if (PAIRS && 2 * ks <= KT / 32) {
-      for (int kk = mine; kk < KT / 32 && n - t * KT - 32 * kk > 0; kk += 2 * ks) add_keys(std::integral_constant<int, 2>{}, t, kk, ks);
-    } else {
-      for (int kk = mine; kk < KT / 32 && n - t * KT - 32 * kk > 0; kk += ks) add_keys(std::integral_constant<int, 1>{}, t, kk, ks);
-    }
+    // (this wavefront's 32 keys of the tile are every KS-th 32)
+#pragma unroll
+    for (int k = 0; k < KT / 32; k += PAIR * KS)
+      if (n - t * KT - 32 * (wv % KS + k) > 0) add_keys(t, wv % KS + k);
   }
   l += other_half(l);
   if constexpr (W::SUMS == 2) {
@@ -392,7 +372,7 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
         await(t);
         if (idle) continue;
 #pragma nounroll
-        for (int kk = wv % ks; kk < KT / 32; kk += ks) {
+        for (int kk = wv % KS; kk < KT / 32; kk += KS) {
           if (n - t * KT - 32 * kk <= 0) break;
           // (the rows past the end repeat the last one, so their weights may stay)
           const floatx16 sc = tile_logits<T, TL>(tiles_lds[0][t % 2] + kk * 32 * CH, qf, l32, half);
@@ -413,25 +393,25 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   }
   m -= BIAS<T>;
 
-  if (ks > 1) {
+  if constexpr (KS > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place
     typedef float Shared[CB * 16][64];
-    static_assert((4 - 128 / KT) * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
+    static_assert((4 - 4 / KS) * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
     Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
-    float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 4 - 128 / KT);
-    const int place = wv / ks * (ks - 1) - 1;                  // + 1 .. ks - 1
+    float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 4 - 4 / KS);
+    const int place = wv / KS * (KS - 1) - 1;                  // + 1 .. KS - 1
     meet();
-    if (wv % ks) {
+    if (wv % KS) {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) others[place + wv % ks][cb * 16 + i][lane] = acc[0][cb][i];
-      ml[place + wv % ks][lane] = make_float2(m, l);
+        for (int i = 0; i < 16; ++i) others[place + wv % KS][cb * 16 + i][lane] = acc[0][cb][i];
+      ml[place + wv % KS][lane] = make_float2(m, l);
     }
     __syncthreads();
-    if (wv % ks) return;
-#pragma nounroll
-    for (int k = 1; k < ks; ++k) {
+    if (wv % KS) return;
+#pragma unroll
+    for (int k = 1; k < KS; ++k) {
       const float2 other = ml[place + k][lane];
       const float mn = fmaxf(m, other.x), f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(other.x - mn);
       m = mn;
@@ -444,14 +424,38 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   }
 
   if (w0 + l32 >= pt.M) return;
-  const long long place = (long long)pt.out * (pt.own ? sh.g : sp.rb) + w0 - pt.row + l32;
-  float *dst = (pt.own ? sums.own_acc : sums.shared_acc) + place * D + 4 * half;
+  const long long place = (long long)pt.out * stride + w0 - pt.row + l32;
+  float *dst = part_acc + place * D + 4 * half;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       *reinterpret_cast<float4 *>(dst + 32 * cb + 8 * k) = make_float4(acc[0][cb][4 * k], acc[0][cb][4 * k + 1], acc[0][cb][4 * k + 2], acc[0][cb][4 * k + 3]);
-  if (half == 0) (pt.own ? sums.own_ml : sums.shared_ml)[place] = make_float2(m, l);
+  if (half == 0) part_ml[place] = make_float2(m, l);
+}
+
+template <typename T, int D, int KS>
+__global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_attn_kernel(Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q,
+                                                                                         Segments shared, Segments own, PrefixSums sums) {
+  typedef Rows<T, D> TL;
+  constexpr int KT = TL::KT, OWN = KT / 32;                    // (own segments have up to 8 query rows)
+  static_assert(TL::TURNS == 2, "the next tile has a place of its own");
+  __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
+  __shared__ int sh_bad[4], sh_scan[24];
+  const int order = sh.order[threadIdx.x & 63];
+  Part pt;
+  if ((int)blockIdx.x < sp.shared_blocks) {
+    if (!find_shared<KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
+    sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, tiles_lds, sh_bad);
+  } else {
+    Work wk;
+    if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
+      return;
+    const int rows = min(sp.own_split, ((wk.rows + wk.parts - 1) / wk.parts + KT - 1) / KT * KT);    // (as above)
+    pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, 0, sh.g, min(wk.rows - wk.j * rows, rows),
+          (int)blockIdx.x - sp.shared_blocks, wk.s / sh.h, true};
+    sum_part<T, D, OWN>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, sh.g, tiles_lds, sh_bad);
+  }
 }
 
 // One workgroup per (own segment, query head of its group) merges the parts of the head's own segment, of the shared one and the row that the call
@@ -486,12 +490,15 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
   int cnt = mine.y;
   long long first = 0, step = 0;
   // (a shared segment without rows has no entry)
-  if (p != Sharing::NONE && shared.seg_len[p * sh.h + c] > 0 && shared.cu[p * sh.h + c + 1] - shared.cu[p * sh.h + c] + shared.headroom > 0) {
-    const int4 e = sums.shared_tab[p * sh.h + c];              // first partial of the first block of rows, parts, from one block to the next
+  if (p != Sharing::NONE) {
+    const int t = p * sh.h + c, len = shared.seg_len[t], cap = shared.cu[t + 1] - shared.cu[t] + shared.headroom;
+    const int4 e = sums.shared_tab[t];         // first partial of the first block of rows, parts, from one block to the next
     const int row = sh.place[b] * sh.g + gi;
-    cnt += e.y;
-    first = ((long long)e.x + row / rb * e.z) * rb + row % rb;
-    step = rb;
+    if (len > 0 && cap > 0) {
+      cnt += e.y;
+      first = ((long long)e.x + row / rb * e.z) * rb + row % rb;
+      step = rb;
+    }
   }
   const int e4 = tid % LPE, slot = tid / LPE;
   float m = M_INIT, l = 0.0f;
@@ -553,8 +560,13 @@ void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const voi
                 const Segments &own, int *seg_len, int *overflow, float *out, float *lse, char *ws, hipStream_t s) {
   const PrefixSums sums = {(float *)(ws + pl.shared_acc), (float *)(ws + pl.own_acc), (float2 *)(ws + pl.shared_ml), (float2 *)(ws + pl.own_ml),
                            (int4 *)(ws + pl.shared_tab), (int4 *)(ws + pl.own_tab)};
-  ADAKV_LAUNCH("prefix_attn", (prefix_attn_kernel<T, D>), dim3(pl.split.shared_blocks + pl.own_blocks), dim3(256), s, sh, pl.split, c_log2,
-               (const char *)q, shared, own, sums);
+#define ADAKV_PREFIX(KS)                                                                                                              \
+  ADAKV_LAUNCH(KS == 1 ? "prefix_attn" : KS == 2 ? "prefix_attn_2" : "prefix_attn_4", (prefix_attn_kernel<T, D, KS>),                  \
+               dim3(pl.split.shared_blocks + pl.own_blocks), dim3(256), s, sh, pl.split, c_log2, (const char *)q, shared, own, sums)
+  if (pl.split.rb == 128) ADAKV_PREFIX(1);
+  else if (pl.split.rb == 64) ADAKV_PREFIX(2);
+  else if constexpr (Rows<T, D>::KT == 128) ADAKV_PREFIX(4);   // (32 rows: plan_prefix)
+#undef ADAKV_PREFIX
   ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, sh.g), dim3(256), s, sh, pl.split.rb, c_log2,
                (const char *)q, (const char *)k_new, (const char *)v_new, shared, own, seg_len, overflow, sums, out, lse);
 }
@@ -593,8 +605,8 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
     n += (long long)blocks_of(p) * dm.h_kv;
     if (blocks_of(p) > 1) padding += 7ll * blocks_of(p);
   }
-  const long long want = 256;
-  pl.split.spare = (int)(want - n > n / 2 + 1 ? want - n : n / 2 + 1);
+  const long long want = rb == 128 ? 512 - n : 256;
+  pl.split.spare = (int)(want > n / 2 + 1 ? want : n / 2 + 1);
   pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
   const int tile = dm.d == 64 && dtype != ADAKV_FP32 ? 128 : 64;
   const long long nseg = (long long)sh.groups * dm.h_kv, own = (long long)st.batch * dm.h_kv;
