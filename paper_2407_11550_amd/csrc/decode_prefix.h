@@ -7,12 +7,10 @@ namespace adakv {
 
 // Which sequences share which cache, passed to kernels by value.
 struct Sharing {
-  static constexpr unsigned char NONE = 255;
   int groups, h, g;
   unsigned char order[ADAKV_MAX_BATCH];        // sequences, those of a shared cache one after the other
   unsigned char first[ADAKV_MAX_BATCH + 1];    // of a shared cache among them
-  unsigned char group[ADAKV_MAX_BATCH];        // a sequence's shared cache, or NONE
-  unsigned char place[ADAKV_MAX_BATCH];        // and which of that cache's sequences it is
+  int whose[ADAKV_MAX_BATCH];                  // a sequence's shared cache, and 256 times which of that cache's sequences it is; or -1
 };
 // A flattened cache with head-room.
 struct Segments {

@@ -123,17 +123,21 @@ template <typename T, int D, typename TL> struct Weights {
   }
 };
 
-// Elements 4 e .. 4 e + 3 of a row, in 32 bits.
-template <typename T> __device__ __forceinline__ void load4(const char *row, int e, float (&f)[4]) {
-  if constexpr (is_f32<T>) {
-    const float4 x = reinterpret_cast<const float4 *>(row)[e];
-    f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
-  } else {
-    const uint2 x = reinterpret_cast<const uint2 *>(row)[e];
-    f[0] = half_of<T>(x.x & 0xffffu); f[1] = half_of<T>(x.x >> 16);
-    f[2] = half_of<T>(x.y & 0xffffu); f[3] = half_of<T>(x.y >> 16);
+// Elements 4 e .. 4 e + 3 of a row as they are in memory.
+template <typename T> struct Four {
+  typedef unsigned Words __attribute__((ext_vector_type(is_f32<T> ? 4 : 2)));
+  Words w;
+  __device__ __forceinline__ void load(const char *row, int e) { w = reinterpret_cast<const Words *>(row)[e]; }
+  __device__ __forceinline__ void store(char *row, int e) const { reinterpret_cast<Words *>(row)[e] = w; }
+  __device__ __forceinline__ void widen(float (&f)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned word = w[is_f32<T> ? i : i / 2];
+      if constexpr (is_f32<T>) f[i] = __uint_as_float(word);
+      else f[i] = half_of<T>(i % 2 ? word >> 16 : word & 0xffffu);
+    }
   }
-}
+};
 
 // What a workgroup works on: n keys from row `first_row` of the cache on, of segment s, for query rows from `row` on of the M that look at it.
 struct Part {
@@ -470,37 +474,29 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
   __shared__ float sh_a[NSLOT][D];
   __shared__ float sh_m[NSLOT], sh_l[NSLOT];
   const int tid = threadIdx.x, s = blockIdx.x, gi = blockIdx.y, b = s / sh.h, c = s % sh.h;
-  const int p = sh.group[b];
+  const int e4 = tid % LPE, slot = tid / LPE;
+  const long long row = (long long)s * sh.g + gi;
+  // everything that follows from the workgroup's number alone is asked for at once: one wait after the other is what the kernel's time is
+  const int whose = sh.whose[b], from = own.cu[s], to = own.cu[s + 1];
   const int4 mine = sums.own_tab[s];           // first partial, partials, rows
-  const int from = own.cu[s];
-  // (the length is what the other kernel saw: this one writes the new one)
-  const bool room = k_new && mine.z < own.cu[s + 1] - from + own.headroom;
-  if (k_new && gi == 0) {
-    const long long at = ((long long)from + (long long)s * own.headroom + mine.z) * ROWB;
-    if (room && tid < 2 * (ROWB / 16)) {
-      const int col = tid % (ROWB / 16) * 16;
-      const bool v = tid >= ROWB / 16;
-      *reinterpret_cast<u32x4 *>(const_cast<char *>(v ? own.V : own.K) + at + col) = *reinterpret_cast<const u32x4 *>((v ? v_new : k_new) + (long long)s * ROWB + col);
-    }
-    if (tid == 0) {
-      if (room) new_len[s] = mine.z + 1;
-      else if (overflow) *overflow = 1;        // the segment was full, its new row was dropped
-    }
+  Four<T> q4, k4, v4;
+  if (k_new) {
+    q4.load(q + row * ROWB, e4);
+    k4.load(k_new + (long long)s * ROWB, e4);
+    v4.load(v_new + (long long)s * ROWB, e4);
   }
   int cnt = mine.y;
   long long first = 0, step = 0;
-  // (a shared segment without rows has no entry)
-  if (p != Sharing::NONE) {
-    const int t = p * sh.h + c, len = shared.seg_len[t], cap = shared.cu[t + 1] - shared.cu[t] + shared.headroom;
+  if (whose >= 0) {
+    const int t = (whose & 255) * sh.h + c, len = shared.seg_len[t], cap = shared.cu[t + 1] - shared.cu[t] + shared.headroom;
     const int4 e = sums.shared_tab[t];         // first partial of the first block of rows, parts, from one block to the next
-    const int row = sh.place[b] * sh.g + gi;
-    if (len > 0 && cap > 0) {
+    const int r = (whose >> 8) * sh.g + gi;
+    if (len > 0 && cap > 0) {                  // (a shared segment without rows has no entry)
       cnt += e.y;
-      first = ((long long)e.x + row / rb * e.z) * rb + row % rb;
+      first = ((long long)e.x + r / rb * e.z) * rb + r % rb;
       step = rb;
     }
   }
-  const int e4 = tid % LPE, slot = tid / LPE;
   float m = M_INIT, l = 0.0f;
   float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   auto add = [&](float om, float ol, const float4 &oa) {
@@ -525,16 +521,26 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
 #pragma unroll
     for (int u = 0; u < UC; ++u) add(ml[u].x, ml[u].y, pa[u]);
   }
-  const long long row = (long long)s * sh.g + gi;
+  // (the length is what the other kernel saw: this one writes the new one)
+  const bool room = k_new && mine.z < to - from + own.headroom;
   if (room && slot == cnt % NSLOT) {           // the appended row: one of weight 1 at its logit
     float x[4], k[4], v[4];
-    load4<T>(q + row * ROWB, e4, x);
-    load4<T>(k_new + (long long)s * ROWB, e4, k);
-    load4<T>(v_new + (long long)s * ROWB, e4, v);
+    q4.widen(x);
+    k4.widen(k);
+    v4.widen(v);
     float dot = fmaf(x[0], k[0], x[1] * k[1]) + fmaf(x[2], k[2], x[3] * k[3]);
 #pragma unroll
     for (int o = 1; o < LPE; o <<= 1) dot += __shfl_xor(dot, o);
     add(dot * c_log2, 1.0f, make_float4(v[0], v[1], v[2], v[3]));
+  }
+  if (k_new && gi == 0) {
+    const long long at = ((long long)from + (long long)s * own.headroom + mine.z) * ROWB;
+    if (room && slot == 0) k4.store(const_cast<char *>(own.K) + at, e4);
+    if (room && slot == 1) v4.store(const_cast<char *>(own.V) + at, e4);
+    if (tid == 0) {
+      if (room) new_len[s] = mine.z + 1;
+      else if (overflow) *overflow = 1;        // the segment was full, its new row was dropped
+    }
   }
   const int all = cnt + room, live = all < NSLOT ? all : NSLOT;                // slots that had any
   if (slot < live) {
@@ -579,13 +585,12 @@ Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of) {
   sh.h = dm.h_kv;
   sh.g = dm.g;
   int at = 0;
-  for (int b = 0; b < st.batch; ++b) sh.group[b] = Sharing::NONE;
+  for (int b = 0; b < st.batch; ++b) sh.whose[b] = -1;
   for (int p = 0; p < groups; ++p) {
     sh.first[p] = (unsigned char)at;
     for (int b = 0; b < st.batch; ++b)
       if (of[b] == p) {
-        sh.group[b] = (unsigned char)p;
-        sh.place[b] = (unsigned char)(at - sh.first[p]);
+        sh.whose[b] = p | (at - sh.first[p]) << 8;
         sh.order[at++] = (unsigned char)b;
       }
   }
@@ -605,7 +610,7 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
     n += (long long)blocks_of(p) * dm.h_kv;
     if (blocks_of(p) > 1) padding += 7ll * blocks_of(p);
   }
-  const long long want = rb == 128 ? 512 - n : 256;
+  const long long want = 256;
   pl.split.spare = (int)(want > n / 2 + 1 ? want : n / 2 + 1);
   pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
   const int tile = dm.d == 64 && dtype != ADAKV_FP32 ? 128 : 64;
