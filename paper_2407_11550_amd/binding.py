@@ -146,7 +146,7 @@ def load_library():
         _marshal = _load_marshal()
     _decode_step_address = ctypes.cast(lib.adakv_decode_step, V).value
     for name in ("decode_window_step", "decode_step_q8", "cache_build_q8", "window_attn", "cache_move", "cache_move_q8", "rotary",
-                 "norm_rotary", "decode_prefix_step"):
+                 "norm_rotary", "decode_prefix_step", "decode_prefix_attn"):
         _addresses[name] = ctypes.cast(getattr(lib, "adakv_" + name), V).value
     _lib = lib
     return lib
@@ -881,6 +881,10 @@ def _decode_prefix(name, layer, q_new, new, cu_seqlens, headroom, K_cache, V_cac
 def decode_prefix_attn(layer: Layer, q_new, cu_seqlens, headroom, K_cache, V_cache, seg_len, prefix: Prefix, out=None, lse=None, ws=None,
                        stream=None, want_lse=False):
     """adakv_decode_prefix_attn: decode_attn over the sequences' shared caches and their own."""
+    if (lse is not None or not want_lse) and _native("decode_prefix_attn", layer, stream, q_new, None, None, cu_seqlens, headroom, K_cache,
+                                                     V_cache, seg_len, None, prefix._address, prefix.device, len(prefix.of), out, lse, ws,
+                                                     check="decode_prefix"):
+        return out if lse is None else (out, lse)
     return _decode_prefix("adakv_decode_prefix_attn", layer, q_new, (), cu_seqlens, headroom, K_cache, V_cache, seg_len, (), prefix, out, lse,
                           ws, stream, want_lse)
 
@@ -889,7 +893,8 @@ def decode_prefix_step(layer: Layer, q_new, k_new, v_new, cu_seqlens, headroom, 
                        out=None, lse=None, ws=None, stream=None, want_lse=False):
     """adakv_decode_prefix_step: append k_new/v_new to every sequence's own segments and attend over the shared caches and these."""
     if (lse is not None or not want_lse) and _native("decode_prefix_step", layer, stream, q_new, k_new, v_new, cu_seqlens, headroom, K_cache,
-                                                     V_cache, seg_len, overflow, prefix._address, prefix.device, len(prefix.of), out, lse, ws):
+                                                     V_cache, seg_len, overflow, prefix._address, prefix.device, len(prefix.of), out, lse, ws,
+                                                     check="decode_prefix"):
         return out if lse is None else (out, lse)
     return _decode_prefix("adakv_decode_prefix_step", layer, q_new, (k_new, v_new), cu_seqlens, headroom, K_cache, V_cache, seg_len,
                           (overflow,), prefix, out, lse, ws, stream, want_lse)

@@ -7,7 +7,7 @@ namespace adakv {
 
 // Which sequences share which cache, passed to kernels by value.
 struct Sharing {
-  int groups, h, g;
+  int groups, h, log_g;                        // shared caches; KV heads; query heads to one of them, a power of two
   unsigned char order[ADAKV_MAX_BATCH];        // sequences, those of a shared cache one after the other
   unsigned char first[ADAKV_MAX_BATCH + 1];    // of a shared cache among them
   int whose[ADAKV_MAX_BATCH];                  // a sequence's shared cache, and 256 times which of that cache's sequences it is; or -1

@@ -142,10 +142,18 @@ template <typename T> struct Four {
 // What a workgroup works on: n keys from row `first_row` of the cache on, of segment s, for query rows from `row` on of the M that look at it.
 struct Part {
   long long first_row;
-  int s, row, M, n;
+  int s, c, row, M, n;                         // (c: the segment's head)
   int out, first;                              // where its sums go; the segment's first sequence in Sharing::order, or its only one
   bool own;
 };
+// a / b of numbers whose quotient is below 2^22: the reciprocal is off by 2^-22 of it at most, which is less than one.  (The compiler's divisions took 0.4 us
+// of the search below.)
+__device__ __forceinline__ int quotient(int a, int b) {
+  const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
+  return q + (r >= b) - (r < 0);
+}
+__device__ __forceinline__ int quotient_up(int a, int b) { return quotient(a + b - 1, b); }
+
 // Finds a part of a shared segment, as find_work does in decode_parts.h from a prefix sum, over the segments, of the parts that their lengths make; but
 // a part is as long as it has to be for all of them to be `spare` and one for each segment at most, whatever the capacities are: the
 // call lasts as long as its longest part.
@@ -157,7 +165,7 @@ template <int TILE, int RB>
 __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spare, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
   const int h = sh.h, groups = sh.groups, nseg = groups * h, lane = threadIdx.x & 63;
   const int my_first = sh.first[lane], my_many = lane < groups ? sh.first[lane + 1] - my_first : 0;    // of shared cache `lane`
-  const int my_blocks = (my_many * sh.g + RB - 1) / RB;
+  const int my_blocks = ((my_many << sh.log_g) + RB - 1) / RB;
   int from, len;
   auto look = [&](int s) {                     // at a segment
     from = cu[s];
@@ -169,10 +177,10 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
   int tiles = 0, split, my_parts = 0, upto = 0;
   if (few) {
     tiles = look(min(lane, nseg - 1));
-    const int blocks = __shfl(my_blocks, min(lane, nseg - 1) / h);             // (of all lanes: one that is off has nothing to give)
+    const int blocks = __shfl(my_blocks, quotient(min(lane, nseg - 1), h));             // (of all lanes: one that is off has nothing to give)
     const int all = wave_sum(lane < nseg ? tiles * blocks : 0);
-    split = max(1, (all + spare - 1) / spare);                 // tiles a part
-    const int parts = lane < nseg && blocks > 0 ? (tiles + split - 1) / split : 0;
+    split = max(1, quotient_up(all, spare));                   // tiles a part
+    const int parts = lane < nseg && blocks > 0 ? quotient_up(tiles, split) : 0;
     upto = wave_scan_incl(parts);
     const int last = __shfl(upto, min(lane * h + h - 1, 63)), before = __shfl(upto, max(min(lane * h, 64) - 1, 0));
     my_parts = lane < groups ? last - (lane ? before : 0) : 0;
@@ -181,9 +189,9 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
 #pragma unroll 4
     for (int c = 0; c < h; ++c) mine += look(min(lane, groups - 1) * h + c);
     const int all = wave_sum(mine * my_blocks);
-    split = max(1, (all + spare - 1) / spare);
+    split = max(1, quotient_up(all, spare));
 #pragma unroll 4
-    for (int c = 0; c < h; ++c) my_parts += (look(min(lane, groups - 1) * h + c) + split - 1) / split;
+    for (int c = 0; c < h; ++c) my_parts += quotient_up(look(min(lane, groups - 1) * h + c), split);
     my_parts = my_blocks > 0 ? my_parts : 0;
   }
   const int size = my_blocks > 1 ? my_blocks * ((my_parts + 7) / 8 * 8) : my_parts, end = wave_scan_incl(size);
@@ -191,7 +199,8 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
   if (here == 0) return false;
   const int p = __ffsll(here) - 1, base = __builtin_amdgcn_readlane(end - size, p), blocks = __builtin_amdgcn_readlane(my_blocks, p);
   const int count = __builtin_amdgcn_readlane(my_parts, p), at = blk - base;
-  const int i = blocks > 1 ? at / (8 * blocks) * 8 + at % 8 : at, block = blocks > 1 ? at / 8 % blocks : 0;    // which part of the cache's
+  const int eights = blocks > 1 ? quotient(at / 8, blocks) : 0;
+  const int i = blocks > 1 ? eights * 8 + at % 8 : at, block = blocks > 1 ? at / 8 - eights * blocks : 0;    // which part of the cache's
   if (i >= count) return false;
   int before;                                  // parts in front of the segment's, in its cache
   if (few) {
@@ -201,19 +210,20 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
     before = (L ? __builtin_amdgcn_readlane(upto, L - 1) : 0) - shift;
   } else {
     tiles = look(p * h + min(lane, h - 1));
-    upto = wave_scan_incl(lane < h ? (tiles + split - 1) / split : 0);
+    upto = wave_scan_incl(lane < h ? quotient_up(tiles, split) : 0);
     const int L = __ffsll(__ballot(upto > i)) - 1;
     pt.s = p * h + L;
     before = L ? __builtin_amdgcn_readlane(upto, L - 1) : 0;
   }
-  const int L = few ? pt.s : pt.s - p * h, j = i - before, all = __builtin_amdgcn_readlane(tiles, L), parts = (all + split - 1) / split;
-  const int rows = (all + parts - 1) / parts * TILE, held = __builtin_amdgcn_readlane(len, L);       // equal parts, none of them empty
+  const int L = few ? pt.s : pt.s - p * h, j = i - before, all = __builtin_amdgcn_readlane(tiles, L), parts = quotient_up(all, split);
+  const int rows = quotient_up(all, parts) * TILE, held = __builtin_amdgcn_readlane(len, L);       // equal parts, none of them empty
   pt.first_row = (long long)__builtin_amdgcn_readlane(from, L) + (long long)pt.s * headroom + (long long)j * rows;
   pt.n = min(held - j * rows, rows);
   pt.row = block * RB;
   pt.out = base + block * count + i;
   pt.first = __builtin_amdgcn_readlane(my_first, p);
-  pt.M = __builtin_amdgcn_readlane(my_many, p) * sh.g;
+  pt.M = __builtin_amdgcn_readlane(my_many, p) << sh.log_g;
+  pt.c = pt.s - p * h;
   pt.own = false;
   if (j == 0 && block == 0 && threadIdx.x == 0) tab[pt.s] = make_int4(base + before, parts, count, held);
   return true;
@@ -234,12 +244,12 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const char *Kh = seg.K + pt.first_row * ROWB, *Vh = seg.V + pt.first_row * ROWB;
-  const int c = pt.s % sh.h, n = pt.n;
+  const int c = pt.c, n = pt.n;
 
   const int w0 = pt.row + 32 * (wv / KS), m_row = min(w0 + l32, pt.M - 1);      // the wavefront's first query row, this lane's
   const bool idle = w0 >= pt.M;
-  const int b = pt.own ? pt.first : __shfl(order, pt.first + m_row / sh.g);
-  const char *Qh = q + ((long long)(b * sh.h + c) * sh.g + m_row % sh.g) * ROWB;
+  const int b = pt.own ? pt.first : __shfl(order, pt.first + (m_row >> sh.log_g));
+  const char *Qh = q + (((long long)(b * sh.h + c) << sh.log_g) + (m_row & ((1 << sh.log_g) - 1))) * ROWB;
   u32x4 qf[CH / 2];
 #pragma unroll
   for (int s = 0; s < CH / 2; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + (2 * s + half) * 16);
@@ -357,12 +367,12 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 
   // Where a sum is infinite or NaN, a value that is none may have met a weight's lower part of 0, or of the other sign, or a
   // weight of 0 of the rows past the end: once more with the upper parts alone, which say what it is.
-  float worst = 0.0f;
+  float worst[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) worst = fmaf(acc[0][cb][i], 0.0f, worst);
-  const bool bad = __any(!(worst == 0.0f));
+    for (int i = 0; i < 16; ++i) worst[i % 4] = fmaf(acc[0][cb][i], 0.0f, worst[i % 4]);
+  const bool bad = __any(!((worst[0] + worst[1]) + (worst[2] + worst[3]) == 0.0f));
   if (lane == 0) sh_bad[wv] = bad;
   __syncthreads();
   if (sh_bad[0] | sh_bad[1] | sh_bad[2] | sh_bad[3]) {
@@ -399,7 +409,7 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 
   if constexpr (KS > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place
-    typedef float Shared[CB * 16][64];
+    typedef float4 Shared[CB * 4][64];
     static_assert((4 - 4 / KS) * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
     Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
     float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 4 - 4 / KS);
@@ -409,7 +419,8 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) others[place + wv % KS][cb * 16 + i][lane] = acc[0][cb][i];
+        for (int k = 0; k < 4; ++k)
+          others[place + wv % KS][cb * 4 + k][lane] = make_float4(acc[0][cb][4 * k], acc[0][cb][4 * k + 1], acc[0][cb][4 * k + 2], acc[0][cb][4 * k + 3]);
       ml[place + wv % KS][lane] = make_float2(m, l);
     }
     __syncthreads();
@@ -423,7 +434,12 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0][cb][i] = acc[0][cb][i] * f0 + others[place + k][cb * 16 + i][lane] * f1;
+        for (int x = 0; x < 4; ++x) {
+          const float4 o = others[place + k][cb * 4 + x][lane];
+          const float four[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[0][cb][4 * x + i] = acc[0][cb][4 * x + i] * f0 + four[i] * f1;
+        }
     }
   }
 
@@ -455,10 +471,11 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     Work wk;
     if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
       return;
-    const int rows = min(sp.own_split, ((wk.rows + wk.parts - 1) / wk.parts + KT - 1) / KT * KT);    // (as above)
-    pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, 0, sh.g, min(wk.rows - wk.j * rows, rows),
-          (int)blockIdx.x - sp.shared_blocks, wk.s / sh.h, true};
-    sum_part<T, D, OWN>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, sh.g, tiles_lds, sh_bad);
+    const int rows = min(sp.own_split, (quotient_up(wk.rows, wk.parts) + KT - 1) / KT * KT);           // (as above)
+    const int b = quotient(wk.s, sh.h), g = 1 << sh.log_g;
+    pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, wk.s - b * sh.h, 0, g, min(wk.rows - wk.j * rows, rows),
+          (int)blockIdx.x - sp.shared_blocks, b, true};
+    sum_part<T, D, OWN>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds, sh_bad);
   }
 }
 
@@ -466,16 +483,16 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
 // appends, which are one list of partial results, and normalises.  They are merged NSLOT side by side, each by D/4 lanes, then across slots.  The
 // first head's workgroup puts the row into the cache.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb, float c_log2, const char *__restrict__ q, const char *__restrict__ k_new,
+__global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int log_rb, float c_log2, const char *__restrict__ q, const char *__restrict__ k_new,
                                                              const char *__restrict__ v_new, Segments shared, Segments own, int *new_len,
                                                              int *__restrict__ overflow, PrefixSums sums, float *__restrict__ out,
                                                              float *__restrict__ lse) {
   constexpr int LPE = D / 4, NSLOT = 256 / LPE, UC = 4, ROWB = D * T::SIZE;
   __shared__ float sh_a[NSLOT][D];
   __shared__ float sh_m[NSLOT], sh_l[NSLOT];
-  const int tid = threadIdx.x, s = blockIdx.x, gi = blockIdx.y, b = s / sh.h, c = s % sh.h;
-  const int e4 = tid % LPE, slot = tid / LPE;
-  const long long row = (long long)s * sh.g + gi;
+  const int tid = threadIdx.x, s = blockIdx.x, gi = blockIdx.y, b = quotient(s, sh.h), c = s - b * sh.h;
+  const int e4 = tid % LPE, slot = tid / LPE, rb = 1 << log_rb;
+  const long long row = ((long long)s << sh.log_g) + gi;
   // everything that follows from the workgroup's number alone is asked for at once: one wait after the other is what the kernel's time is
   const int whose = sh.whose[b], from = own.cu[s], to = own.cu[s + 1];
   const int4 mine = sums.own_tab[s];           // first partial, partials, rows
@@ -490,10 +507,10 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
   if (whose >= 0) {
     const int t = (whose & 255) * sh.h + c, len = shared.seg_len[t], cap = shared.cu[t + 1] - shared.cu[t] + shared.headroom;
     const int4 e = sums.shared_tab[t];         // first partial of the first block of rows, parts, from one block to the next
-    const int r = (whose >> 8) * sh.g + gi;
+    const int r = ((whose >> 8) << sh.log_g) + gi;
     if (len > 0 && cap > 0) {                  // (a shared segment without rows has no entry)
       cnt += e.y;
-      first = ((long long)e.x + r / rb * e.z) * rb + r % rb;
+      first = ((long long)e.x + (r >> log_rb) * e.z << log_rb) + (r & (rb - 1));
       step = rb;
     }
   }
@@ -513,7 +530,7 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int rb,
     for (int u = 0; u < UC; ++u) {
       const int i = i0 + u * NSLOT, ii = i < cnt ? i : i0;
       const bool of_own = ii < mine.y;
-      const long long at = of_own ? (long long)(mine.x + ii) * sh.g + gi : first + (ii - mine.y) * step;
+      const long long at = of_own ? ((long long)(mine.x + ii) << sh.log_g) + gi : first + (ii - mine.y) * step;
       ml[u] = (of_own ? sums.own_ml : sums.shared_ml)[at];
       pa[u] = *reinterpret_cast<const float4 *>((of_own ? sums.own_acc : sums.shared_acc) + at * D + e4 * 4);
       if (i >= cnt) { ml[u] = make_float2(M_INIT, 0.0f); pa[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
@@ -573,7 +590,8 @@ void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const voi
   else if (pl.split.rb == 64) ADAKV_PREFIX(2);
   else if constexpr (Rows<T, D>::KT == 128) ADAKV_PREFIX(4);   // (32 rows: plan_prefix)
 #undef ADAKV_PREFIX
-  ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, sh.g), dim3(256), s, sh, pl.split.rb, c_log2,
+  ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, 1 << sh.log_g), dim3(256), s, sh,
+               pl.split.rb == 128 ? 7 : pl.split.rb == 64 ? 6 : 5, c_log2,
                (const char *)q, (const char *)k_new, (const char *)v_new, shared, own, seg_len, overflow, sums, out, lse);
 }
 
@@ -583,7 +601,7 @@ Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of) {
   Sharing sh = {};
   sh.groups = groups;
   sh.h = dm.h_kv;
-  sh.g = dm.g;
+  sh.log_g = dm.g == 8 ? 3 : dm.g / 2;
   int at = 0;
   for (int b = 0; b < st.batch; ++b) sh.whose[b] = -1;
   for (int p = 0; p < groups; ++p) {
@@ -600,7 +618,7 @@ Sharing share(const SeqTab &st, const Dims &dm, int groups, const int *of) {
 
 PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom, const Sharing &sh) {
   PrefixPlan pl = {};
-  const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) * sh.g; };
+  const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) << sh.log_g; };
   int most = 0;
   for (int p = 0; p < sh.groups; ++p) most = rows_of(p) > most ? rows_of(p) : most;
   const int rb = pl.split.rb = most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;

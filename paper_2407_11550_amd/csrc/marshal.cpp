@@ -200,13 +200,20 @@ PyObject *decode_window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // (device, function, layer, q, k, v, cu_seqlens, headroom, K_cache, V_cache, seg_len, overflow, shared caches, their device, sequences that
-// they are given for, out, lse, ws, stream)
-PyObject *decode_prefix_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return checked("decode_prefix_step", n, 19, a, [](Args &x) {
-    const auto fn = reinterpret_cast<decltype(&adakv_decode_prefix_step)>(x.pointer());
+// they are given for, out, lse, ws, stream); k and v are None for the function that appends nothing
+PyObject *decode_prefix(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return checked("decode_prefix", n, 19, a, [](Args &x) {
+    void *fn = x.pointer();
     const Layer l(x);
     const adakv_layer *L = l.L;
-    void *q = x.rows(l.type, L->batch, L->h_q, L->d), *k = x.rows(l.type, L->batch, L->h_kv, L->d), *v = x.rows(l.type, L->batch, L->h_kv, L->d);
+    void *q = x.rows(l.type, L->batch, L->h_q, L->d), *k = nullptr, *v = nullptr;
+    if (x.a[x.at] != Py_None) {
+      k = x.rows(l.type, L->batch, L->h_kv, L->d);
+      v = x.rows(l.type, L->batch, L->h_kv, L->d);
+    } else {
+      if (x.a[x.at + 1] != Py_None) throw Refused();
+      x.at += 2;
+    }
     const int32_t *cu = x.data<int32_t>(at::kInt, l.nseg + 1);
     const int32_t headroom = x.i32();
     void *K = x.cache(l.type, l.rows(headroom), L->d), *V = x.cache(l.type, l.rows(headroom), L->d);
@@ -217,7 +224,10 @@ PyObject *decode_prefix_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor &ws = x.buffer(at::kByte, 0);
     const size_t ws_bytes = (size_t)ws.numel();
     void *p = ws.data_ptr(), *stream = x.pointer();
-    return unlocked([&] { return fn(L, q, k, v, cu, headroom, K, V, len, over, P, out, lse, p, ws_bytes, stream); });
+    return unlocked([&] {
+      if (k) return reinterpret_cast<decltype(&adakv_decode_prefix_step)>(fn)(L, q, k, v, cu, headroom, K, V, len, over, P, out, lse, p, ws_bytes, stream);
+      return reinterpret_cast<decltype(&adakv_decode_prefix_attn)>(fn)(L, q, cu, headroom, K, V, len, P, out, lse, p, ws_bytes, stream);
+    });
   });
 }
 
@@ -383,7 +393,7 @@ PyMethodDef methods[] = {
     ADAKV_METHOD(window_attn),
     ADAKV_METHOD(cache_move),
     ADAKV_METHOD(rotary),
-    ADAKV_METHOD(decode_prefix_step),
+    ADAKV_METHOD(decode_prefix),
 #undef ADAKV_METHOD
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
