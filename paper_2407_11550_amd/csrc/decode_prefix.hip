@@ -637,7 +637,12 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
   pl.split.own_segments = (int)own;
   pl.split.own_per = (int)((own + 255) / 256);
   pl.split.own_split = (int)((a_part < tile ? tile : a_part) + tile - 1) / tile * tile;
-  pl.own_blocks = (int)(own_cap / pl.split.own_split + own);
+  long long longest = 0;                       // an own segment's capacity at most
+  for (int b = 0; b < st.batch; ++b) {
+    const long long most_kept = st.Bp[b] < st.n[b] ? st.Bp[b] : st.n[b];
+    longest = most_kept + dm.w + headroom > longest ? most_kept + dm.w + headroom : longest;
+  }
+  pl.own_blocks = (int)(longest <= pl.split.own_split ? own : own_cap / pl.split.own_split + own);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t here = at;
