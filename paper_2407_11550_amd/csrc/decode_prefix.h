@@ -19,9 +19,10 @@ struct Segments {
   int headroom;
 };
 // How segments are split.  Shared ones, which come first: query rows of a workgroup; parts beyond one for each segment and block of rows;
-// workgroups, an upper bound.  Own ones: rows of a part; segments, and how many of them a thread counts.
+// workgroups, an upper bound; what a part's sums cost (tiles_a_part).  Own ones: rows of a part; segments, and how many of them a thread counts.
 struct PrefixSplit {
   int rb, spare, shared_blocks;
+  float sums_cost;
   int own_split, own_segments, own_per;
 };
 // Partial results: sums, maxima and sums of weights, and which are whose.

@@ -154,6 +154,15 @@ __device__ __forceinline__ int quotient(int a, int b) {
 }
 __device__ __forceinline__ int quotient_up(int a, int b) { return quotient(a + b - 1, b); }
 
+// Tiles of a part: at most `spare` parts and one for each segment, which is what the call takes at once; and no fewer than pay for the sums that a part
+// leaves for the merge.  With P tiles a part the call takes P tiles' time and that of all / P parts' sums, least for P^2 = all * sums_cost (the
+// time of a part's sums over a tile's).  us a call with parts of 1 | 2 | 4 tiles, bf16, d = 128, 8 KV heads, g = 4, 100 own rows: 24 sequences over 2000
+// rows a head (all = 250) 22.5 | 17.9 | 19.3, 48 over 2000 (500) 26.2 | 26.1 | 22.2, 48 over 541 (136) 22.5 | 17.9 | 18.4, 24 over 541 (68) 14.6 |
+// 15.4 | 16.4, 16 over 2000 (250) 17.8 | 15.4 | 16.2, 8 over 541 (68) 11.5 | 12.1 | 13.1.
+__device__ __forceinline__ int tiles_a_part(int all, int spare, float sums_cost) {
+  return max(max(1, quotient_up(all, spare)), (int)(__builtin_amdgcn_sqrtf((float)all * sums_cost) + 0.5f));
+}
+
 // Finds a part of a shared segment, as find_work does in decode_parts.h from a prefix sum, over the segments, of the parts that their lengths make; but
 // a part is as long as it has to be for all of them to be `spare` and one for each segment at most, whatever the capacities are: the
 // call lasts as long as its longest part.
@@ -162,7 +171,7 @@ __device__ __forceinline__ int quotient_up(int a, int b) { return quotient(a + b
 // once makes the next ones come two to a compute unit where another has room (512 parts with 50 of those among them: 98 us, behind them 71).
 // The first part's workgroup files the segment's entry.
 template <int TILE, int RB>
-__device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spare, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
+__device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spare, float sums_cost, int headroom, const int *cu, const int *seg_len, int4 *tab, Part &pt) {
   const int h = sh.h, groups = sh.groups, nseg = groups * h, lane = threadIdx.x & 63;
   const int my_first = sh.first[lane], my_many = lane < groups ? sh.first[lane + 1] - my_first : 0;    // of shared cache `lane`
   const int my_blocks = ((my_many << sh.log_g) + RB - 1) / RB;
@@ -179,7 +188,7 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
     tiles = look(min(lane, nseg - 1));
     const int blocks = __shfl(my_blocks, quotient(min(lane, nseg - 1), h));             // (of all lanes: one that is off has nothing to give)
     const int all = wave_sum(lane < nseg ? tiles * blocks : 0);
-    split = max(1, quotient_up(all, spare));                   // tiles a part
+    split = tiles_a_part(all, spare, sums_cost);
     const int parts = lane < nseg && blocks > 0 ? quotient_up(tiles, split) : 0;
     upto = wave_scan_incl(parts);
     const int last = __shfl(upto, min(lane * h + h - 1, 63)), before = __shfl(upto, max(min(lane * h, 64) - 1, 0));
@@ -189,7 +198,7 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
 #pragma unroll 4
     for (int c = 0; c < h; ++c) mine += look(min(lane, groups - 1) * h + c);
     const int all = wave_sum(mine * my_blocks);
-    split = max(1, quotient_up(all, spare));
+    split = tiles_a_part(all, spare, sums_cost);
 #pragma unroll 4
     for (int c = 0; c < h; ++c) my_parts += quotient_up(look(min(lane, groups - 1) * h + c), split);
     my_parts = my_blocks > 0 ? my_parts : 0;
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   const int order = sh.order[threadIdx.x & 63];
   Part pt;
   if ((int)blockIdx.x < sp.shared_blocks) {
-    if (!find_shared<KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
+    if (!find_shared<KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, sp.sums_cost, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
     sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, tiles_lds, sh_bad);
   } else {
     Work wk;
@@ -630,6 +639,10 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
   }
   const long long want = 256;
   pl.split.spare = (int)(want > n / 2 + 1 ? want : n / 2 + 1);
+  // sums of a block's rows, written and read at 5 TB/s, over a tile of 64 rows' (or 128 of 128 bytes) time in a workgroup
+  const int sum_rows = most < rb ? most : rb;
+  const float tile_us = dtype != ADAKV_FP32 ? 1.0f : dm.d == 64 ? 3.0f : 6.0f;
+  pl.split.sums_cost = sum_rows * (dm.d + 2) * 8.0f / 5.0e6f / tile_us;
   pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
   const int tile = dm.d == 64 && dtype != ADAKV_FP32 ? 128 : 64;
   const long long nseg = (long long)sh.groups * dm.h_kv, own = (long long)st.batch * dm.h_kv;
