@@ -168,6 +168,42 @@ def test_more_segments_than_a_wavefront_has_lanes():
     c.check(out, lse, c.own, "140 shared segments")
 
 
+@pytest.mark.parametrize("dtype,d,groups,h", [(BF, 128, 3, 2), (FH, 64, 3, 2), (BF, 64, 9, 8), (FS, 64, 13, 5)])
+def test_shared_caches_of_many_and_of_few(dtype, d, groups, h):
+    """One cache for most sequences, whose query rows make several blocks, others for a few of them, one for none; up to 64 segments and more."""
+    rng = np.random.default_rng(groups)
+    of = [0] * 37 + [1] * 9 + ([int(p) for p in rng.integers(3, groups, size=10)] if groups > 3 else []) + [-1]
+    c = Case(dtype, 8, h, d, of, spread(rng, groups * h, 900), spread(rng, len(of) * h, 20), shared_headroom=3)
+    out, lse = c.attn()
+    c.check(out, lse, c.own, f"{groups} shared caches, {h} heads")
+
+
+@pytest.mark.parametrize("dtype,d,batch,name", [(BF, 128, 4, "prefix_attn_2"), (BF, 64, 4, "prefix_attn_4"), (FH, 128, 4, "prefix_attn_2"), (FH, 64, 4, "prefix_attn_4"),
+                                                (FS, 128, 4, "prefix_attn_2"), (FS, 64, 4, "prefix_attn_2"), (BF, 128, 16, "prefix_attn_2"), (BF, 64, 16, "prefix_attn_2"),
+                                                (FH, 64, 16, "prefix_attn_2"), (BF, 128, 17, "prefix_attn"), (BF, 64, 40, "prefix_attn"), (FH, 128, 17, "prefix_attn"),
+                                                (FH, 64, 33, "prefix_attn"), (FS, 128, 17, "prefix_attn"), (FS, 64, 20, "prefix_attn")])
+def test_every_kernel_over_several_tiles(dtype, d, batch, name):
+    """By its name; segments of many tiles, in parts of several, whose last tile has few rows."""
+    c = Case(dtype, 4, 2, d, [0] * batch, [18001, 2000], [300] * (2 * batch))
+    with adakv.KernelTrace(8) as trace:
+        out, lse = c.attn()
+    torch.cuda.synchronize()
+    assert [n for n, _ in trace.durations_us()] == [name, "prefix_combine"]
+    some = [0, 1, batch - 1]                   # (all query rows are alike in this: three sequences are looked at)
+    for b in some:
+        for h in range(2):
+            s = b * 2 + h
+            Ks, Vs = c.rows(s, 300)
+            for i in range(4):
+                ref, z, mag, big = S.attend(f64(c.q[b, 4 * h + i]), Ks, Vs, 1 / math.sqrt(d))
+                keys = np.array(len(Ks))
+                bound = attention_bound(dtype, d, ref, mag, np.array(big), np.array(z), keys, rounded=False) + (mag * 2.0 ** -23 if dtype != FS else 0.0)
+                if dtype == FH:
+                    bound = bound + len(Ks) * 2.0 ** -45 * np.abs(Vs).max()
+                assert (np.abs(f64(out[b, 4 * h + i]) - ref) <= bound).all(), (b, h, i)
+                assert abs(float(lse[b, 4 * h + i]) - z) <= lse_bound(d, np.array(big), np.array(z), keys), (b, h, i)
+
+
 def test_nothing_shared_and_nothing_at_all():
     c = Case(BF, 4, 2, 128, [-1, 0, -1], [0, 0], [0, 5, 0, 0, 3, 0])
     out, lse = c.attn()
