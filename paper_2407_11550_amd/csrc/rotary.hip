@@ -20,7 +20,7 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// E elements of a row as they are in memory: 16 bytes, or one.
+// E elements of a row, 16 bytes, as they are in memory.
 template <typename T, int E> struct Chunk;
 template <typename T> struct Chunk<T, 4> : Elem<T> {
   typedef u32x4 Word;
@@ -41,21 +41,6 @@ template <typename T> struct Chunk<T, 8> : Elem<T> {
     return {round2<T>(f[0], f[1]), round2<T>(f[2], f[3]), round2<T>(f[4], f[5]), round2<T>(f[6], f[7])};
   }
 };
-template <typename T> struct Chunk<T, 1> {
-  typedef unsigned short Word;
-  static __device__ __forceinline__ void widen(Word v, float (&f)[1]) {
-    float w[8];
-    Elem<T>::widen(u32x4{v, 0u, 0u, 0u}, w);
-    f[0] = w[0];
-  }
-  static __device__ __forceinline__ Word narrow(const float (&f)[1]) { return (Word)round2<T>(f[0], 0.0f); }
-};
-template <> struct Chunk<float, 1> {
-  typedef float Word;
-  static __device__ __forceinline__ void widen(Word v, float (&f)[1]) { f[0] = v; }
-  static __device__ __forceinline__ Word narrow(const float (&f)[1]) { return f[0]; }
-};
-
 // The rows of a call, each in `shares` pieces of `share` heads; without positions the rows of `batch` sequences, which begin at `off` among
 // them and at `tok` in the tensors.
 struct Rows {
@@ -96,25 +81,38 @@ template <bool ONCE, typename Word> __device__ __forceinline__ Word load_word(co
   else return *p;
 }
 
-// E: elements of a pair's one half that a lane loads at a time, 16 bytes of them, or 1 where the halves are not so aligned.
-template <typename T, int D, bool NEIGHBOURS, bool NORM, int E>
+// How a lane comes by its pairs.  HALVES: it has elements a of a half and elements b of the other.  NEIGHBOURS: its elements are whole pairs.  SHIFTED: halves
+// that are not 16 bytes apart by some number; an element's other one is another lane's, and they meet in LDS.  (One element a lane at a time
+// instead: 63.9 us, now 34.3, 8192 rows of 40 heads in bf16, d = 128, 100 of it turned.)
+enum Way { HALVES, NEIGHBOURS, SHIFTED };
+
+template <typename T, int D, Way WAY, bool NORM>
 __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k, int dims, float magnitude, const double *__restrict__ freq,
                                                      const void *__restrict__ q_weight, const void *__restrict__ k_weight, float eps) {
+  constexpr int E = 16 / (int)sizeof(T);
   typedef Chunk<T, E> C;
   typedef typename C::Word Word;
   constexpr int S = (int)sizeof(T), LPH = D / 2 / E;           // lanes a head
   constexpr int HPW = 64 / LPH;                                // heads a wavefront sees at a time
-  constexpr bool ONCE = E > 1 && D * S / 2 >= 128;             // (a load is of whole lines of 128 bytes)
-  constexpr int U = E == 1 ? 2 : 4;                            // ... times those whose loads are in flight together
+  constexpr bool ONCE = D * S / 2 >= 128;                      // (a load is of whole lines of 128 bytes)
+  constexpr int U = 4;                                         // ... times those whose loads are in flight together
+  constexpr int MINE = WAY == SHIFTED ? 2 * E : E;             // angles of a lane: its pairs', or its elements'
   __shared__ float2 sh_cs[4][D / 2];
+  // the heads of a wavefront, elements of a lane an odd number of words from the next lane's
+  __shared__ float sh_x[WAY == SHIFTED ? 4 : 1][WAY == SHIFTED ? HPW * (D + D / E) : 1];
   const int lane = threadIdx.x & 63, unit = lane % LPH, slot = lane / LPH;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = dims / 2;
-  // the lane's elements: a and b of the same pairs, and behind the turned ones some of the others, as they come; or (NEIGHBOURS) whole pairs, a piece
-  // of either half of the head, so that neighbouring lanes read on (16 of every 32 bytes at a time: 68.7 us, now 58.4, 16384 rows of 40 heads in bf16)
-  const int ea = NEIGHBOURS || E * unit < half ? E * unit : dims + 2 * (E * unit - half);
-  const int eb = NEIGHBOURS ? ea + D / 2 : E * unit >= half ? ea + E : ea + half;
-  const auto pair = [&](int e) { return !NEIGHBOURS ? E * unit + e : E / 2 * unit + (e < E / 2 ? e : e - E / 2 + D / 4); };
+  // the lane's elements: a and b of the same pairs, and behind the turned ones some of the others, as they come; or a piece of either half of the
+  // head, so that neighbouring lanes read on (NEIGHBOURS with 16 of every 32 bytes at a time: 68.7 us, now 58.4, 16384 rows of 40 heads in bf16)
+  const int ea = WAY != HALVES || E * unit < half ? E * unit : dims + 2 * (E * unit - half);
+  const int eb = WAY != HALVES ? ea + D / 2 : E * unit >= half ? ea + E : ea + half;
+  const auto pair = [&](int e) {
+    if constexpr (WAY == HALVES) return E * unit + e;
+    if constexpr (WAY == NEIGHBOURS) return E / 2 * unit + (e < E / 2 ? e : e - E / 2 + D / 4);
+    const int at = e < E ? ea + e : eb + e - E;                // (SHIFTED: of the lane's element e)
+    return at < half ? at : at < dims ? at - half : half;
+  };
   Word wa[2], wb[2];
   if constexpr (NORM) {
 #pragma unroll
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
       pos = r - rows.off[b];
       row = rows.tok[b] + pos;
     }
-    float cs[E], sn[E];
+    float cs[MINE], sn[MINE];
     if (half) {
       if (lane < D / 2) {
         const float2 v = cos_sin(pos, f);
@@ -151,8 +149,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
       }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float2 v = sh_cs[wv][pair(e)];
+      for (int e = 0; e < MINE; ++e) {
+        const float2 v = sh_cs[wv][WAY == SHIFTED ? min(pair(e), D / 2 - 1) : pair(e)];
         cs[e] = v.x;
         sn[e] = v.y;
       }
@@ -176,6 +174,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (h0 + u * HPW >= end) break;        // (of all lanes)
         float a[E], b[E];
         C::widen(xa[u], a);
         C::widen(xb[u], b);
@@ -184,7 +183,6 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
 #pragma unroll
           for (int e = 0; e < E; ++e) sum = fmaf(a[e], a[e], fmaf(b[e], b[e], sum));
           sum = row_sum<LPH>(sum);
-          if (LPH == 64) sum += __shfl_xor(sum, 32);
           const float by = rsqrtf(fmaf(sum, 1.0f / D, eps));
           const bool is_k = h0 + u * HPW + slot >= q.count;
           float w0[E], w1[E];
@@ -203,13 +201,29 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
             x[e] = a[e];
             x[E + e] = b[e];
           }
+          if constexpr (WAY == SHIFTED) {
+            float *mine = sh_x[wv] + slot * (D + D / E);
+            const auto place = [](int at) { return at + at / E; };
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int i = NEIGHBOURS ? 2 * e : e, j = NEIGHBOURS ? i + 1 : E + e;
-            const bool turned = pair(e) < half;
-            const float y0 = fmaf(x[i], cs[e], -x[j] * sn[e]), y1 = fmaf(x[j], cs[e], x[i] * sn[e]);
-            x[i] = turned ? y0 : x[i];
-            x[j] = turned ? y1 : x[j];
+            for (int e = 0; e < 2 * E; ++e) mine[place(e < E ? ea + e : eb + e - E)] = x[e];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int e = 0; e < 2 * E; ++e) {
+              const int at = e < E ? ea + e : eb + e - E;
+              const float other = mine[place(at < half ? at + half : at < dims ? at - half : at)];
+              const float y = fmaf(x[e], cs[e], at < half ? -other * sn[e] : other * sn[e]);
+              x[e] = at < dims ? y : x[e];
+            }
+            __builtin_amdgcn_wave_barrier();
+          } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const int i = WAY == NEIGHBOURS ? 2 * e : e, j = WAY == NEIGHBOURS ? i + 1 : E + e;
+              const bool turned = pair(e) < half;
+              const float y0 = fmaf(x[i], cs[e], -x[j] * sn[e]), y1 = fmaf(x[j], cs[e], x[i] * sn[e]);
+              x[i] = turned ? y0 : x[i];
+              x[j] = turned ? y1 : x[j];
+            }
           }
 #pragma unroll
           for (int e = 0; e < E; ++e) {
@@ -233,18 +247,18 @@ void run_rotary(bool neighbours, int dims, Rows rows, const Heads &q, const Head
   // A wavefront takes a row, and where there are fewer rows than the chip holds wavefronts (a batch's new tokens), some of its heads.  64 rows of 72
   // heads, bf16, d = 128, behind a norm: 8.3 us a call with a row each, 4.6 with 8 heads each; 1021 rows of 10 fp32 heads, halves that are not aligned:
   // 6.4 and 5.6 with two each.
-  const int at_a_time = 64 / (D / 2 / (!neighbours && dims % (2 * E) != 0 ? 1 : E)), heads = q.count + k.count;
+  const int at_a_time = 64 / (D / 2 / E), heads = q.count + k.count;
   const int pieces = (heads + at_a_time - 1) / at_a_time, most = 8192 / rows.total;
   rows.share = most <= 1 ? heads : (pieces + most - 1) / most * at_a_time;
   rows.shares = (heads + rows.share - 1) / rows.share;
   rows.items = rows.total * rows.shares;
   const dim3 grid((unsigned)((rows.items + 3) / 4 < 4096 ? (rows.items + 3) / 4 : 4096));
   const char *name = NORM ? "norm_rotary" : "rotary";
-#define ADAKV_ROTARY(NB, EL) \
-  ADAKV_LAUNCH(name, (rotary_kernel<T, D, NB, NORM, EL>), grid, dim3(256), s, rows, q, k, dims, magnitude, freq, qw, kw, eps)
-  if (neighbours) ADAKV_ROTARY(true, E);
-  else if (dims % (2 * E) == 0) ADAKV_ROTARY(false, E);
-  else ADAKV_ROTARY(false, 1);                 // elements i and i + dims/2 that are not both 16 bytes into a row
+#define ADAKV_ROTARY(WAY) \
+  ADAKV_LAUNCH(name, (rotary_kernel<T, D, WAY, NORM>), grid, dim3(256), s, rows, q, k, dims, magnitude, freq, qw, kw, eps)
+  if (neighbours) ADAKV_ROTARY(NEIGHBOURS);
+  else if (dims % (2 * E) == 0) ADAKV_ROTARY(HALVES);
+  else ADAKV_ROTARY(SHIFTED);
 #undef ADAKV_ROTARY
 }
 
