@@ -380,7 +380,7 @@ size_t adakv_prefix_workspace_bytes(const adakv_layer *L, int32_t headroom, cons
  * with L's scale.  No rows at all give a zero row and lse = -inf.  fp16 layers hold a softmax weight in 22 bits down to 2^-23 of the
  * largest in its part of a segment, and to 2^-45 of it beyond.  Logits and values that are no finite numbers, the
  * appended row, seg_len and overflow, and the other arguments: as for adakv_decode_attn and adakv_decode_step.  In a step the shared
- * caches are no part of the layer's own (ADAKV_EINVAL).
+ * caches and their seg_len are no part of the layer's own (ADAKV_EINVAL).
  *   ws (device) adakv_prefix_workspace_bytes(L, headroom, P) bytes
  * ADAKV_EINVAL for an entry of `of` that names no shared cache, or a shared layer of another dtype or other h_q, h_kv or d.
  */

@@ -516,6 +516,7 @@ static int decode_prefix(const adakv_layer *L, const void *q_new, const void *k_
     for (const void *x : {(const void *)K_cache, (const void *)V_cache})
       for (const void *y : {P->K_cache, P->V_cache})
         if (overlap({x, own}, {y, theirs})) return ADAKV_EINVAL;
+    if (overlap({seg_len, t.st.batch * heads * sizeof(int32_t)}, {P->seg_len, t.shared.batch * heads * sizeof(int32_t)})) return ADAKV_EINVAL;
   }
   if (!ws || ws_bytes < t.plan.total + 256) return ADAKV_EWORKSPACE;
   char *wsp = (char *)(((uintptr_t)ws + 255) & ~(uintptr_t)255);

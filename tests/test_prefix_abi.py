@@ -17,7 +17,7 @@ def layer(**kw):
     return adakv.Layer(**args)
 
 
-def shared(L=None, of=(0, 0), cu=A, headroom=0, K=BIG, V=2 * BIG, seg_len=A):
+def shared(L=None, of=(0, 0), cu=A, headroom=0, K=BIG, V=2 * BIG, seg_len=3 * BIG):
     L = L or layer(n=[4096], B=[8 * 300])
     c = binding._CPrefix(ctypes.pointer(L.c), (ctypes.c_int32 * len(of))(*of), cu, headroom, K, V, seg_len)
     c.keep = L
@@ -68,6 +68,10 @@ def test_a_step_writes_into_no_shared_cache(lib):
         assert step(lib, P=shared(K=K, V=V), K=4 * BIG, ws_bytes=0) == -1
         assert attn(lib, P=shared(K=K, V=V), ws_bytes=0) == -3           # (reading is free)
     assert step(lib, P=shared(K=A + own, V=BIG), V=4 * BIG, ws_bytes=0) == -3
+    for at in (A, A + 60, A - 28):                         # 16 lengths of its own, 8 of theirs
+        assert step(lib, P=shared(seg_len=at), ws_bytes=0) == -1
+        assert attn(lib, P=shared(seg_len=at), ws_bytes=0) == -3
+    assert step(lib, P=shared(seg_len=A + 64), ws_bytes=0) == -3 and step(lib, P=shared(seg_len=A - 32), ws_bytes=0) == -3
     assert step(lib, k=None) == -1 and step(lib, v=None) == -1
     assert step(lib, k=ODD) == -2 and step(lib, v=ODD) == -2
 
