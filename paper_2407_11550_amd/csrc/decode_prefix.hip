@@ -525,8 +525,10 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int log
   }
   float m = M_INIT, l = 0.0f;
   float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  auto add = [&](float om, float ol, const float4 &oa) {
-    const float mn = fmaxf(m, om), fo = fast_exp2(m - mn), fn = fast_exp2(om - mn);
+  // sums taken against the reference om = z * by, of which only the exponent's difference is made from both, so that an om too large to be
+  // one fp32 number loses nothing
+  auto add = [&](float z, float by, float ol, const float4 &oa) {
+    const float mn = fmaxf(m, z * by), fo = fast_exp2(m - mn), fn = fast_exp2(fmaf(z, by, -mn));
     l = l * fo + ol * fn;
     a.x = a.x * fo + oa.x * fn; a.y = a.y * fo + oa.y * fn;
     a.z = a.z * fo + oa.z * fn; a.w = a.w * fo + oa.w * fn;
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int log
       if (i >= cnt) { ml[u] = make_float2(M_INIT, 0.0f); pa[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
     }
 #pragma unroll
-    for (int u = 0; u < UC; ++u) add(ml[u].x, ml[u].y, pa[u]);
+    for (int u = 0; u < UC; ++u) add(ml[u].x, 1.0f, ml[u].y, pa[u]);
   }
   // (the length is what the other kernel saw: this one writes the new one)
   const bool room = k_new && mine.z < to - from + own.headroom;
@@ -557,7 +559,7 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(Sharing sh, int log
     float dot = fmaf(x[0], k[0], x[1] * k[1]) + fmaf(x[2], k[2], x[3] * k[3]);
 #pragma unroll
     for (int o = 1; o < LPE; o <<= 1) dot += __shfl_xor(dot, o);
-    add(dot * c_log2, 1.0f, make_float4(v[0], v[1], v[2], v[3]));
+    add(dot, c_log2, 1.0f, make_float4(v[0], v[1], v[2], v[3]));
   }
   if (k_new && gi == 0) {
     const long long at = ((long long)from + (long long)s * own.headroom + mine.z) * ROWB;

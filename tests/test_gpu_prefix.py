@@ -241,6 +241,35 @@ def f64_norm(t):
     return t.double().norm(dim=1)
 
 
+@pytest.mark.parametrize("batch", [2, 8, 20, 40])
+@pytest.mark.parametrize("dtype", [BF, FH, FS])
+def test_logits_of_two_to_the_26(dtype, batch):
+    """2^26 less 0, 4, 8 or 12, all of them fp32 numbers, in shared and own segments and in the appended row."""
+    c = Case(dtype, 4, 1, 64, [0] * batch, [200], [9] * batch)
+    c.layer = adakv.Layer(dtype, 4, 1, 64, 1, 7, 0.2, [9] * batch, [9] * batch, scale=1.0)
+    less = 4 * torch.randint(0, 4, (200 + 10 * batch,), generator=torch.Generator().manual_seed(5))
+    seen = torch.zeros(len(less), 64)
+    seen[:, 0], seen[:, 1] = 2.0 ** 13, -less.float()
+    seen = seen.to(dtype).to(DEV)
+    c.pK[:200], c.k[:, 0] = seen[:200], seen[200:200 + batch]
+    c.q.zero_()
+    c.q[..., 0], c.q[..., 1] = 2.0 ** 13, 1.0
+    own = seen[200 + batch:].view(batch, 9, 64)
+    starts = D.segment_starts(c.cu.cpu().numpy(), c.headroom)
+    for b in range(batch):
+        c.K[starts[b]:starts[b] + 9] = own[b]
+    out, lse = c.step()
+    for b in range(batch):
+        w = torch.exp(-torch.cat([less[:200], less[200 + batch + 9 * b:][:9], less[200 + b:][:1]]).double())
+        V = torch.cat([c.pV[:200], c.V[starts[b]:starts[b] + 9], c.v[b]]).double().cpu()
+        want, mag = (w[:, None] * V).sum(0) / w.sum(), (w[:, None] * V.abs()).sum(0) / w.sum()
+        # exponents of up to 2^26 log2 e, of which 17.4 are the largest difference and up to 9 a reference's rounding or its bias: off by 2^-20
+        # at most, with the factor log2 e by 17.4 * 2^-25 more; a weight is cut to 2^-23, and 210 of them are added
+        error = 2.0 ** -19 + 17.4 * 2.0 ** -25 + 2.0 ** -23 + 2 * 210 * 2.0 ** -24
+        assert ((out[b].double().cpu() - want).abs() <= 2 * error * mag).all(), f"sequence {b}"
+        assert ((lse[b].double().cpu() - 2.0 ** 26).abs() <= 16).all()
+
+
 @pytest.mark.parametrize("batch", [2, 8, 20])
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 64), (FH, 128), (FS, 64)])
 def test_values_that_are_no_numbers(dtype, d, batch):
