@@ -240,6 +240,26 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
 
 template <typename T, int D> using Rows = Tile<T, D, D == 64 && T::SIZE == 2 ? 4 : 2>;         // tiles of 64 or (256 bytes a row less) 128 rows
 
+// A wavefront's share of tile t of n rows: rows on (wv * LOADS + i) * RPI + lane / CH; rows past the end repeat the last one.
+template <typename T, int D>
+__device__ __forceinline__ void load_tile(const char *Kh, const char *Vh, int n, int t, int wv, int lane, u32x4 (&tiles_lds)[2][2][Rows<T, D>::WORDS]) {
+  typedef Rows<T, D> TL;
+  constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT;
+  const char *kb = scalar_address(Kh + (long long)t * KT * ROWB), *vb = scalar_address(Vh + (long long)t * KT * ROWB);
+  const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
+  const int end = n - 1 - t * KT;
+#pragma unroll
+  for (int i = 0; i < TL::LOADS; ++i) {
+    const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
+    load_to_lds(kb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_k(row)) * 16, 0u, dk + i * 64);
+  }
+#pragma unroll
+  for (int i = 0; i < TL::LOADS; ++i) {
+    const int row = (wv * TL::LOADS + i) * TL::RPI + lane / CH;
+    load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
+  }
+}
+
 // Sums of a part, `KS` wavefronts to 32 query rows.
 template <typename T, int D, int KS>
 __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
@@ -264,23 +284,10 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   for (int s = 0; s < CH / 2; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + (2 * s + half) * 16);
 
   const int tiles = (n + KT - 1) / KT;
-  // the wavefront's share of a tile: rows on (wv * LOADS + i) * RPI + lane / CH; rows past the end repeat the last one
   auto load = [&](int t) __attribute__((always_inline)) {
-    const char *kb = scalar_address(Kh + (long long)t * KT * ROWB), *vb = scalar_address(Vh + (long long)t * KT * ROWB);
-    const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
-    const int end = n - 1 - t * KT;
     int here = lane;
     if (TIGHT) asm volatile("" : "+v"(here));
-#pragma unroll
-    for (int i = 0; i < TL::LOADS; ++i) {
-      const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH;
-      load_to_lds(kb, (unsigned)min(row, end) * ROWB + ((here % CH) ^ TL::swz_k(row)) * 16, 0u, dk + i * 64);
-    }
-#pragma unroll
-    for (int i = 0; i < TL::LOADS; ++i) {
-      const int row = (wv * TL::LOADS + i) * TL::RPI + here / CH;
-      load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((here % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
-    }
+    load_tile<T, D>(Kh, Vh, n, t, wv, here, tiles_lds);
   };
   // tile t is there, and the next one on its way
   auto await = [&](int t) __attribute__((always_inline)) {
@@ -463,11 +470,136 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   if (half == 0) part_ml[place] = make_float2(m, l);
 }
 
+// The same in 32 bits for no more than 16 query rows, each wavefront on 16 keys of a tile.  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
+// on, and of each value row 16 bytes: what they add to are columns 4 apart, so that what a lane has of a query in the end are 16 bytes again.
+template <int D>
+__device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
+                                        int stride, u32x4 (&tiles_lds)[2][2][Rows<FP32, D>::WORDS]) {
+  typedef Rows<FP32, D> TL;
+  typedef float floatx4 __attribute__((ext_vector_type(4)));
+  constexpr int ROWB = TL::ROWB, CH = TL::CH, VB = D / 64;
+  static_assert(TL::KT == 64, "16 keys a wavefront");
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char *Kh = seg.K + pt.first_row * ROWB, *Vh = seg.V + pt.first_row * ROWB;
+  const int n = pt.n, m_row = min(pt.row + l16, pt.M - 1);
+  const int b = pt.own ? pt.first : __shfl(order, pt.first + (m_row >> sh.log_g));
+  const char *Qh = q + (((long long)(b * sh.h + pt.c) << sh.log_g) + (m_row & ((1 << sh.log_g) - 1))) * ROWB;
+  u32x4 qf[CH / 4];
+#pragma unroll
+  for (int s = 0; s < CH / 4; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + (4 * s + quad) * 16);
+  const int tiles = (n + TL::KT - 1) / TL::KT;
+  load_tile<FP32, D>(Kh, Vh, n, 0, wv, lane, tiles_lds);
+#pragma unroll
+  for (int s = 0; s < CH / 4; ++s) asm volatile("" : "+v"(qf[s]));             // (as above)
+
+  floatx4 acc[VB][4];
+#pragma unroll
+  for (int c = 0; c < VB; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[c][e] = floatx4{0};
+  float m = M_INIT, l = 0.0f;
+  const int row = 16 * wv + l16;
+  for (int t = 0; t < tiles; ++t) {
+    meet();
+    if (t + 1 < tiles) load_tile<FP32, D>(Kh, Vh, n, t + 1, wv, lane, tiles_lds);
+    const int left = n - t * TL::KT - 16 * wv;
+    if (left <= 0) continue;
+    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
+    floatx4 sc = floatx4{0};
+#pragma unroll
+    for (int s = 0; s < CH / 4; ++s) {
+      const u32x4 kw = tk[row * CH + ((4 * s + quad) ^ TL::swz_k(row))];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned ka = kw[e], qa = qf[s][e];
+        sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(ka), __uint_as_float(qa), sc, 0, 0, 0);
+      }
+    }
+    if (left < 16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[i] = 4 * quad + i < left ? sc[i] : -INFINITY;
+    }
+    float pr[4];
+    auto weigh = [&]() {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_log2, BIAS<FP32> - m));
+      return (pr[0] + pr[1]) + (pr[2] + pr[3]);
+    };
+    float sum = weigh();
+    if (__builtin_expect(__any(!(sum <= MOST<FP32>)), 0)) {
+      float top = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top * c_log2), corr = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int c = 0; c < VB; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][e] *= corr;
+      sum = weigh();
+    }
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 4 * quad + i, at = 16 * wv + key;
+#pragma unroll
+      for (int c = 0; c < VB; ++c) {
+        u32x4 vw = tv[at * CH + ((16 * c + l16) ^ TL::swz_v(at))];
+        if (left < 16) {                       // (what repeats the last row has no part in the sums, whatever it is)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vw[e] = key < left ? vw[e] : 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned va = vw[e];
+          acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(va), pr[i], acc[c][e], 0, 0, 0);
+        }
+      }
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  m -= BIAS<FP32>;
+
+  typedef floatx4 Shared[VB * 4][64];
+  static_assert(3 * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
+  Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
+  float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 3);
+  meet();
+  if (wv) {
+#pragma unroll
+    for (int x = 0; x < VB * 4; ++x) others[wv - 1][x][lane] = acc[x / 4][x % 4];
+    ml[wv - 1][lane] = make_float2(m, l);
+  }
+  __syncthreads();
+  if (wv) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const float2 other = ml[k][lane];
+    const float mn = fmaxf(m, other.x), f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(other.x - mn);
+    m = mn;
+    l = l * f0 + other.y * f1;
+#pragma unroll
+    for (int x = 0; x < VB * 4; ++x) acc[x / 4][x % 4] = acc[x / 4][x % 4] * f0 + others[k][x][lane] * f1;
+  }
+  if (pt.row + l16 >= pt.M) return;
+  const long long place = (long long)pt.out * stride + l16;
+  float *dst = part_acc + place * D + 16 * quad;
+#pragma unroll
+  for (int c = 0; c < VB; ++c)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *reinterpret_cast<float4 *>(dst + 64 * c + 4 * r) = make_float4(acc[c][0][r], acc[c][1][r], acc[c][2][r], acc[c][3][r]);
+  if (quad == 0) part_ml[place] = make_float2(m, l);
+}
+
 template <typename T, int D, int KS>
 __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_attn_kernel(Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q,
                                                                                          Segments shared, Segments own, PrefixSums sums) {
   typedef Rows<T, D> TL;
-  constexpr int KT = TL::KT, OWN = KT / 32;                    // (own segments have up to 8 query rows)
+  constexpr int KT = TL::KT;                                   // (own segments have up to 8 query rows)
   static_assert(TL::TURNS == 2, "the next tile has a place of its own");
   __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
   __shared__ int sh_bad[4], sh_scan[24];
@@ -475,7 +607,8 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
   Part pt;
   if ((int)blockIdx.x < sp.shared_blocks) {
     if (!find_shared<KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, sp.sums_cost, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
-    sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, tiles_lds, sh_bad);
+    if constexpr (KS == 8) sum_few<D>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 16, tiles_lds);
+    else sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, tiles_lds, sh_bad);
   } else {
     Work wk;
     if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
@@ -484,7 +617,8 @@ __global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_
     const int b = quotient(wk.s, sh.h), g = 1 << sh.log_g;
     pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, wk.s - b * sh.h, 0, g, min(wk.rows - wk.j * rows, rows),
           (int)blockIdx.x - sp.shared_blocks, b, true};
-    sum_part<T, D, OWN>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds, sh_bad);
+    if constexpr (is_f32<T>) sum_few<D>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds);
+    else sum_part<T, D, KT / 32>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds, sh_bad);
   }
 }
 
@@ -595,14 +729,15 @@ void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const voi
   const PrefixSums sums = {(float *)(ws + pl.shared_acc), (float *)(ws + pl.own_acc), (float2 *)(ws + pl.shared_ml), (float2 *)(ws + pl.own_ml),
                            (int4 *)(ws + pl.shared_tab), (int4 *)(ws + pl.own_tab)};
 #define ADAKV_PREFIX(KS)                                                                                                              \
-  ADAKV_LAUNCH(KS == 1 ? "prefix_attn" : KS == 2 ? "prefix_attn_2" : "prefix_attn_4", (prefix_attn_kernel<T, D, KS>),                  \
+  ADAKV_LAUNCH(KS == 1 ? "prefix_attn" : KS == 2 ? "prefix_attn_2" : KS == 4 ? "prefix_attn_4" : "prefix_attn_8", (prefix_attn_kernel<T, D, KS>),                  \
                dim3(pl.split.shared_blocks + pl.own_blocks), dim3(256), s, sh, pl.split, c_log2, (const char *)q, shared, own, sums)
   if (pl.split.rb == 128) ADAKV_PREFIX(1);
   else if (pl.split.rb == 64) ADAKV_PREFIX(2);
-  else if constexpr (Rows<T, D>::KT == 128) ADAKV_PREFIX(4);   // (32 rows: plan_prefix)
+  else if constexpr (is_f32<T>) ADAKV_PREFIX(8);               // (16 rows: plan_prefix)
+  else if constexpr (Rows<T, D>::KT == 128) ADAKV_PREFIX(4);   // (32)
 #undef ADAKV_PREFIX
   ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, 1 << sh.log_g), dim3(256), s, sh,
-               pl.split.rb == 128 ? 7 : pl.split.rb == 64 ? 6 : 5, c_log2,
+               pl.split.rb == 128 ? 7 : pl.split.rb == 64 ? 6 : pl.split.rb == 32 ? 5 : 4, c_log2,
                (const char *)q, (const char *)k_new, (const char *)v_new, shared, own, seg_len, overflow, sums, out, lse);
 }
 
@@ -632,7 +767,7 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
   const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) << sh.log_g; };
   int most = 0;
   for (int p = 0; p < sh.groups; ++p) most = rows_of(p) > most ? rows_of(p) : most;
-  const int rb = pl.split.rb = most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;
+  const int rb = pl.split.rb = dtype == ADAKV_FP32 && most <= 16 ? 16 : most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;
   const auto blocks_of = [&](int p) { return (rows_of(p) + rb - 1) / rb; };
   long long n = 0, padding = 0;                // workgroups at least, one for each segment and block of rows; places that groups of 8 take
   for (int p = 0; p < sh.groups; ++p) {
