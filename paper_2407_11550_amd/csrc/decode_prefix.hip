@@ -470,7 +470,8 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   if (half == 0) part_ml[place] = make_float2(m, l);
 }
 
-// The same in 32 bits for no more than 16 query rows, each wavefront on 16 keys of a tile.  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
+// The same in 32 bits for no more than 16 query rows, each wavefront on 16 keys of a tile (32 keys of two wavefronts times 32 query rows, of which half
+// or more are none: 64 sequences of 500 own rows, 8 heads of 128, g = 4 100 us, now 61, 4.3 TB/s).  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
 // on, and of each value row 16 bytes: what they add to are columns 4 apart, so that what a lane has of a query in the end are 16 bytes again.
 template <int D>
 __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
@@ -767,21 +768,28 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
   const auto rows_of = [&](int p) { return (sh.first[p + 1] - sh.first[p]) << sh.log_g; };
   int most = 0;
   for (int p = 0; p < sh.groups; ++p) most = rows_of(p) > most ? rows_of(p) : most;
-  const int rb = pl.split.rb = dtype == ADAKV_FP32 && most <= 16 ? 16 : most <= 32 && dm.d == 64 && dtype != ADAKV_FP32 ? 32 : most <= 64 ? 64 : 128;
+  // Query rows of a workgroup: as many as the longest shared list has, but then fewer, so that its wavefronts all have some.  us a call, 8 KV heads, g = 4, 60
+  // to 100 own rows.  fp32, d = 128, 16 | 64: 8 sequences over 2000 rows a head 19.4 | 21.7, over 20000 56.5 | 62.5, 12 over 8000 48.7 | 38.8.
+  // 16 bits, 32 | 64, d = 64: 8 over 2000 10.5 | 11.1, 2 over 20000 14.5 | 15.8.  64 | 128, bf16, d = 128: 18 over 2000 20.4 | 21.7, over 32768 48.9 |
+  // 44.0, 48 over 8192 34.3 | 30.3.
+  const bool wide = dtype == ADAKV_FP32;
+  const int rb = pl.split.rb = wide && most <= 32 ? 16 : !wide && dm.d == 64 && most <= 32 ? 32 : most <= 64 ? 64 : 128;
   const auto blocks_of = [&](int p) { return (rows_of(p) + rb - 1) / rb; };
   long long n = 0, padding = 0;                // workgroups at least, one for each segment and block of rows; places that groups of 8 take
   for (int p = 0; p < sh.groups; ++p) {
     n += (long long)blocks_of(p) * dm.h_kv;
     if (blocks_of(p) > 1) padding += 7ll * blocks_of(p);
   }
+  // A workgroup for each compute unit: own segments run beside them, and more of them only begin later.  us, 256 parts | twice as many, bf16, d = 128, g = 4:
+  // 64 sequences over 32768 rows with 500 own rows 85.7 | 99.5, with none 82.7 | 77.5; 8 over 32768 29.3 | 34.5 (320 parts), and with 192 33.7.
   const long long want = 256;
   pl.split.spare = (int)(want > n / 2 + 1 ? want : n / 2 + 1);
   // sums of a block's rows, written and read at 5 TB/s, over a tile of 64 rows' (or 128 of 128 bytes) time in a workgroup
   const int sum_rows = most < rb ? most : rb;
-  const float tile_us = dtype != ADAKV_FP32 ? 1.0f : dm.d == 64 ? 3.0f : 6.0f;
+  const float tile_us = !wide ? 1.0f : (dm.d == 64 ? 3.0f : 6.0f) * (rb == 16 ? 0.25f : 1.0f);
   pl.split.sums_cost = sum_rows * (dm.d + 2) * 8.0f / 5.0e6f / tile_us;
   pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
-  const int tile = dm.d == 64 && dtype != ADAKV_FP32 ? 128 : 64;
+  const int tile = dm.d == 64 && !wide ? 128 : 64;
   const long long nseg = (long long)sh.groups * dm.h_kv, own = (long long)st.batch * dm.h_kv;
   const long long own_cap = (long long)st.out_off[st.batch] + own * headroom, a_part = (own_cap + 511) / 512;
   pl.split.own_segments = (int)own;

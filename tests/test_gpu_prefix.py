@@ -179,7 +179,7 @@ def test_shared_caches_of_many_and_of_few(dtype, d, groups, h):
 
 
 @pytest.mark.parametrize("dtype,d,batch,name", [(BF, 128, 4, "prefix_attn_2"), (BF, 64, 4, "prefix_attn_4"), (FH, 128, 4, "prefix_attn_2"), (FH, 64, 4, "prefix_attn_4"),
-                                                (FS, 128, 4, "prefix_attn_8"), (FS, 64, 3, "prefix_attn_8"), (FS, 128, 5, "prefix_attn_2"), (FS, 64, 16, "prefix_attn_2"), (BF, 128, 16, "prefix_attn_2"), (BF, 64, 16, "prefix_attn_2"),
+                                                (FS, 128, 4, "prefix_attn_8"), (FS, 64, 3, "prefix_attn_8"), (FS, 128, 8, "prefix_attn_8"), (FS, 128, 9, "prefix_attn_2"), (FS, 64, 16, "prefix_attn_2"), (BF, 128, 16, "prefix_attn_2"), (BF, 64, 16, "prefix_attn_2"),
                                                 (FH, 64, 16, "prefix_attn_2"), (BF, 128, 17, "prefix_attn"), (BF, 64, 40, "prefix_attn"), (FH, 128, 17, "prefix_attn"),
                                                 (FH, 64, 33, "prefix_attn"), (FS, 128, 17, "prefix_attn"), (FS, 64, 20, "prefix_attn")])
 def test_every_kernel_over_several_tiles(dtype, d, batch, name):
