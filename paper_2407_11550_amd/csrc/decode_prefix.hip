@@ -9,8 +9,12 @@
 // of the largest and 2^-45 of it beyond.  fp32: the fp32 matrix instruction.
 //
 // A segment is split into parts as in decode.hip; a workgroup takes a part for 128, 64 or 32 rows of queries (1, 2 or 4 wavefronts
-// share 32 of them) and files the sums.  A second kernel merges, for each query head, the parts of its own segment and of the shared one, and
+// share 32 of them; 16 rows in 32 bits) and files the sums.  A second kernel merges, for each query head, the parts of its own segment and of the shared one, and
 // the row that the call appends, which it also puts into the cache.
+//
+// Bound by HBM while few sequences share a cache (8 sequences with 700 to 900 own rows over 3 caches of 16384 rows, 64 query heads: attention 33 us, 5.8
+// TB/s), by the matrix units where many do (64 over one cache of 32768 rows, 8 heads of 128, g = 4, bf16: 85 us, 70 GFLOP of matrix work with the
+// three parts of the weights), and by its two launches and a workgroup's start where there is little to do (2 over 541 rows: 6.6 us and 4.5).
 #include <math.h>
 
 #include "attn_tiles.h"
