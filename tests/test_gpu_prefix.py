@@ -179,7 +179,8 @@ def test_shared_caches_of_many_and_of_few(dtype, d, groups, h):
 
 
 @pytest.mark.parametrize("dtype,d,batch,name", [(BF, 128, 4, "prefix_attn_2"), (BF, 64, 4, "prefix_attn_4"), (FH, 128, 4, "prefix_attn_2"), (FH, 64, 4, "prefix_attn_4"),
-                                                (FS, 128, 4, "prefix_attn_8"), (FS, 64, 3, "prefix_attn_8"), (FS, 128, 8, "prefix_attn_8"), (FS, 128, 9, "prefix_attn_2"), (FS, 64, 16, "prefix_attn_2"), (BF, 128, 16, "prefix_attn_2"), (BF, 64, 16, "prefix_attn_2"),
+                                                (FS, 128, 4, "prefix_attn_8"), (FS, 64, 3, "prefix_attn_8"), (FS, 128, 8, "prefix_attn_8"), (FS, 128, 9, "prefix_attn_2"),
+                                                (FS, 64, 16, "prefix_attn_2"), (BF, 128, 16, "prefix_attn_2"), (BF, 64, 16, "prefix_attn_2"),
                                                 (FH, 64, 16, "prefix_attn_2"), (BF, 128, 17, "prefix_attn"), (BF, 64, 40, "prefix_attn"), (FH, 128, 17, "prefix_attn"),
                                                 (FH, 64, 33, "prefix_attn"), (FS, 128, 17, "prefix_attn"), (FS, 64, 20, "prefix_attn")])
 def test_every_kernel_over_several_tiles(dtype, d, batch, name):
@@ -202,6 +203,23 @@ def test_every_kernel_over_several_tiles(dtype, d, batch, name):
                     bound = bound + len(Ks) * 2.0 ** -45 * np.abs(Vs).max()
                 assert (np.abs(f64(out[b, 4 * h + i]) - ref) <= bound).all(), (b, h, i)
                 assert abs(float(lse[b, 4 * h + i]) - z) <= lse_bound(d, np.array(big), np.array(z), keys), (b, h, i)
+
+
+@pytest.mark.parametrize("dtype,d", [(t, d) for t in (BF, FH, FS) for d in (64, 128)])
+def test_every_length_up_to_two_tiles(dtype, d):
+    """64 sequences, each with a shared cache to itself: own lengths 0 to 127, shared ones 130 to 3."""
+    c = Case(dtype, 4, 2, d, list(range(64)), [130 - n for n in range(128)], list(range(128)))
+    out, lse = c.attn()
+    c.check(out, lse, c.own, "every length")
+
+
+@pytest.mark.parametrize("dtype", [BF, FS])
+def test_the_largest_tables(dtype):
+    """64 sequences, 64 KV heads, 64 shared caches: 4096 segments of either kind."""
+    rng = np.random.default_rng(8)
+    c = Case(dtype, 1, 64, 64, [63 - b for b in range(64)], [int(n) for n in rng.integers(0, 40, 4096)], [int(n) for n in rng.integers(0, 12, 4096)])
+    out, lse = c.attn()
+    c.check(out, lse, c.own, "4096 segments")
 
 
 def test_nothing_shared_and_nothing_at_all():
@@ -385,6 +403,22 @@ def test_on_another_stream():
     out, lse = c.attn(stream=side)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_two_streams_over_one_shared_cache():
+    """Two batches at once, each with a cache and a workspace of its own, read the same shared one."""
+    c = Case(BF, 4, 2, 128, [0] * 20, [5000, 3000], [40] * 40)
+    made = [(c.K.clone(), c.V.clone(), c.lens.clone()) for _ in range(3)]
+    step = lambda t, **kw: adakv.decode_prefix_step(c.layer, c.q, c.k, c.v, c.cu, c.headroom, *t, c.prefix, want_lse=True, **kw)
+    want, want_lse = step(made[0])
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for side in sides:
+        side.wait_stream(torch.cuda.current_stream())
+    got = [step(t, stream=side) for t, side in zip(made[1:], sides)]
+    torch.cuda.synchronize()
+    for (out, lse), t in zip(got, made[1:]):
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(t, made[0]))
 
 
 def test_results_do_not_change_from_run_to_run():
