@@ -242,15 +242,23 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
   return true;
 }
 
-template <typename T, int D> using Rows = Tile<T, D, D == 64 && T::SIZE == 2 ? 4 : 2>;         // tiles of 64 or (256 bytes a row less) 128 rows
+// A tile of a workgroup whose wavefronts share 32 query rows `KS` at a time: 64 rows, 128 of 128 bytes, 32 of 512 where each wavefront takes all of them.  With
+// tiles of 64 KB of keys and values two workgroups fit on a compute unit.
+template <typename T, int D, int KS> using Rows = Tile<T, D, D * T::SIZE == 512 && KS == 1 ? 1 : D * T::SIZE == 128 ? 4 : 2>;
+// Tiles in LDS: the keys of one or two of them, and behind these the values.
+template <typename TL, int TURNS> struct Place {
+  static constexpr int BYTES = 2 * TURNS * TL::WORDS * 16;
+  u32x4 *lds;
+  __device__ __forceinline__ u32x4 *keys(int t) const { return lds + t % TURNS * TL::WORDS; }
+  __device__ __forceinline__ u32x4 *values(int t) const { return lds + (TURNS + t % TURNS) * TL::WORDS; }
+};
 
 // A wavefront's share of tile t of n rows: rows on (wv * LOADS + i) * RPI + lane / CH; rows past the end repeat the last one.
-template <typename T, int D>
-__device__ __forceinline__ void load_tile(const char *Kh, const char *Vh, int n, int t, int wv, int lane, u32x4 (&tiles_lds)[2][2][Rows<T, D>::WORDS]) {
-  typedef Rows<T, D> TL;
+template <typename TL, int TURNS>
+__device__ __forceinline__ void load_tile(const char *Kh, const char *Vh, int n, int t, int wv, int lane, const Place<TL, TURNS> &place) {
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT;
   const char *kb = scalar_address(Kh + (long long)t * KT * ROWB), *vb = scalar_address(Vh + (long long)t * KT * ROWB);
-  const u32x4 *dk = tiles_lds[0][t % 2] + wv * TL::LOADS * 64, *dv = tiles_lds[1][t % 2] + wv * TL::LOADS * 64;
+  const u32x4 *dk = place.keys(t) + wv * TL::LOADS * 64, *dv = place.values(t) + wv * TL::LOADS * 64;
   const int end = n - 1 - t * KT;
 #pragma unroll
   for (int i = 0; i < TL::LOADS; ++i) {
@@ -263,12 +271,26 @@ __device__ __forceinline__ void load_tile(const char *Kh, const char *Vh, int n,
     load_to_lds(vb, (unsigned)min(row, end) * ROWB + ((lane % CH) ^ TL::swz_v(row)) * 16, 0u, dv + i * 64);
   }
 }
+// Tile t is there, and the next one on its way if it has a place; tile 0 has been asked for.
+template <int TURNS, typename Load> __device__ __forceinline__ void await_tile(int t, int tiles, Load &&load) {
+  if constexpr (TURNS == 2) {
+    meet();
+    if (t + 1 < tiles) load(t + 1);
+  } else {
+    if (t) {
+      meet();                                  // (what was there has been read)
+      load(t);
+    }
+    meet();
+  }
+}
 
 // Sums of a part, `KS` wavefronts to 32 query rows.
 template <typename T, int D, int KS>
 __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
-                                         int stride, u32x4 (&tiles_lds)[2][2][Rows<T, D>::WORDS], int (&sh_bad)[4]) {
-  typedef Rows<T, D> TL;
+                                         int stride, u32x4 *lds, int (&sh_bad)[4]) {
+  typedef Rows<T, D, KS> TL;
+  const Place<TL, 2> place_of{lds};
   typedef Weights<T, D, TL> W;
   constexpr int ROWB = TL::ROWB, CH = TL::CH, KT = TL::KT, CB = D / 32;
   // 32 keys at a time, or two times 32 where a wavefront has so many of a tile (fp16, d = 128: its two sets of sums leave no registers for the logits of two)
@@ -291,13 +313,10 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   auto load = [&](int t) __attribute__((always_inline)) {
     int here = lane;
     if (TIGHT) asm volatile("" : "+v"(here));
-    load_tile<T, D>(Kh, Vh, n, t, wv, here, tiles_lds);
+    load_tile(Kh, Vh, n, t, wv, here, place_of);
   };
   // tile t is there, and the next one on its way
-  auto await = [&](int t) __attribute__((always_inline)) {
-    meet();
-    if (t + 1 < tiles) load(t + 1);
-  };
+  auto await = [&](int t) __attribute__((always_inline)) { await_tile<2>(t, tiles, load); };
 
   load(0);
   // (the wait for the queries stands here, once, and not in front of the first products of every tile, where it would be one for the next tile's loads)
@@ -326,7 +345,7 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
     constexpr int N = PAIR, apart = KS;
     int here = lane;
     if (TIGHT) asm volatile("" : "+v"(here));
-    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
+    const u32x4 *tk = place_of.keys(t), *tv = place_of.values(t);
     floatx16 sc[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) sc[k] = tile_logits<T, TL>(tk + (kk + k * apart) * 32 * CH, qf, here & 31, here >> 5);
@@ -409,7 +428,7 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
         for (int kk = wv % KS; kk < KT / 32; kk += KS) {
           if (n - t * KT - 32 * kk <= 0) break;
           // (the rows past the end repeat the last one, so their weights may stay)
-          const floatx16 sc = tile_logits<T, TL>(tiles_lds[0][t % 2] + kk * 32 * CH, qf, l32, half);
+          const floatx16 sc = tile_logits<T, TL>(place_of.keys(t) + kk * 32 * CH, qf, l32, half);
           float pr[16];
           weigh(sc, pr);
           if constexpr (is_f16<T>) {                           // (none is too small for the type)
@@ -418,7 +437,7 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
           }
           W w;
           w.set(pr);
-          w.add_first(o, tiles_lds[1][t % 2] + kk * 32 * CH, lane, cb);
+          w.add_first(o, place_of.values(t) + kk * 32 * CH, lane, cb);
         }
       }
 #pragma unroll
@@ -430,8 +449,8 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   if constexpr (KS > 1) {
     // the first of those that share their rows takes the others' sums, through the tiles' place
     typedef float4 Shared[CB * 4][64];
-    static_assert((4 - 4 / KS) * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
-    Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
+    static_assert((4 - 4 / KS) * (sizeof(Shared) + 64 * sizeof(float2)) <= Place<TL, 2>::BYTES, "the sums have room");
+    Shared *others = reinterpret_cast<Shared *>(lds);
     float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 4 - 4 / KS);
     const int place = wv / KS * (KS - 1) - 1;                  // + 1 .. KS - 1
     meet();
@@ -477,10 +496,11 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 // The same in 32 bits for no more than 16 query rows, each wavefront on 16 keys of a tile (32 keys of two wavefronts times 32 query rows, of which half
 // or more are none: 64 sequences of 500 own rows, 8 heads of 128, g = 4 100 us, now 61, 4.3 TB/s).  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
 // on, and of each value row 16 bytes: what they add to are columns 4 apart, so that what a lane has of a query in the end are 16 bytes again.
-template <int D>
+template <int D, int TURNS>
 __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
-                                        int stride, u32x4 (&tiles_lds)[2][2][Rows<FP32, D>::WORDS]) {
-  typedef Rows<FP32, D> TL;
+                                        int stride, u32x4 *lds) {
+  typedef Rows<FP32, D, 8> TL;
+  const Place<TL, TURNS> place_of{lds};
   typedef float floatx4 __attribute__((ext_vector_type(4)));
   constexpr int ROWB = TL::ROWB, CH = TL::CH, VB = D / 64;
   static_assert(TL::KT == 64, "16 keys a wavefront");
@@ -494,7 +514,8 @@ __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int o
 #pragma unroll
   for (int s = 0; s < CH / 4; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(Qh + (4 * s + quad) * 16);
   const int tiles = (n + TL::KT - 1) / TL::KT;
-  load_tile<FP32, D>(Kh, Vh, n, 0, wv, lane, tiles_lds);
+  auto load = [&](int t) __attribute__((always_inline)) { load_tile(Kh, Vh, n, t, wv, lane, place_of); };
+  load(0);
 #pragma unroll
   for (int s = 0; s < CH / 4; ++s) asm volatile("" : "+v"(qf[s]));             // (as above)
 
@@ -506,11 +527,10 @@ __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int o
   float m = M_INIT, l = 0.0f;
   const int row = 16 * wv + l16;
   for (int t = 0; t < tiles; ++t) {
-    meet();
-    if (t + 1 < tiles) load_tile<FP32, D>(Kh, Vh, n, t + 1, wv, lane, tiles_lds);
+    await_tile<TURNS>(t, tiles, load);
     const int left = n - t * TL::KT - 16 * wv;
     if (left <= 0) continue;
-    const u32x4 *tk = tiles_lds[0][t % 2], *tv = tiles_lds[1][t % 2];
+    const u32x4 *tk = place_of.keys(t), *tv = place_of.values(t);
     floatx4 sc = floatx4{0};
 #pragma unroll
     for (int s = 0; s < CH / 4; ++s) {
@@ -569,8 +589,8 @@ __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int o
   m -= BIAS<FP32>;
 
   typedef floatx4 Shared[VB * 4][64];
-  static_assert(3 * (sizeof(Shared) + 64 * sizeof(float2)) <= sizeof(tiles_lds), "the sums have room");
-  Shared *others = reinterpret_cast<Shared *>(&tiles_lds[0][0][0]);
+  static_assert(3 * (sizeof(Shared) + 64 * sizeof(float2)) <= Place<TL, TURNS>::BYTES, "the sums have room");
+  Shared *others = reinterpret_cast<Shared *>(lds);
   float2(*ml)[64] = reinterpret_cast<float2(*)[64]>(others + 3);
   meet();
   if (wv) {
@@ -600,30 +620,34 @@ __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int o
   if (quad == 0) part_ml[place] = make_float2(m, l);
 }
 
+// Workgroups on a compute unit.
+template <typename T, int D, int KS> constexpr int AT_ONCE = Place<Rows<T, D, KS>, 2>::BYTES > 64 * 1024 ? 1 : 2;
+
 template <typename T, int D, int KS>
-__global__ __launch_bounds__(256, D == 128 && T::SIZE == 4 ? 1 : 2) void prefix_attn_kernel(Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q,
-                                                                                         Segments shared, Segments own, PrefixSums sums) {
-  typedef Rows<T, D> TL;
-  constexpr int KT = TL::KT;                                   // (own segments have up to 8 query rows)
-  static_assert(TL::TURNS == 2, "the next tile has a place of its own");
-  __shared__ __align__(16) u32x4 tiles_lds[2][2][TL::WORDS];                    // keys and values, two tiles of each
+__global__ __launch_bounds__(256, (AT_ONCE<T, D, KS>)) void prefix_attn_kernel(
+    Sharing sh, PrefixSplit sp, float c_log2, const char *__restrict__ q, Segments shared, Segments own, PrefixSums sums) {
+  typedef Rows<T, D, KS> TL;
+  typedef Rows<T, D, D * T::SIZE == 128 ? 4 : 2> OL;           // of own segments, which have up to 8 query rows
+  constexpr int OWN_TURNS = Place<OL, 2>::BYTES > Place<TL, 2>::BYTES ? 1 : 2;
+  static_assert(Place<OL, OWN_TURNS>::BYTES <= Place<TL, 2>::BYTES, "own segments' tiles have room");
+  __shared__ __align__(16) u32x4 lds[Place<TL, 2>::BYTES / 16];
   __shared__ int sh_bad[4], sh_scan[24];
   const int order = sh.order[threadIdx.x & 63];
   Part pt;
   if ((int)blockIdx.x < sp.shared_blocks) {
-    if (!find_shared<KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, sp.sums_cost, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
-    if constexpr (KS == 8) sum_few<D>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 16, tiles_lds);
-    else sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, tiles_lds, sh_bad);
+    if (!find_shared<TL::KT, 128 / KS>(sh, (int)blockIdx.x, sp.spare, sp.sums_cost, shared.headroom, shared.cu, shared.seg_len, sums.shared_tab, pt)) return;
+    if constexpr (KS == 8) sum_few<D, 2>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 16, lds);
+    else sum_part<T, D, KS>(sh, pt, order, c_log2, q, shared, sums.shared_acc, sums.shared_ml, 128 / KS, lds, sh_bad);
   } else {
     Work wk;
     if (!find_work<4, false>(sp.own_segments, sp.own_per, sp.own_split, own.headroom, 0, own.cu, own.seg_len, sh_scan, sums.own_tab, wk, {}, sp.shared_blocks))
       return;
-    const int rows = min(sp.own_split, (quotient_up(wk.rows, wk.parts) + KT - 1) / KT * KT);           // (as above)
+    const int rows = min(sp.own_split, (quotient_up(wk.rows, wk.parts) + OL::KT - 1) / OL::KT * OL::KT);       // (as above)
     const int b = quotient(wk.s, sh.h), g = 1 << sh.log_g;
     pt = {(long long)wk.first_row + (long long)wk.s * own.headroom + wk.j * rows, wk.s, wk.s - b * sh.h, 0, g, min(wk.rows - wk.j * rows, rows),
           (int)blockIdx.x - sp.shared_blocks, b, true};
-    if constexpr (is_f32<T>) sum_few<D>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds);
-    else sum_part<T, D, KT / 32>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, tiles_lds, sh_bad);
+    if constexpr (is_f32<T>) sum_few<D, OWN_TURNS>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, lds);
+    else sum_part<T, D, OL::KT / 32>(sh, pt, order, c_log2, q, own, sums.own_acc, sums.own_ml, g, lds, sh_bad);
   }
 }
 
@@ -739,7 +763,7 @@ void run_prefix(const Sharing &sh, const PrefixPlan &pl, float c_log2, const voi
   if (pl.split.rb == 128) ADAKV_PREFIX(1);
   else if (pl.split.rb == 64) ADAKV_PREFIX(2);
   else if constexpr (is_f32<T>) ADAKV_PREFIX(8);               // (16 rows: plan_prefix)
-  else if constexpr (Rows<T, D>::KT == 128) ADAKV_PREFIX(4);   // (32)
+  else if constexpr (D == 64) ADAKV_PREFIX(4);   // (32)
 #undef ADAKV_PREFIX
   ADAKV_LAUNCH("prefix_combine", (prefix_combine_kernel<T, D>), dim3(pl.split.own_segments, 1 << sh.log_g), dim3(256), s, sh,
                pl.split.rb == 128 ? 7 : pl.split.rb == 64 ? 6 : pl.split.rb == 32 ? 5 : 4, c_log2,
