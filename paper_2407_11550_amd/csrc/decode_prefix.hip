@@ -193,7 +193,18 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
     const int blocks = __shfl(my_blocks, quotient(min(lane, nseg - 1), h));             // (of all lanes: one that is off has nothing to give)
     const int all = wave_sum(lane < nseg ? tiles * blocks : 0);
     split = tiles_a_part(all, spare, sums_cost);
-    const int parts = lane < nseg && blocks > 0 ? quotient_up(tiles, split) : 0;
+    // Segments' last parts are shorter than the others, so that there may be up to one part more for each segment and block of rows; and where one
+    // compute unit gets two workgroups because of them, the call lasts as long as these take side by side.  So longer parts, twice at most.  us,
+    // uneven heads, one part more | as many as fit: 64 sequences over 32768 rows a head, g = 8, bf16 199 | 138, 28 over 16000, fp32 237 | 166, 48 over 8000, g = 4
+    // 30.5 | 27.9.
+    int parts = 0;
+#pragma nounroll
+    for (int turn = 0; turn < 3; ++turn) {
+      parts = lane < nseg && blocks > 0 ? quotient_up(tiles, split) : 0;
+      const int over = turn < 2 ? wave_sum(parts * blocks) - spare : 0;
+      if (over <= 0) break;
+      split += max(1, (int)((float)split * (float)over * __builtin_amdgcn_rcpf((float)spare) + 0.999f));
+    }
     upto = wave_scan_incl(parts);
     const int last = __shfl(upto, min(lane * h + h - 1, 63)), before = __shfl(upto, max(min(lane * h, 64) - 1, 0));
     my_parts = lane < groups ? last - (lane ? before : 0) : 0;
