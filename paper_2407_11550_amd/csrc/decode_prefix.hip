@@ -112,18 +112,10 @@ template <typename T, int D, typename TL> struct Weights {
       }
     }
   }
-  // The first parts alone, columns 32 cb on.
+  // The first parts alone, columns 32 cb on (16 bits).
   __device__ __forceinline__ void add_first(floatx16 &o, const u32x4 *tv, int lane, int cb) const {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      if constexpr (is_f32<T>) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          o = __builtin_amdgcn_mfma_f32_32x32x2f32(tile_value<D, TL>(tv, lane & 31, lane >> 5, ks, cb, i), __uint_as_float(w[0][8 * ks + i]), o, 0, 0, 0);
-      } else {
-        o = product<T>(tile_values<TL>(tv, lane, ks, cb), operand(0, ks), o);
-      }
-    }
+    for (int ks = 0; ks < 2; ++ks) o = product<T>(tile_values<TL>(tv, lane, ks, cb), operand(0, ks), o);
   }
 };
 
@@ -403,6 +395,10 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 
   for (int t = 0; t < tiles; ++t) {
     await(t);
+    if (is_f32<T> && n - t * KT < KT) {        // (the last tile: values past the end are cleared, as their weights are 0 and they may be no numbers)
+      for (int i = (n - t * KT) * CH + tid; i < KT * CH; i += 256) place_of.values(t)[i] = u32x4{0, 0, 0, 0};
+      __syncthreads();
+    }
     if (idle) continue;
     // (this wavefront's 32 keys of the tile are every KS-th 32)
 #pragma unroll
@@ -416,43 +412,46 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
   }
 
   // Where a sum is infinite or NaN, a value that is none may have met a weight's lower part of 0, or of the other sign, or a
-  // weight of 0 of the rows past the end: once more with the upper parts alone, which say what it is.
-  float worst[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  // weight of 0 of the rows past the end: once more with the upper parts alone, which say what it is.  (32 bits: a weight has no parts, and
+  // there are no values past the end.)
+  if constexpr (!is_f32<T>) {
+    float worst[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
+    for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) worst[i % 4] = fmaf(acc[0][cb][i], 0.0f, worst[i % 4]);
-  const bool bad = __any(!((worst[0] + worst[1]) + (worst[2] + worst[3]) == 0.0f));
-  if (lane == 0) sh_bad[wv] = bad;
-  __syncthreads();
-  if (sh_bad[0] | sh_bad[1] | sh_bad[2] | sh_bad[3]) {
+      for (int i = 0; i < 16; ++i) worst[i % 4] = fmaf(acc[0][cb][i], 0.0f, worst[i % 4]);
+    const bool bad = __any(!((worst[0] + worst[1]) + (worst[2] + worst[3]) == 0.0f));
+    if (lane == 0) sh_bad[wv] = bad;
+    __syncthreads();
+    if (sh_bad[0] | sh_bad[1] | sh_bad[2] | sh_bad[3]) {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      floatx16 o = floatx16{0};
-      __syncthreads();
-      load(0);
+      for (int cb = 0; cb < CB; ++cb) {
+        floatx16 o = floatx16{0};
+        __syncthreads();
+        load(0);
 #pragma nounroll
-      for (int t = 0; t < tiles; ++t) {
-        await(t);
-        if (idle) continue;
+        for (int t = 0; t < tiles; ++t) {
+          await(t);
+          if (idle) continue;
 #pragma nounroll
-        for (int kk = wv % KS; kk < KT / 32; kk += KS) {
-          if (n - t * KT - 32 * kk <= 0) break;
-          // (the rows past the end repeat the last one, so their weights may stay)
-          const floatx16 sc = tile_logits<T, TL>(place_of.keys(t) + kk * 32 * CH, qf, l32, half);
-          float pr[16];
-          weigh(sc, pr);
-          if constexpr (is_f16<T>) {                           // (none is too small for the type)
+          for (int kk = wv % KS; kk < KT / 32; kk += KS) {
+            if (n - t * KT - 32 * kk <= 0) break;
+            // (the rows past the end repeat the last one, so their weights may stay)
+            const floatx16 sc = tile_logits<T, TL>(place_of.keys(t) + kk * 32 * CH, qf, l32, half);
+            float pr[16];
+            weigh(sc, pr);
+            if constexpr (is_f16<T>) {                           // (none is too small for the type)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) pr[i] = pr[i] > 0.0f ? fmaxf(pr[i], 0x1p-24f) : pr[i];
+              for (int i = 0; i < 16; ++i) pr[i] = pr[i] > 0.0f ? fmaxf(pr[i], 0x1p-24f) : pr[i];
+            }
+            W w;
+            w.set(pr);
+            w.add_first(o, place_of.values(t) + kk * 32 * CH, lane, cb);
           }
-          W w;
-          w.set(pr);
-          w.add_first(o, place_of.values(t) + kk * 32 * CH, lane, cb);
         }
-      }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[0][cb][i] = __builtin_fabsf(acc[0][cb][i]) < INFINITY ? acc[0][cb][i] : o[i];
+        for (int i = 0; i < 16; ++i) acc[0][cb][i] = __builtin_fabsf(acc[0][cb][i]) < INFINITY ? acc[0][cb][i] : o[i];
+      }
     }
   }
   m -= BIAS<T>;
@@ -823,9 +822,9 @@ PrefixPlan plan_prefix(const SeqTab &st, const Dims &dm, int dtype, int headroom
   // 64 sequences over 32768 rows with 500 own rows 85.7 | 99.5, with none 82.7 | 77.5; 8 over 32768 29.3 | 34.5 (320 parts), and with 192 33.7.
   const long long want = 256;
   pl.split.spare = (int)(want > n / 2 + 1 ? want : n / 2 + 1);
-  // sums of a block's rows, written and read at 5 TB/s, over a tile of 64 rows' (or 128 of 128 bytes) time in a workgroup
+  // sums of a block's rows, written and read at 5 TB/s, over a tile's time in a workgroup (Rows)
   const int sum_rows = most < rb ? most : rb;
-  const float tile_us = !wide ? 1.0f : (dm.d == 64 ? 3.0f : 6.0f) * (rb == 16 ? 0.25f : 1.0f);
+  const float tile_us = !wide ? 1.0f : (dm.d == 64 || rb == 128 ? 3.0f : 6.0f) * (rb == 16 ? 0.25f : 1.0f);
   pl.split.sums_cost = sum_rows * (dm.d + 2) * 8.0f / 5.0e6f / tile_us;
   pl.split.shared_blocks = (int)(n ? pl.split.spare + n + padding : 0);
   const int tile = dm.d == 64 && !wide ? 128 : 64;

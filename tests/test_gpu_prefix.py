@@ -288,8 +288,8 @@ def test_logits_of_two_to_the_26(dtype, batch):
         assert ((lse[b].double().cpu() - 2.0 ** 26).abs() <= 16).all()
 
 
-@pytest.mark.parametrize("batch", [2, 8, 20])
-@pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 64), (FH, 128), (FS, 64)])
+@pytest.mark.parametrize("batch", [2, 8, 12, 20])
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FH, 64), (FH, 128), (FS, 64), (FS, 128)])
 def test_values_that_are_no_numbers(dtype, d, batch):
     """An infinite value makes its column infinite, NaN (or infinities of both signs) NaN; other columns and heads stay."""
     c = Case(dtype, 4, 2, d, [0] * (batch - 1) + [-1], [333, 100], [20] * (2 * batch), seed=3)
