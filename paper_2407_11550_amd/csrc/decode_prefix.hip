@@ -504,7 +504,7 @@ __device__ __forceinline__ void sum_part(const Sharing &sh, const Part &pt, int 
 }
 
 // The same in 32 bits for no more than 16 query rows, each wavefront on 16 keys of a tile (32 keys of two wavefronts times 32 query rows, of which half
-// or more are none: 64 sequences of 500 own rows, 8 heads of 128, g = 4 100 us, now 61, 4.3 TB/s).  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
+// or more are none: 64 sequences of 500 own rows, 8 heads of 128, g = 4 100 us, now 54, 4.9 TB/s).  A lane has query lane % 16, of the logits those of keys 4 (lane / 16)
 // on, and of each value row 16 bytes: what they add to are columns 4 apart, so that what a lane has of a query in the end are 16 bytes again.
 template <int D, int TURNS>
 __device__ __forceinline__ void sum_few(const Sharing &sh, const Part &pt, int order, float c_log2, const char *q, const Segments &seg, float *part_acc, float2 *part_ml,
