@@ -451,9 +451,10 @@ int adakv_rotary_frequencies(int32_t dims, double base, int32_t scaling, double 
  *   k, k_out     (host)   [rows][h_kv][d]; both NULL: only q is turned.  (k_out with L's strides of K is what adakv_score and
  *                         adakv_window_attn read)
  * An output may be its own input, at the same address and with the same strides (else ADAKV_EINVAL); no other element of
- * an output may be one of an input, or of another place of an output: either a token's heads lie within stride_tok, or a head's tokens
- * within stride_head (else ADAKV_EINVAL).
- * Supported (else ADAKV_EUNSUPPORTED): up to 2^30 rows in all.
+ * an output may be one of an input (positions and freq included), or of another place of an output: either a token's heads lie within
+ * stride_tok, or a head's tokens within stride_head (else ADAKV_EINVAL).  Rows that are left out by their position count, rows of no sequence do not.
+ * Supported (else ADAKV_EUNSUPPORTED): up to 2^30 rows in all; 1024 heads where an output lies between the elements of another tensor that
+ * has other strides.
  */
 int adakv_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows,
                  const int32_t *positions, const adakv_heads *q, const adakv_heads *k,

@@ -7,6 +7,7 @@
 
 #include "common.h"
 #include "decode_prefix.h"
+#include "places.h"
 
 namespace adakv {
 
@@ -580,6 +581,34 @@ static int check_heads(const adakv_heads *x, const adakv_heads *o, long long row
   return ADAKV_OK;
 }
 
+// Whether an output has memory of another tensor of the call, which is rows of `x_count` heads or, with x_count == 0, `piece` bytes at x->x.
+// `rows` rows; without positions only st's sequences' count.
+static int check_apart(const SeqTab &st, const Dims &dm, long long rows, bool positions, int esz, const adakv_heads *o, int o_count,
+                       const adakv_heads *x, int x_count, long long piece = 0) {
+  const auto places = [&](const adakv_heads *t, int count, long long from, long long n) {
+    if (count == 0) return Places((uintptr_t)t->x, piece);
+    const long long tok = t->stride_tok * esz, head = t->stride_head * esz;
+    return Places((uintptr_t)t->x + (uintptr_t)from * (uintptr_t)tok, (long long)dm.d * esz, {n, tok}, {count, head});
+  };
+  const auto said = [](Meet m) { return m == Meet::NO ? ADAKV_OK : m == Meet::YES ? ADAKV_EINVAL : ADAKV_EUNSUPPORTED; };
+  const Meet all = meet_places(places(o, o_count, 0, rows), places(x, x_count, 0, rows));
+  if (all == Meet::NO || positions) return said(all);
+  // what meets may be rows of no sequence: once more by the runs of sequences one behind the other
+  long long from[ADAKV_MAX_BATCH], n[ADAKV_MAX_BATCH];
+  int runs = 0;
+  for (int b = 0; b < st.batch; ++b) {
+    const long long mine = (long long)st.n[b] + dm.w;
+    if (runs && from[runs - 1] + n[runs - 1] == st.tok_off[b]) n[runs - 1] += mine;
+    else from[runs] = st.tok_off[b], n[runs++] = mine;
+  }
+  for (int i = 0; i < runs; ++i)
+    for (int j = 0; j < (x_count ? runs : 1); ++j) {
+      const Meet m = meet_places(places(o, o_count, from[i], n[i]), places(x, x_count, from[j], n[j]));
+      if (m != Meet::NO) return said(m);
+    }
+  return ADAKV_OK;
+}
+
 // (both forms)
 static int rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, const int32_t *positions, const adakv_heads *q,
                   const adakv_heads *k, const adakv_heads *q_out, const adakv_heads *k_out, bool norm, const void *q_weight,
@@ -608,6 +637,27 @@ static int rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, c
   const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
   if (q && (rc = check_heads(q, q_out, reach, dm.h_q, dm.d, esz)) != ADAKV_OK) return rc;
   if (k && (rc = check_heads(k, k_out, reach, dm.h_kv, dm.d, esz)) != ADAKV_OK) return rc;
+  const auto apart = [&](const adakv_heads *o, int o_count, const adakv_heads *x, int x_count, long long piece = 0) {
+    if (rc == ADAKV_OK && o && x) rc = check_apart(st, dm, reach, positions != nullptr, esz, o, o_count, x, x_count, piece);
+  };
+  const auto piece_apart = [&](const void *x, long long bytes) {
+    const adakv_heads at = {const_cast<void *>(x), 0, 0};
+    if (!x || !bytes) return;
+    apart(q_out, dm.h_q, &at, 0, bytes);
+    apart(k_out, dm.h_kv, &at, 0, bytes);
+  };
+  if (q && q_out->x != q->x) apart(q_out, dm.h_q, q, dm.h_q);  // (at one address all places are alike)
+  if (k && k_out->x != k->x) apart(k_out, dm.h_kv, k, dm.h_kv);
+  apart(q_out, dm.h_q, k, dm.h_kv);
+  apart(k_out, dm.h_kv, q, dm.h_q);
+  apart(q_out, dm.h_q, k_out, dm.h_kv);
+  piece_apart(positions, rows * (long long)sizeof(int32_t));
+  piece_apart(R->freq, R->dims / 2 * (long long)sizeof(double));
+  if (norm) {
+    piece_apart(q_weight, q ? (long long)dm.d * esz : 0);
+    piece_apart(k_weight, k ? (long long)dm.d * esz : 0);
+  }
+  if (rc != ADAKV_OK) return rc;
   if (norm && (!aligned16(q_weight) || !aligned16(k_weight))) return ADAKV_EUNSUPPORTED;
   if (((uintptr_t)R->freq & 7u) != 0 || ((uintptr_t)positions & 3u) != 0) return ADAKV_EUNSUPPORTED;
   hipError_t e = launch_rotary(st, dm, L->dtype, *R, (int)all, positions, q, k, q_out, k_out, norm, q_weight, k_weight, eps,
