@@ -64,6 +64,14 @@ __device__ __forceinline__ int wave_sum(int x) {       // the same in all lanes
   return __builtin_amdgcn_readlane(wave_scan_incl(x), 63);
 }
 
+// What lanes of this wavefront have written to LDS is there for its other lanes to read, and they have read what is written over next.  LDS takes a
+// wavefront's accesses in their order, so this is no instruction; but only the fences keep the compiler from another order.
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct Dims {

@@ -148,14 +148,14 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
         const float2 v = cos_sin(pos, f);
         sh_cs[wv][lane] = make_float2(v.x * magnitude, v.y * magnitude);
       }
-      __builtin_amdgcn_wave_barrier();
+      lanes_meet();
 #pragma unroll
       for (int e = 0; e < MINE; ++e) {
         const float2 v = sh_cs[wv][WAY == SHIFTED ? min(pair(e), D / 2 - 1) : pair(e)];
         cs[e] = v.x;
         sn[e] = v.y;
       }
-      __builtin_amdgcn_wave_barrier();
+      lanes_meet();
     }
     for (int h0 = from; h0 < end; h0 += HPW * U) {
       Word xa[U], xb[U];
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
             const auto place = [](int at) { return at + at / E; };
 #pragma unroll
             for (int e = 0; e < 2 * E; ++e) mine[place(e < E ? ea + e : eb + e - E)] = x[e];
-            __builtin_amdgcn_wave_barrier();
+            lanes_meet();
 #pragma unroll
             for (int e = 0; e < 2 * E; ++e) {
               const int at = e < E ? ea + e : eb + e - E;
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rows rows, Heads q, Heads k
               const float y = fmaf(x[e], cs[e], at < half ? -other * sn[e] : other * sn[e]);
               x[e] = at < dims ? y : x[e];
             }
-            __builtin_amdgcn_wave_barrier();
+            lanes_meet();
           } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
