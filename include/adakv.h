@@ -430,7 +430,7 @@ typedef struct {
  *   freq (host) [dims/2], written
  * Returns ADAKV_EINVAL for a NULL freq, dims odd or below 2, a base not above 0, an unknown scaling, and where the scaling uses them, factor < 1,
  * original_len < 1, low < 0 or high <= low; also for
- * numbers that are not finite, the stretched base among them.  ADAKV_EUNSUPPORTED for dims > 128.
+ * numbers that are not finite, the stretched base and the frequencies among them.  ADAKV_EUNSUPPORTED for dims > 128.
  */
 int adakv_rotary_frequencies(int32_t dims, double base, int32_t scaling, double factor,
                              int32_t original_len, double low, double high, double *freq);

@@ -552,7 +552,7 @@ int adakv_rotary_frequencies(int32_t dims, double base, int32_t scaling, double 
   if (scaling == ADAKV_ROTARY_PARTS && (original_len < 1 || !(low >= 0.0) || !(high > low) || isinf(high))) return ADAKV_EINVAL;
   if (dims > 128) return ADAKV_EUNSUPPORTED;
   if (scaling == ADAKV_ROTARY_BASE && dims > 2) base *= pow(factor, dims / (dims - 2.0));
-  if (isinf(base)) return ADAKV_EINVAL;
+  if (isinf(base) || isinf(pow(base, 2.0 / dims - 1.0))) return ADAKV_EINVAL;        // (of a base below 1 the last frequency is the largest)
   for (int i = 0; i < dims / 2; ++i) {
     const double f = pow(base, -2.0 * i / dims);
     double by = 1.0;
