@@ -925,8 +925,8 @@ class Rotary:
                  freq=None, device="cuda"):
         if layout not in ROTARY_LAYOUTS:
             raise ValueError(f"layout must be one of {', '.join(ROTARY_LAYOUTS)}, got {layout!r}")
-        if not magnitude > 0:
-            raise ValueError(f"magnitude must be above 0, got {magnitude}")
+        if not ctypes.c_float(magnitude).value > 0:             # (as the library gets it: 0 would mean 1)
+            raise ValueError(f"magnitude must be above 0 in fp32, got {magnitude}")
         self.dims, self.layout, self.magnitude = int(dims), layout, float(magnitude)
         if freq is None:
             made = rotary_frequencies(dims, base, scaling, factor, original_len, low, high) if self.dims else []
