@@ -11,6 +11,7 @@ import importlib.machinery
 import importlib.util
 import itertools
 import os
+import types
 from typing import NamedTuple
 
 import torch
@@ -814,20 +815,29 @@ def window_attn(layer: Layer, q, K, V, window, sinks=0, out=None, row_lse=None, 
     return (out, row_lse) if (want_lse or row_lse is not None) else out
 
 
+class _Fixed:
+    """A description that the library reads at the address it was first given: its attributes stay what they were made."""
+
+    def __setattr__(self, name, value):
+        if "_address" in self.__dict__:
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot be replaced: make another one")
+        super().__setattr__(name, value)
+
+
 # ---- a decoding step over shared caches -------------------------------------------------------------------
-class Prefix:
+class Prefix(_Fixed):
     """Caches that sequences share (adakv_prefix): `layer` describes the shared caches, which are its sequences, the tensors are
     a cache as cache_build makes it, and of[b] is the shared cache of sequence b of the layer that decodes, or -1.  The tensors
-    are read, never written, and may change between calls."""
+    are read, never written, and what they hold may change between calls."""
 
     def __init__(self, layer: Layer, cu_seqlens, headroom, K_cache, V_cache, seg_len, of):
-        self.layer, self.headroom, self.of = layer, int(headroom), [int(p) for p in of]
+        self.layer, self.headroom, self.of = layer, int(headroom), tuple(int(p) for p in of)
         if any(not -1 <= p < layer.batch for p in self.of):
             raise ValueError(f"of must name the shared caches, 0 to {layer.batch - 1}, or -1")
         _check_cache(layer, headroom, K_cache, V_cache)
         _need(cu_seqlens, layer._segments + 1, "cu_seqlens")
         _need(seg_len, layer._segments, "seg_len")
-        self.tensors = dict(cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len)
+        self.tensors = types.MappingProxyType(dict(cu_seqlens=cu_seqlens, K_cache=K_cache, V_cache=V_cache, seg_len=seg_len))
         at = (_ptr(cu_seqlens, "cu_seqlens", torch.int32), _ptr(K_cache, "K_cache", layer.torch_dtype),
               _ptr(V_cache, "V_cache", layer.torch_dtype), _ptr(seg_len, "seg_len", torch.int32))
         self.device = K_cache.get_device()
@@ -917,7 +927,7 @@ def rotary_frequencies(dims, base=10000.0, scaling="none", factor=1.0, original_
     return list(out)
 
 
-class Rotary:
+class Rotary(_Fixed):
     """How heads are turned (adakv_rotation): `dims` elements of each, pairs in the given `layout`, frequencies as
     adakv_rotary_frequencies makes them, or those of the tensor `freq` (float64, [dims/2], on the device)."""
 
