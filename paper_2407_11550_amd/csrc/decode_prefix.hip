@@ -62,8 +62,7 @@ template <typename T, int D, typename TL> struct Weights {
   static constexpr int SUMS = is_f16<T> ? 2 : 1;               // sets of sums
   unsigned w[PARTS][is_f32<T> ? 16 : 8];
 
-  // p: their values; `first` alone: what is needed to know where a product is no finite number
-  __device__ __forceinline__ void set(const float (&p)[16], bool first = false) {
+  __device__ __forceinline__ void set(const float (&p)[16]) {
     if constexpr (is_f32<T>) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) w[0][i] = __float_as_uint(p[i]);
