@@ -581,6 +581,13 @@ static int check_heads(const adakv_heads *x, const adakv_heads *o, long long row
   return ADAKV_OK;
 }
 
+// From its first byte to its last (as far as there are addresses).
+static Range reach_of(const adakv_heads *x, long long rows, int count, int d, int esz) {
+  if (!x || rows < 1) return {nullptr, 0};
+  const wide bytes = ((wide)(rows - 1) * x->stride_tok + (wide)(count - 1) * x->stride_head + d) * esz, most = UINTPTR_MAX - (uintptr_t)x->x;
+  return {x->x, (size_t)(bytes < most ? bytes : most)};
+}
+
 // Whether an output has memory of another tensor of the call, which is rows of `x_count` heads or, with x_count == 0, `piece` bytes at x->x.
 // `rows` rows; without positions only st's sequences' count.
 static int check_apart(const SeqTab &st, const Dims &dm, long long rows, bool positions, int esz, const adakv_heads *o, int o_count,
@@ -590,6 +597,12 @@ static int check_apart(const SeqTab &st, const Dims &dm, long long rows, bool po
     const long long tok = t->stride_tok * esz, head = t->stride_head * esz;
     return Places((uintptr_t)t->x + (uintptr_t)from * (uintptr_t)tok, (long long)dm.d * esz, {n, tok}, {count, head});
   };
+  if (x_count && o->stride_tok == x->stride_tok) {             // parts of one tensor's rows: their places within a row tell
+    const bool o_first = (uintptr_t)o->x <= (uintptr_t)x->x;
+    const uintptr_t tok = (uintptr_t)(o->stride_tok * esz), apart = o_first ? (uintptr_t)x->x - (uintptr_t)o->x : (uintptr_t)o->x - (uintptr_t)x->x;
+    const wide o_row = ((wide)(o_count - 1) * o->stride_head + dm.d) * esz, x_row = ((wide)(x_count - 1) * x->stride_head + dm.d) * esz;
+    if ((o_first ? o_row : x_row) <= apart % tok && apart % tok + (o_first ? x_row : o_row) <= tok) return ADAKV_OK;
+  }
   const auto said = [](Meet m) { return m == Meet::NO ? ADAKV_OK : m == Meet::YES ? ADAKV_EINVAL : ADAKV_EUNSUPPORTED; };
   const Meet all = meet_places(places(o, o_count, 0, rows), places(x, x_count, 0, rows));
   if (all == Meet::NO || positions) return said(all);
@@ -637,25 +650,22 @@ static int rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows, c
   const int esz = L->dtype == ADAKV_FP32 ? 4 : 2;
   if (q && (rc = check_heads(q, q_out, reach, dm.h_q, dm.d, esz)) != ADAKV_OK) return rc;
   if (k && (rc = check_heads(k, k_out, reach, dm.h_kv, dm.d, esz)) != ADAKV_OK) return rc;
-  const auto apart = [&](const adakv_heads *o, int o_count, const adakv_heads *x, int x_count, long long piece = 0) {
-    if (rc == ADAKV_OK && o && x) rc = check_apart(st, dm, reach, positions != nullptr, esz, o, o_count, x, x_count, piece);
-  };
-  const auto piece_apart = [&](const void *x, long long bytes) {
-    const adakv_heads at = {const_cast<void *>(x), 0, 0};
-    if (!x || !bytes) return;
-    apart(q_out, dm.h_q, &at, 0, bytes);
-    apart(k_out, dm.h_kv, &at, 0, bytes);
-  };
-  if (q && q_out->x != q->x) apart(q_out, dm.h_q, q, dm.h_q);  // (at one address all places are alike)
-  if (k && k_out->x != k->x) apart(k_out, dm.h_kv, k, dm.h_kv);
-  apart(q_out, dm.h_q, k, dm.h_kv);
-  apart(k_out, dm.h_kv, q, dm.h_q);
-  apart(q_out, dm.h_q, k_out, dm.h_kv);
-  piece_apart(positions, rows * (long long)sizeof(int32_t));
-  piece_apart(R->freq, R->dims / 2 * (long long)sizeof(double));
-  if (norm) {
-    piece_apart(q_weight, q ? (long long)dm.d * esz : 0);
-    piece_apart(k_weight, k ? (long long)dm.d * esz : 0);
+  // outputs against all else: by where they begin and end, and only if these meet, place by place
+  const Range ends[4] = {reach_of(q, reach, dm.h_q, dm.d, esz), reach_of(k, reach, dm.h_kv, dm.d, esz), reach_of(q_out, reach, dm.h_q, dm.d, esz),
+                         reach_of(k_out, reach, dm.h_kv, dm.d, esz)};
+  const adakv_heads *const all_heads[4] = {q, k, q_out, k_out};
+  for (int o = 2; o < 4 && rc == ADAKV_OK; ++o) {
+    const int o_count = o == 2 ? dm.h_q : dm.h_kv;
+    for (int x = 0; x < o && rc == ADAKV_OK; ++x)
+      if (overlap(ends[o], ends[x]) && !(x == o - 2 && ends[x].at == ends[o].at))      // (an output at its input's address has its places)
+        rc = check_apart(st, dm, reach, positions != nullptr, esz, all_heads[o], o_count, all_heads[x], x % 2 == 0 ? dm.h_q : dm.h_kv);
+    const Range pieces[4] = {{positions, positions ? (size_t)rows * sizeof(int32_t) : 0}, {R->freq, (size_t)(R->dims / 2) * sizeof(double)},
+                             {q_weight, norm && q ? (size_t)dm.d * esz : 0}, {k_weight, norm && k ? (size_t)dm.d * esz : 0}};
+    for (const Range &x : pieces)
+      if (rc == ADAKV_OK && x.bytes && overlap(ends[o], x)) {
+        const adakv_heads at = {const_cast<void *>(x.at), 0, 0};
+        rc = check_apart(st, dm, reach, positions != nullptr, esz, all_heads[o], o_count, &at, 0, (long long)x.bytes);
+      }
   }
   if (rc != ADAKV_OK) return rc;
   if (norm && (!aligned16(q_weight) || !aligned16(k_weight))) return ADAKV_EUNSUPPORTED;
