@@ -90,11 +90,14 @@ template <typename T> __device__ __forceinline__ unsigned round2(float x0, float
 }
 
 // 32 keys of a tile times 32 queries, a query per lane (twice: the halves of the wavefront hold different keys, lane `half` of a
-// query those numbered 8 (i / 4) + 4 half + i % 4).
-template <typename T, typename TL>
+// query those numbered 8 (i / 4) + 4 half + i % 4).  In 32 bits a logit is one chain of D / 2 products, or the sum of `CHAINS` shorter ones.
+template <typename T, typename TL, int CHAINS = 1>
 __device__ __forceinline__ floatx16 tile_logits(const u32x4 *tk, const u32x4 (&qf)[TL::CH / 2], int l32, int half) {
   constexpr int CH = TL::CH;
-  floatx16 sc = floatx16{0};
+  static_assert(CHAINS == 1 || (CHAINS == 2 && is_f32<T>), "chains");
+  floatx16 sc[CHAINS];
+#pragma unroll
+  for (int i = 0; i < CHAINS; ++i) sc[i] = floatx16{0};
 #pragma unroll
   for (int s = 0; s < CH / 2; ++s) {
     const u32x4 kw = tk[l32 * CH + ((2 * s + half) ^ TL::swz_k(l32))];
@@ -102,13 +105,14 @@ __device__ __forceinline__ floatx16 tile_logits(const u32x4 *tk, const u32x4 (&q
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const unsigned ka = kw[e], qa = qf[s][e];
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc, 0, 0, 0);
+        sc[e % CHAINS] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ka), __builtin_bit_cast(float, qa), sc[e % CHAINS], 0, 0, 0);
       }
     } else {
-      sc = product<T>(kw, qf[s], sc);
+      sc[0] = product<T>(kw, qf[s], sc[0]);
     }
   }
-  return sc;
+  if constexpr (CHAINS == 2) return sc[0] + sc[1];
+  else return sc[0];
 }
 
 }  // namespace

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2407_11550_amd as adakv
 from oracle import decode_oracle as D
 from oracle import serve_oracle as S
 from prefix_parts import own_parts, plan, shared_parts
@@ -127,3 +128,21 @@ def test_shared_parts_that_are_made_longer(dtype, d, g, h, batch, groups, rows, 
     check_some(c, out, lse, c.own, [0, batch // 2, batch - 1], heads)
     some = [b for b in range(batch) if of[b] == of[0]][-1]                      # (the last block of rows)
     check_some(c, out, lse, c.own, [some], heads)
+
+
+@pytest.mark.parametrize("batch,chains", [(2, 4), (12, 2), (40, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_are_sums_of_short_chains(d, batch, chains):
+    """2^24, then d - 2 products of 1 + 2^-4, then -2^24, in 32 bits: a chain that begins with 2^24 is off by nearly 1, half a step, with every
+    product.  There are d / chains in it, and 2 roundings join the chains; own segments have four chains everywhere."""
+    for of, lens, most in ((0, ([1], [0] * batch), d / chains), (-1, ([1], [1] * batch), d / 4)):
+        c = Case(FS, 4, 1, d, [of] * batch, *lens)
+        c.layer = adakv.Layer(FS, 4, 1, d, 1, 7, 0.2, [1] * batch, [1] * batch, scale=1.0)
+        row = torch.ones(d, device=DEV)
+        row[0], row[-1] = 2.0 ** 12, -2.0 ** 12
+        c.q[:] = 1 + 2.0 ** -4
+        c.q[..., 0] = c.q[..., -1] = 2.0 ** 12
+        (c.pK if of == 0 else c.K).copy_(row)
+        out, lse = c.attn()
+        print(f"  of {of}: off by {float((lse - (d - 2) * 1.0625).abs().max())}, at most {most + 2}", flush=True)
+        assert ((lse.double() - (d - 2) * 1.0625).abs() <= most + 2).all()
