@@ -426,7 +426,8 @@ typedef struct {
  *     BASE     those of the base  base * factor^(dims/(dims-2))  (dims = 2: the one frequency is 1)
  *     PARTS    freq[i] * (u + (1 - u)/factor),  u = (original_len * freq[i] / (2 pi) - low) / (high - low) held to 0..1: what
  *              turns `high` times within the original length and more keeps its frequency, what turns `low` times or less is as with
- *              LINEAR (with such a schedule a magnitude of 1 + 0.1 ln(factor) is usual)
+ *              LINEAR (with such a schedule a magnitude of 1 + 0.1 ln(factor) is usual).  u goes by turns; frequencies whose u goes by the pairs' numbers, or
+ *              any others, are the caller's to make: the calls below take what is in freq
  *   freq (host) [dims/2], written
  * Returns ADAKV_EINVAL for a NULL freq, dims odd or below 2, a base not above 0, an unknown scaling, and where the scaling uses them, factor < 1,
  * original_len < 1, low < 0 or high <= low; also for
@@ -462,7 +463,8 @@ int adakv_rotary(const adakv_layer *L, const adakv_rotation *R, int64_t rows,
 
 /*
  * The same behind a norm of every head: x / sqrt(mean of the squares of its d elements + eps), times a weight for each element,
- * is what is turned.  Squares are summed in fp32: elements of 2^60 and more may give zeros or NaN, as a head of zeros does with eps = 0.
+ * is what is turned.  Squares are summed in fp32: heads with elements of 2^60 and more may give zeros or NaN, and
+ * with eps = 0 those of none above 2^-50 infinities or NaN, as a head of zeros does.
  *
  *   q_weight, k_weight (device) [d] L->dtype, 16-byte aligned; each may be NULL if its q or k is
  *   eps                >= 0 and finite (else ADAKV_EINVAL)

@@ -12,9 +12,10 @@
 // share 32 of them; 16 rows in 32 bits) and files the sums.  A second kernel merges, for each query head, the parts of its own segment and of the shared one, and
 // the row that the call appends, which it also puts into the cache.
 //
-// Bound by HBM while few sequences share a cache (8 sequences with 700 to 900 own rows over 3 caches of 16384 rows, 64 query heads: attention 33 us, 5.8
-// TB/s), by the matrix units where many do (64 over one cache of 32768 rows, 8 heads of 128, g = 4, bf16: 85 us, 70 GFLOP of matrix work with the
-// three parts of the weights), and by its two launches and a workgroup's start where there is little to do (2 over 541 rows: 6.6 us and 4.5).
+// Bound by HBM while few sequences share a cache (8 sequences with 700 to 900 own rows over 3 caches of 16384 rows, 64 query heads: attention 34 us, 5.7
+// TB/s), by matrix and vector instructions that take turns where many do (64 over one cache of 32768 rows, 8 heads of 128, g = 4, bf16: 86 us and, when the clock falls, up to 119; 70 GFLOP of
+// matrix work with the three parts of the weights; matrix units busy for 39 %, vector units for 39 %, both for 15 %), and by its two launches and a workgroup's start where there is
+// little to do (2 over 541 rows: 7.3 us and 5.0).
 #include <math.h>
 
 #include "attn_tiles.h"
@@ -199,7 +200,7 @@ __device__ __forceinline__ bool find_shared(const Sharing &sh, int blk, int spar
     upto = wave_scan_incl(parts);
     const int last = __shfl(upto, min(lane * h + h - 1, 63)), before = __shfl(upto, max(min(lane * h, 64) - 1, 0));
     my_parts = lane < groups ? last - (lane ? before : 0) : 0;
-  } else {
+  } else {                                     // (not so here: each turn would look at every segment again)
     int mine = 0;
 #pragma unroll 4
     for (int c = 0; c < h; ++c) mine += look(min(lane, groups - 1) * h + c);

@@ -246,8 +246,8 @@ void run_rotary(bool neighbours, int dims, Rows rows, const Heads &q, const Head
                 const void *kw, float eps, hipStream_t s) {
   constexpr int E = 16 / (int)sizeof(T);
   // A wavefront takes a row, and where there are fewer rows than the chip holds wavefronts (a batch's new tokens), some of its heads.  64 rows of 72
-  // heads, bf16, d = 128, behind a norm: 8.3 us a call with a row each, 4.6 with 8 heads each; 1021 rows of 10 fp32 heads, halves that are not aligned:
-  // 6.4 and 5.6 with two each.
+  // heads, bf16, d = 128, behind a norm: 7.6 us a call with a row each, 5.1 with 8 heads each; 1021 rows of 10 fp32 heads, halves that are not aligned, where there is
+  // little to share: 5.7 and 5.9 with four each.
   const int at_a_time = 64 / (D / 2 / E), heads = q.count + k.count;
   const int pieces = (heads + at_a_time - 1) / at_a_time, most = 8192 / rows.total;
   rows.share = most <= 1 ? heads : (pieces + most - 1) / most * at_a_time;
