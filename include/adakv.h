@@ -378,7 +378,8 @@ size_t adakv_prefix_workspace_bytes(const adakv_layer *L, int32_t headroom, cons
  *     out[b][i][:] = sum_t softmax_t(scale * q_new[b][i] . k_t) v_t,   lse[b][i] = ln sum_t exp(scale * q_new[b][i] . k_t)
  *
  * with L's scale.  No rows at all give a zero row and lse = -inf.  fp16 layers hold a softmax weight in 22 bits down to 2^-23 of the
- * largest in its part of a segment, and to 2^-45 of it beyond.  Logits and values that are no finite numbers, the
+ * largest in its part of a segment, and to 2^-45 of it beyond.  In the other types a row's part of a sum is held to 2^-135, so that results below
+ * 2^-110 have fewer than 24 bits.  Logits and values that are no finite numbers, the
  * appended row, seg_len and overflow, and the other arguments: as for adakv_decode_attn and adakv_decode_step.  In a step the shared
  * caches and their seg_len are no part of the layer's own (ADAKV_EINVAL).
  *   ws (device) adakv_prefix_workspace_bytes(L, headroom, P) bytes
